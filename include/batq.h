@@ -387,6 +387,105 @@ batq_status batq_kv_append(const batq_transform* t, const void* X, batq_dtype xd
 batq_status batq_kv_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t capacity_rows, int64_t row_offset,
                                int M, int K, int bits, void* out, batq_dtype odtype, int64_t ldo, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * Paged 8-bit key/value cache (Sec. 3.2, "Self-Attention Module", for many sequences at once).
+ * Keys and values of all sequences live in pages of page_size tokens; a sequence owns any pages, in any order, and a
+ * table lists them.  The arrays (DEVICE, caller-owned, 16-byte aligned) hold per page:
+ *   codes   [kv_heads][page_size][head_dim] E4M3 bytes, batq_kv_paged_code_bytes() in all
+ *   scales  [kv_heads][head_dim / 32][page_size] E8M0 bytes, batq_kv_paged_scale_bytes() in all
+ * A block is one token's 32 channels, quantised exactly as batq_kv_append with act_bits 8 does, so a token's bytes do
+ * not depend on the call or the order that brought it.  head_dim is 64 or 128, page_size 16, 32, 64, 128 or 256, and
+ * num_pages * page_size may pass 2^31.  The size functions return 0 for invalid arguments. */
+typedef struct {
+    int num_pages, page_size, kv_heads, head_dim;
+    uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+} batq_paged_cache;
+size_t batq_kv_paged_code_bytes(int num_pages, int page_size, int kv_heads, int head_dim);
+size_t batq_kv_paged_scale_bytes(int num_pages, int page_size, int kv_heads, int head_dim);
+
+/* Rotation by position: row p of `table` (DEVICE fp32, 16-byte aligned, [positions][rotary_dim]) holds the cosines of
+ * the rotary_dim / 2 angles of position p and then their sines.  The first rotary_dim channels of a head (a multiple of
+ * 16, at most head_dim) are rotated in pairs: channels (j, j + rotary_dim / 2), or (2 j, 2 j + 1) if interleaved != 0;
+ * pair (a, b) becomes (fl(fl(a cos) - fl(b sin)), fl(fl(b cos) + fl(a sin))) in fp32. */
+typedef struct {
+    const float* table;
+    int positions, rotary_dim, interleaved;
+} batq_rope;
+
+/* The step between a fused projection and the attention, for M tokens of any sequences:
+ *   keys    k (M x kv_heads * head_dim) are rotated, transformed (k T_k), clipped and quantised into the cache;
+ *   values  v (likewise) are transformed (v T_v), clipped and quantised into the cache;
+ *   queries q (M x q_heads * head_dim; NULL with q_heads 0: none) are rotated, take T_k^-T of the key head they read
+ *           ((q T^-T)(k T)^T = q k^T; q_heads is a multiple of kv_heads, query head h reads key head
+ *           h / (q_heads / kv_heads)) and are rounded once to bf16 into q_out.
+ *   tk, tv  transforms of width kv_heads * head_dim, or NULL (no transform, no clipping)
+ *   rope    NULL: no rotation; `positions` (DEVICE int32 [M]) is then not read and may be NULL
+ *   slots   DEVICE int64 [M]: token m goes to offset slots[m] % page_size of page slots[m] / page_size.
+ *           A slot outside [0, num_pages * page_size) leaves the cache as it is (a padding token: its query is still
+ *           written).  A token whose position is outside the table is left out: neither cache nor q_out are written.
+ *           The slots of a call must differ: what one holds that two tokens were written to is unspecified.
+ * q, k, v share xdtype (bf16 or fp32) and may be column ranges of one tensor; all pointers and row pitches are 16-byte
+ * aligned (slots 8-byte, positions 4-byte).  q_out must not overlap q.  The products of the transform are carried to
+ * fp32 accuracy: rotated values are not rounded to 16 bits.  M == 0 is a no-op.
+ * BATQ_ERR_MISMATCH: tk or tv has another width. */
+batq_status batq_kv_paged_append(const batq_paged_cache* cache, const batq_transform* tk, const batq_transform* tv,
+                                 const batq_rope* rope, const void* q, int64_t ldq, int q_heads, void* q_out,
+                                 int64_t ldq_out, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                 batq_dtype xdtype, const int32_t* positions, const int64_t* slots, int M,
+                                 void* stream);
+
+/* Attention of a ragged batch over the paged cache.  Sequence b holds kv_len[b] tokens in pages page_table[b][0 ..],
+ * and its queries are rows cu_q[b] .. cu_q[b + 1] - 1 of q: its last cu_q[b + 1] - cu_q[b] tokens (already appended).
+ *   o_i = sum_t p_t v_t,  p = softmax over the visible t of scale * (q_i . k_t),  lse_i = log sum_t exp(scale * (q_i . k_t))
+ * with keys and values as the cache holds them.  A query at position i of its sequence sees t <= i if causal != 0 (else
+ * every t < kv_len) and, with window > 0, only t > i - window.  A query that sees nothing gets zeros and lse -infinity.
+ *   cu_q        DEVICE int32 [batch + 1], not decreasing, from 0 to at most total_q (rows of q, out and lse); rows of no
+ *               sequence are left as they are
+ *   kv_len      DEVICE int32 [batch]
+ *   page_table  DEVICE int32 [batch][table_width]; entries behind a sequence's last page are not read
+ *   max_q, max_kv  bounds of the query and token counts that the call is planned for: of a sequence with more, the
+ *               first max_q queries are served, and it counts as max_kv tokens long
+ * The lists are read on the device and nothing in them is trusted: rows outside total_q, tokens behind table_width
+ * pages and pages outside [0, num_pages) take no part.
+ *   q, out      bf16, total_q x q_heads * head_dim, 16-byte aligned rows; q_heads a multiple of kv_heads, at most
+ *               128 query heads to a key head.  Scores, softmax and sums are fp32; the probabilities are multiplied with
+ *               the values as bf16 (sequences of few queries: as two bf16 terms).
+ *   lse         DEVICE fp32 [total_q][q_heads] or NULL
+ *   workspace   DEVICE, 256-byte aligned, batq_paged_attention_workspace() bytes: partial results of long
+ *               sequences that are cut into parts.  Its contents need not be cleared.
+ * For queries and keys through batq_kv_paged_append with tk, out is in the basis of tv: batq_transform_apply with
+ * BATQ_APPLY_INVERSE takes it back, or T_v^-1 is folded into the output projection offline. */
+typedef struct {
+    const int32_t* cu_q;
+    const int32_t* kv_len;
+    const int32_t* page_table;
+    int batch, table_width, total_q, max_q, max_kv;
+} batq_paged_batch;
+size_t batq_paged_attention_workspace(const batq_paged_cache* cache, int q_heads, int batch, int total_q, int max_q,
+                                      int max_kv);
+batq_status batq_paged_attention(const batq_paged_cache* cache, const batq_paged_batch* b, const void* q, int64_t ldq,
+                                 int q_heads, float scale, int causal, int window, void* out, int64_t ldo, float* lse,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------
+ * Low-rank adapters of many requests beside a shared projection:
+ *   out[m] = base[m] + scales[a] * (X[m] A_a^T) B_a^T,  a = index[m];  out[m] = base[m] if a is outside [0, adapters)
+ *   X        M x K, bf16 or fp32 (the projection's input), K a multiple of 32
+ *   A        DEVICE bf16 [adapters][rank][K], B  DEVICE bf16 [adapters][N][rank]; rank a multiple of 8, at most 128 (pad
+ *            smaller adapters with zeros)
+ *   scales   DEVICE fp32 [adapters] or NULL (1)
+ *   index    DEVICE int32 [M], any order; rows of one adapter side by side are fastest
+ *   base     M x N, bf16 or fp32 (the projection's output), or NULL (0); out: likewise, may be base itself, but must not
+ *            overlap it otherwise, nor X.  One rounding to the output type.
+ * X, A, B 16-byte aligned, row pitch of X a multiple of 16 bytes; base and out aligned to their elements.  The products
+ * are carried to fp32 accuracy (the intermediate X A^T is not rounded to 16 bits).
+ *   workspace  DEVICE, 256-byte aligned, batq_lora_workspace() bytes; its contents need not be cleared. */
+size_t batq_lora_workspace(int M, int K, int N, int rank, int adapters);
+batq_status batq_lora_add(const void* X, batq_dtype xdtype, int M, int K, int64_t ldx, const void* A, const void* B,
+                          int N, int rank, int adapters, const float* scales, const int32_t* index, const void* base,
+                          int64_t ldb, void* out, int64_t ldo, batq_dtype ydtype, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -75,6 +75,13 @@ SYMBOLS = {
     "batq_kv_append": (_i, [_vp, _vp, _i, _i, _i, _i64, _i, _vp, _vp, _i64, _i64, _vp]),
     "batq_kv_dequantize": (_i, [_vp, _vp, _i64, _i64, _i, _i, _i, _vp, _i, _i64, _vp]),
     "batq_transform_apply": (_i, [_vp, _vp, _i, _i, _i, _i64, _i, _vp, _i, _i64, _vp]),
+    "batq_kv_paged_code_bytes": (_sz, [_i, _i, _i, _i]),
+    "batq_kv_paged_scale_bytes": (_sz, [_i, _i, _i, _i]),
+    "batq_kv_paged_append": (_i, [_vp, _vp, _vp, _vp, _vp, _i64, _i, _vp, _i64, _vp, _i64, _vp, _i64, _i, _vp, _vp, _i, _vp]),
+    "batq_paged_attention_workspace": (_sz, [_vp, _i, _i, _i, _i, _i]),
+    "batq_paged_attention": (_i, [_vp, _vp, _vp, _i64, _i, C.c_float, _i, _i, _vp, _i64, _vp, _vp, _sz, _vp]),
+    "batq_lora_workspace": (_sz, [_i, _i, _i, _i, _i]),
+    "batq_lora_add": (_i, [_vp, _i, _i, _i, _i64, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _i64, _vp, _i64, _i, _vp, _sz, _vp]),
 }
 
 
@@ -612,3 +619,182 @@ def batq_linear_ex(t: Transform, w: Weight, X, act_bits: int = 4, row_scale=None
                               _dtype_code(Y), Y.stride(0) if M > 1 else max(w.N, Y.stride(0)),
                               workspace.data_ptr(), workspace.numel(), _stream()), "batq_linear_ex")
     return Y
+
+
+# ---- serving: paged 8-bit cache, attention over it, low-rank adapters
+class _CacheDesc(C.Structure):
+    """batq_paged_cache of include/batq.h."""
+    _fields_ = [("num_pages", _i), ("page_size", _i), ("kv_heads", _i), ("head_dim", _i),
+                ("k_codes", _vp), ("k_scales", _vp), ("v_codes", _vp), ("v_scales", _vp)]
+
+
+class _Rope(C.Structure):
+    """batq_rope of include/batq.h."""
+    _fields_ = [("table", _vp), ("positions", _i), ("rotary_dim", _i), ("interleaved", _i)]
+
+
+class _PagedBatch(C.Structure):
+    """batq_paged_batch of include/batq.h."""
+    _fields_ = [("cu_q", _vp), ("kv_len", _vp), ("page_table", _vp), ("batch", _i), ("table_width", _i), ("total_q", _i),
+                ("max_q", _i), ("max_kv", _i)]
+
+
+def _on_current_device(*tensors):
+    """The library launches on the current device and the current stream of it: every tensor has to live there."""
+    import torch
+    dev = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and not (t.is_cuda and t.get_device() == dev):
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+
+
+def _rows(t, width: int, what: str) -> int:
+    """The row pitch of a 2-D tensor of `width` columns with unit column stride."""
+    if t.dim() != 2 or t.shape[1] != width or (t.stride(1) != 1 and width > 1):
+        raise ValueError(f"{what}: expected [rows, {width}] with unit column stride, got {tuple(t.shape)} with strides {t.stride()}")
+    return t.stride(0) if t.shape[0] > 1 else max(width, t.stride(0))
+
+
+def _list(t, dtype, shape, what: str):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+
+
+class PagedCache:
+    """The arrays of a paged MXFP8 key/value cache (batq_paged_cache): ``k_codes`` and ``v_codes``
+    [pages, kv_heads, page_size, head_dim], ``k_scales`` and ``v_scales`` [pages, kv_heads, head_dim / 32, page_size],
+    uint8.  Allocated on the current device, or ``tensors`` in that order: codes, scales of the keys, of the values."""
+
+    def __init__(self, num_pages: int, page_size: int, kv_heads: int, head_dim: int, tensors=None):
+        import torch
+        self.num_pages, self.page_size, self.kv_heads, self.head_dim = num_pages, page_size, kv_heads, head_dim
+        if not lib.batq_kv_paged_code_bytes(num_pages, page_size, kv_heads, head_dim):
+            raise ValueError(f"a paged cache of {num_pages} pages of {page_size} tokens, {kv_heads} heads of {head_dim} channels is not supported")
+        codes, scales = (num_pages, kv_heads, page_size, head_dim), (num_pages, kv_heads, head_dim // 32, page_size)
+        if tensors is None:
+            tensors = [torch.zeros(s, dtype=torch.uint8, device="cuda") for s in (codes, scales, codes, scales)]
+        for t, shape in zip(tensors, (codes, scales, codes, scales)):
+            _list(t, torch.uint8, shape, "cache")
+        _on_current_device(*tensors)
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = tensors
+        self._d = _CacheDesc(num_pages, page_size, kv_heads, head_dim, *(t.data_ptr() for t in tensors))
+
+    @property
+    def desc(self):
+        return C.byref(self._d)
+
+
+def batq_kv_paged_append(cache: PagedCache, k, v, slots, positions=None, q=None, q_out=None, rope=None,
+                         interleaved: bool = False, tk: Optional[Transform] = None, tv: Optional[Transform] = None):
+    """Rotate (``rope``: fp32 table [positions, rotary_dim], cosines then sines), transform and quantise the keys and
+    values of M tokens into the cache at ``slots`` (int64 [M], outside the cache: not written), and rotate and transform
+    their queries.  k, v: [M, kv_heads * head_dim], q: [M, q_heads * head_dim] or None.  Returns q_out (bf16)."""
+    import torch
+    D, M = cache.head_dim, k.shape[0]
+    width = cache.kv_heads * D
+    ldk, ldv = _rows(k, width, "k"), _rows(v, width, "v")
+    if v.shape[0] != M or v.dtype != k.dtype:
+        raise ValueError("k and v differ in rows or type")
+    _list(slots, torch.int64, (M,), "slots")
+    r = None
+    if rope is not None:
+        if positions is None:
+            raise ValueError("a rotation needs positions")
+        if rope.dim() != 2:
+            raise ValueError("rope: expected [positions, rotary_dim]")
+        _list(rope, torch.float32, rope.shape, "rope")
+        _list(positions, torch.int32, (M,), "positions")
+        r = C.byref(_Rope(rope.data_ptr(), rope.shape[0], rope.shape[1], int(interleaved)))
+    q_heads = ldq = ldq_out = 0
+    if q is not None:
+        q_heads = q.shape[1] // D
+        ldq = _rows(q, q_heads * D, "q")
+        if q.shape[0] != M or q.dtype != k.dtype:
+            raise ValueError("q and k differ in rows or type")
+        if q_out is None:
+            q_out = torch.empty((M, q_heads * D), dtype=torch.bfloat16, device=q.device)
+        ldq_out = _rows(q_out, q_heads * D, "q_out")
+        if q_out.shape[0] != M or q_out.dtype != torch.bfloat16:
+            raise ValueError("q_out: expected bf16 with the rows of q")
+    _on_current_device(cache.k_codes, k, v, slots, positions if r is not None else None, rope, q, q_out)
+    _check(lib.batq_kv_paged_append(cache.desc, tk.handle if tk is not None else None, tv.handle if tv is not None else None, r,
+                                    q.data_ptr() if q is not None else None, ldq, q_heads,
+                                    q_out.data_ptr() if q is not None else None, ldq_out, k.data_ptr(), ldk, v.data_ptr(), ldv,
+                                    _dtype_code(k), positions.data_ptr() if r is not None else None, slots.data_ptr(), M,
+                                    _stream()), "batq_kv_paged_append")
+    return q_out
+
+
+def batq_paged_attention_workspace(cache: PagedCache, q_heads: int, batch: int, total_q: int, max_q: int, max_kv: int) -> int:
+    """Bytes of scratch for batq_paged_attention calls within these bounds on the current device."""
+    return int(lib.batq_paged_attention_workspace(cache.desc, q_heads, batch, total_q, max_q, max_kv))
+
+
+def batq_paged_attention(cache: PagedCache, q, cu_q, kv_len, page_table, max_q: int, max_kv: int, scale: Optional[float] = None,
+                         causal: bool = True, window: int = 0, out=None, lse=None, workspace=None):
+    """Attention of the ragged batch q (bf16 [total_q, q_heads * head_dim]; sequence b owns rows cu_q[b] .. cu_q[b + 1] - 1,
+    its last tokens) over the cache.  cu_q, kv_len: int32 [batch + 1], [batch]; page_table: int32 [batch, width].
+    scale: 1 / sqrt(head_dim) if None.  lse: fp32 [total_q, q_heads] to be filled, or None.  Returns out (bf16)."""
+    import torch
+    if q.dim() != 2 or q.dtype != torch.bfloat16:
+        raise ValueError("q: expected bf16 [total_q, q_heads * head_dim]")
+    T, q_heads = q.shape[0], q.shape[1] // cache.head_dim
+    ldq, batch = _rows(q, q_heads * cache.head_dim, "q"), kv_len.shape[0]
+    _list(cu_q, torch.int32, (batch + 1,), "cu_q")
+    _list(kv_len, torch.int32, (batch,), "kv_len")
+    if page_table.dim() != 2:
+        raise ValueError("page_table: expected [batch, width]")
+    _list(page_table, torch.int32, (batch, page_table.shape[1]), "page_table")
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    ldo = _rows(out, q.shape[1], "out")
+    if out.shape[0] != T or out.dtype != torch.bfloat16:
+        raise ValueError("out: expected bf16 with the rows of q")
+    if lse is not None:
+        _list(lse, torch.float32, (T, q_heads), "lse")
+    if workspace is None:
+        n = batq_paged_attention_workspace(cache, q_heads, batch, T, max_q, max_kv)
+        workspace = torch.empty((max(n, 16),), dtype=torch.uint8, device=q.device)
+    _on_current_device(cache.k_codes, q, cu_q, kv_len, page_table, out, lse, workspace)
+    b = _PagedBatch(cu_q.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), batch, page_table.shape[1], T, max_q, max_kv)
+    _check(lib.batq_paged_attention(cache.desc, C.byref(b), q.data_ptr(), ldq, q_heads,
+                                    cache.head_dim ** -0.5 if scale is None else scale, int(causal), window, out.data_ptr(), ldo,
+                                    lse.data_ptr() if lse is not None else None, workspace.data_ptr(),
+                                    workspace.numel() * workspace.element_size(), _stream()), "batq_paged_attention")
+    return out
+
+
+def batq_lora_workspace(M: int, K: int, N: int, rank: int, adapters: int) -> int:
+    return int(lib.batq_lora_workspace(M, K, N, rank, adapters))
+
+
+def batq_lora_add(X, A, B, index, base=None, scales=None, out=None, out_dtype=None, workspace=None):
+    """out[m] = base[m] + scales[a] * (X[m] A[a]^T) B[a]^T with a = index[m] (outside the adapters: base alone).
+    X: [M, K] (bf16 or fp32); A: bf16 [adapters, rank, K]; B: bf16 [adapters, N, rank]; index: int32 [M]; base, out:
+    [M, N] of one type (out may be base); base None: zeros."""
+    import torch
+    if A.dim() != 3 or B.dim() != 3:
+        raise ValueError("A, B: expected [adapters, rank, K] and [adapters, N, rank]")
+    n, rank, K = A.shape
+    N, M = B.shape[1], X.shape[0]
+    ldx = _rows(X, K, "X")
+    _list(A, torch.bfloat16, (n, rank, K), "A")
+    _list(B, torch.bfloat16, (n, N, rank), "B")
+    _list(index, torch.int32, (M,), "index")
+    if scales is not None:
+        _list(scales, torch.float32, (n,), "scales")
+    if out is None:
+        out = torch.empty((M, N), dtype=base.dtype if base is not None else out_dtype or torch.bfloat16, device=X.device)
+    ldo, ldb = _rows(out, N, "out"), N
+    if out.shape[0] != M or (base is not None and (base.shape[0] != M or base.dtype != out.dtype)):
+        raise ValueError("base and out: expected [M, N] of one type")
+    if base is not None:
+        ldb = _rows(base, N, "base")
+    if workspace is None:
+        workspace = torch.empty((max(batq_lora_workspace(M, K, N, rank, n), 16),), dtype=torch.uint8, device=X.device)
+    _on_current_device(X, A, B, index, scales, base, out, workspace)
+    _check(lib.batq_lora_add(X.data_ptr(), _dtype_code(X), M, K, ldx, A.data_ptr(), B.data_ptr(), N, rank, n,
+                             scales.data_ptr() if scales is not None else None, index.data_ptr(),
+                             base.data_ptr() if base is not None else None, ldb, out.data_ptr(), ldo, _dtype_code(out),
+                             workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()), "batq_lora_add")
+    return out

@@ -854,4 +854,148 @@ batq_status batq_row_rms_scale(const void* X, batq_dtype xdtype, int M, int K, i
     return BATQ_OK;
 }
 
+// ---- paged 8-bit cache
+static batq_status check_paged_dims(int num_pages, int page_size, int kv_heads, int head_dim) {
+    if (head_dim != 64 && head_dim != 128) return BATQ_ERR_UNSUPPORTED;
+    if (num_pages < 1 || kv_heads < 1 || kv_heads > 4096 || page_size < 16 || page_size > 256 ||
+        (page_size & (page_size - 1)) != 0)
+        return BATQ_ERR_SHAPE;
+    return BATQ_OK;
+}
+
+static batq_status check_paged_cache(const batq_paged_cache* c) {
+    if (!c) return BATQ_ERR_NULL;
+    if (batq_status st = check_paged_dims(c->num_pages, c->page_size, c->kv_heads, c->head_dim); st != BATQ_OK) return st;
+    if (!c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales) return BATQ_ERR_NULL;
+    if (!aligned16(c->k_codes) || !aligned16(c->k_scales) || !aligned16(c->v_codes) || !aligned16(c->v_scales))
+        return BATQ_ERR_SHAPE;
+    return BATQ_OK;
+}
+
+size_t batq_kv_paged_code_bytes(int num_pages, int page_size, int kv_heads, int head_dim) {
+    if (check_paged_dims(num_pages, page_size, kv_heads, head_dim) != BATQ_OK) return 0;
+    return (size_t)num_pages * page_size * kv_heads * head_dim;
+}
+
+size_t batq_kv_paged_scale_bytes(int num_pages, int page_size, int kv_heads, int head_dim) {
+    return batq_kv_paged_code_bytes(num_pages, page_size, kv_heads, head_dim) / 32;
+}
+
+batq_status batq_kv_paged_append(const batq_paged_cache* cache, const batq_transform* tk, const batq_transform* tv,
+                                 const batq_rope* rope, const void* q, int64_t ldq, int q_heads, void* q_out,
+                                 int64_t ldq_out, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                 batq_dtype xdtype, const int32_t* positions, const int64_t* slots, int M,
+                                 void* stream) {
+    if (batq_status st = check_paged_cache(cache); st != BATQ_OK) return st;
+    if (!dtype_ok(xdtype)) return BATQ_ERR_DTYPE;
+    const int D = cache->head_dim, width = cache->kv_heads * D;
+    if (M < 0 || ldk < width || ldv < width || q_heads < 0 || q_heads > (1 << 19) || q_heads % cache->kv_heads != 0)
+        return BATQ_ERR_SHAPE;
+    if (q_heads > 0 && (ldq < (int64_t)q_heads * D || ldq_out < (int64_t)q_heads * D)) return BATQ_ERR_SHAPE;
+    if ((tk && tk->K != width) || (tv && tv->K != width)) return BATQ_ERR_MISMATCH;
+    if (rope) {
+        if (!rope->table) return BATQ_ERR_NULL;
+        if (rope->positions < 1 || rope->rotary_dim < 16 || rope->rotary_dim > D || rope->rotary_dim % 16 != 0 ||
+            !aligned16(rope->table))
+            return BATQ_ERR_SHAPE;
+    }
+    if (M == 0) return BATQ_OK;
+    if (!k || !v || !slots || (rope && !positions) || (q_heads > 0 && (!q || !q_out)) || (q_heads == 0 && q)) return BATQ_ERR_NULL;
+    const int64_t size = (int64_t)dtype_size(xdtype);
+    if (!aligned16(k) || !aligned16(v) || (ldk * size) % 16 != 0 || (ldv * size) % 16 != 0 ||
+        (reinterpret_cast<uintptr_t>(slots) & 7u) != 0 || (reinterpret_cast<uintptr_t>(positions) & 3u) != 0)
+        return BATQ_ERR_SHAPE;
+    if (q_heads > 0 && (!aligned16(q) || !aligned16(q_out) || (ldq * size) % 16 != 0 || (ldq_out * 2) % 16 != 0 || q == q_out))
+        return BATQ_ERR_SHAPE;
+    if (batq_status st = check_device(); st != BATQ_OK) return st;
+    BATQ_HIP(batq::launch_kv_paged_append(*cache, tk, tv, rope, q, ldq, q_heads, q_out, ldq_out, k, ldk, v, ldv, xdtype,
+                                          positions, slots, M, static_cast<hipStream_t>(stream)));
+    return BATQ_OK;
+}
+
+// ---- attention over the paged cache
+static batq_status check_attention_dims(const batq_paged_cache* c, int q_heads, int batch, int total_q, int max_q, int max_kv) {
+    if (!c) return BATQ_ERR_NULL;
+    if (batq_status st = check_paged_dims(c->num_pages, c->page_size, c->kv_heads, c->head_dim); st != BATQ_OK) return st;
+    if (q_heads < 1 || q_heads % c->kv_heads != 0 || q_heads / c->kv_heads > 128) return BATQ_ERR_SHAPE;
+    if (batch < 0 || batch > (1 << 20) || total_q < 0 || max_q < 0 || max_kv < 0 ||
+        (int64_t)total_q * q_heads > INT32_MAX || (int64_t)max_q * q_heads > INT32_MAX)
+        return BATQ_ERR_SHAPE;
+    return BATQ_OK;
+}
+
+// Compute units of the current device, or 0.
+static int current_compute_units() {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    const int cus = e == hipSuccess ? batq::device_compute_units(dev, &e) : 0;
+    if (e != hipSuccess) (void)hipGetLastError();
+    return e == hipSuccess ? cus : 0;
+}
+
+size_t batq_paged_attention_workspace(const batq_paged_cache* cache, int q_heads, int batch, int total_q, int max_q,
+                                      int max_kv) {
+    if (check_attention_dims(cache, q_heads, batch, total_q, max_q, max_kv) != BATQ_OK) return 0;
+    const int cus = current_compute_units();
+    return cus ? batq::paged_attention_workspace_bytes(*cache, q_heads, batch, total_q, max_q, max_kv, cus) : 0;
+}
+
+batq_status batq_paged_attention(const batq_paged_cache* cache, const batq_paged_batch* b, const void* q, int64_t ldq,
+                                 int q_heads, float scale, int causal, int window, void* out, int64_t ldo, float* lse,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+    if (!b) return BATQ_ERR_NULL;
+    if (batq_status st = check_attention_dims(cache, q_heads, b->batch, b->total_q, b->max_q, b->max_kv); st != BATQ_OK) return st;
+    if (batq_status st = check_paged_cache(cache); st != BATQ_OK) return st;
+    const int64_t width = (int64_t)q_heads * cache->head_dim;
+    if (ldq < width || ldo < width || b->table_width < 0 || window < 0 || !(scale > 0.0f) || !(scale < 3.0e38f)) return BATQ_ERR_SHAPE;
+    if (b->batch == 0 || b->total_q == 0 || b->max_q == 0) return BATQ_OK;
+    if (!q || !out || !b->cu_q || !b->kv_len || (!b->page_table && b->table_width > 0)) return BATQ_ERR_NULL;
+    if (!aligned16(q) || !aligned16(out) || (ldq * 2) % 16 != 0 || (ldo * 2) % 16 != 0 || q == out ||
+        ((reinterpret_cast<uintptr_t>(b->cu_q) | reinterpret_cast<uintptr_t>(b->kv_len) |
+          reinterpret_cast<uintptr_t>(b->page_table) | reinterpret_cast<uintptr_t>(lse)) & 3u) != 0 ||
+        (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+        return BATQ_ERR_SHAPE;
+    if (batq_status st = check_device(); st != BATQ_OK) return st;
+    const int cus = current_compute_units();
+    if (!cus) return BATQ_ERR_DEVICE;
+    const size_t need = batq::paged_attention_workspace_bytes(*cache, q_heads, b->batch, b->total_q, b->max_q, b->max_kv, cus);
+    if (need > workspace_bytes || (need > 0 && !workspace)) return BATQ_ERR_WORKSPACE;
+    BATQ_HIP(batq::launch_paged_attention(*cache, *b, q, ldq, q_heads, scale, causal != 0, window, out, ldo, lse, workspace,
+                                          static_cast<hipStream_t>(stream)));
+    return BATQ_OK;
+}
+
+// ---- low-rank adapters
+static batq_status check_lora_dims(int M, int K, int N, int rank, int adapters) {
+    if (M < 0 || K <= 0 || K % 32 != 0 || N <= 0 || rank < 8 || rank > 128 || rank % 8 != 0 || adapters < 1) return BATQ_ERR_SHAPE;
+    return BATQ_OK;
+}
+
+size_t batq_lora_workspace(int M, int K, int N, int rank, int adapters) {
+    return check_lora_dims(M, K, N, rank, adapters) == BATQ_OK ? batq::lora_workspace_bytes(M, K, N, rank, adapters) : 0;
+}
+
+batq_status batq_lora_add(const void* X, batq_dtype xdtype, int M, int K, int64_t ldx, const void* A, const void* B,
+                          int N, int rank, int adapters, const float* scales, const int32_t* index, const void* base,
+                          int64_t ldb, void* out, int64_t ldo, batq_dtype ydtype, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+    if (!dtype_ok(xdtype) || !dtype_ok(ydtype)) return BATQ_ERR_DTYPE;
+    if (batq_status st = check_lora_dims(M, K, N, rank, adapters); st != BATQ_OK) return st;
+    if (ldx < K || ldo < N || (base && ldb < N)) return BATQ_ERR_SHAPE;
+    if (M == 0) return BATQ_OK;
+    if (!X || !A || !B || !index || !out) return BATQ_ERR_NULL;
+    const uintptr_t el = dtype_size(ydtype) - 1;
+    if (!aligned16(X) || !aligned16(A) || !aligned16(B) || (ldx * (int64_t)dtype_size(xdtype)) % 16 != 0 ||
+        ((reinterpret_cast<uintptr_t>(base) | reinterpret_cast<uintptr_t>(out)) & el) != 0 ||
+        ((reinterpret_cast<uintptr_t>(scales) | reinterpret_cast<uintptr_t>(index)) & 3u) != 0 ||
+        (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || X == out || (base == out && ldb != ldo))
+        return BATQ_ERR_SHAPE;
+    if (batq_status st = check_device(); st != BATQ_OK) return st;
+    const size_t need = batq::lora_workspace_bytes(M, K, N, rank, adapters);
+    if (need > workspace_bytes || (need > 0 && !workspace)) return BATQ_ERR_WORKSPACE;
+    BATQ_HIP(batq::launch_lora_add(X, xdtype, M, K, ldx, A, B, N, rank, adapters, scales, index, base, ldb, out, ldo, ydtype,
+                                   workspace, static_cast<hipStream_t>(stream)));
+    return BATQ_OK;
+}
+
 }  // extern "C"

@@ -125,4 +125,20 @@ hipError_t launch_codes_to_rowmajor(const uint8_t* blocked, uint8_t* rowmajor, i
 hipError_t launch_scales_to_internal(const uint8_t* canon, uint8_t* internal, int rows, int nb, hipStream_t stream);
 hipError_t launch_scales_to_canonical(const uint8_t* internal, uint8_t* canon, int rows, int nb, hipStream_t stream);
 
+// Paged cache and the operators on it (arguments checked by the C ABI).
+hipError_t launch_kv_paged_append(const batq_paged_cache& c, const batq_transform* tk, const batq_transform* tv,
+                                  const batq_rope* rope, const void* q, int64_t ldq, int q_heads, void* q_out,
+                                  int64_t ldq_out, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                  batq_dtype xdtype, const int32_t* positions, const int64_t* slots, int M,
+                                  hipStream_t stream);
+size_t paged_attention_workspace_bytes(const batq_paged_cache& c, int q_heads, int batch, int total_q, int max_q,
+                                       int max_kv, int compute_units);
+hipError_t launch_paged_attention(const batq_paged_cache& c, const batq_paged_batch& b, const void* q, int64_t ldq,
+                                  int q_heads, float scale, bool causal, int window, void* out, int64_t ldo, float* lse,
+                                  void* workspace, hipStream_t stream);
+size_t lora_workspace_bytes(int M, int K, int N, int rank, int adapters);
+hipError_t launch_lora_add(const void* X, batq_dtype xdtype, int M, int K, int64_t ldx, const void* A, const void* B,
+                           int N, int rank, int adapters, const float* scales, const int32_t* index, const void* base,
+                           int64_t ldb, void* out, int64_t ldo, batq_dtype ydtype, void* workspace, hipStream_t stream);
+
 }  // namespace batq

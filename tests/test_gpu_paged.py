@@ -1,0 +1,530 @@
+"""The paged 8-bit cache: batq_kv_paged_append (rotation, transforms, MXFP8, scatter) and batq_paged_attention
+against plain 64-bit statements, separately and together as a serving step uses them."""
+import numpy as np
+import pytest
+
+import batq_inputs as bi
+from oracle import batq_oracle as o
+from gpu_util import require_gpu, to_dev, y_to_f32
+import serving_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    require_gpu()
+    import paper_2603_16590_amd as b
+    return b
+
+
+def dev(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def make_cache(B, rng, pages, page, heads, D):
+    arrays = ref.random_cache(rng, pages, page, heads, D) + ref.random_cache(rng, pages, page, heads, D)
+    return arrays, B.PagedCache(pages, page, heads, D, tensors=[dev(a) for a in arrays])
+
+
+def host(cache):
+    return [t.cpu().numpy() for t in (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)]
+
+
+APPEND = [
+    # M, q heads, kv heads, D, page, rot, interleaved, dtype
+    (1, 4, 4, 64, 16, 64, False, "bf16"),
+    (1, 32, 8, 128, 16, 128, False, "bf16"),
+    (31, 7, 1, 128, 32, 64, True, "f32"),
+    (33, 0, 3, 64, 256, 16, False, "f32"),
+    (33, 6, 2, 128, 64, 48, False, "bf16"),
+    (65, 8, 2, 64, 16, 32, True, "bf16"),
+    (200, 28, 4, 128, 16, 0, False, "bf16"),
+    (311, 12, 3, 64, 128, 64, False, "f32"),
+]
+
+
+def append_case(rng, M, hq, hkv, D, page, rot, dtype):
+    """(X storage, q, k, v as fp32 [M, heads, D], positions, slots, pages): slots scattered, some unused."""
+    X = rng.standard_normal((M, (hq + 2 * hkv) * D + 8)).astype(np.float32)
+    X[:, ::37] *= 30.0
+    X[M // 2, :64] = 0.0                                    # zero blocks
+    if dtype == "bf16":
+        bits = bi.f32_to_bf16_bits(X)
+        X, Xd = bi.bf16_bits_to_f32(bits), to_dev(bits, "bf16")
+    else:
+        Xd = to_dev(X, "f32")
+    cut = np.cumsum([0, hq * D, hkv * D, hkv * D])
+    parts = [X[:, cut[i]: cut[i + 1]].reshape(M, -1, D) for i in range(3)]
+    dparts = [Xd[:, cut[i]: cut[i + 1]] for i in range(3)]
+    pages = -(-M // page) + 3
+    slots = rng.permutation(pages * page)[:M].astype(np.int64)
+    positions = rng.integers(0, 1000, M).astype(np.int32)
+    if M > 4:
+        slots[[1, M // 2]] = -1, pages * page               # unused and past the end
+        positions[[2, 3]] = -1, 1000                        # outside the table
+    return parts, dparts, positions, slots, pages
+
+
+@pytest.mark.parametrize("M,hq,hkv,D,page,rot,inter,dtype", APPEND)
+def test_append_without_transforms_is_bit_exact(B, M, hq, hkv, D, page, rot, inter, dtype):
+    import torch
+    rng = np.random.default_rng(M + hq + D + rot)
+    (q, k, v), (qd, kd, vd), positions, slots, pages = append_case(rng, M, hq, hkv, D, page, rot, dtype)
+    arrays, cache = make_cache(B, rng, pages, page, hkv, D)
+    table = ref.rope_table(1000, rot) if rot else None
+    q_out = torch.full((M, hq * D + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    B.batq_kv_paged_append(cache, kd, vd, dev(slots), positions=dev(positions) if rot else None, q=qd if hq else None,
+                           q_out=q_out[:, : hq * D] if hq else None, rope=dev(table) if rot else None, interleaved=inter)
+    torch.cuda.synchronize()
+    left_out = np.zeros(M, bool)
+    if rot:
+        left_out = (positions < 0) | (positions >= 1000)
+        at = np.where(left_out, 0, positions)
+        q, k = ref.rotate(q, table, at, rot, inter), ref.rotate(k, table, at, rot, inter)
+    used = np.where(left_out, -1, slots)
+    want = [a.copy() for a in arrays]
+    for n, x in ((0, k), (2, v)):
+        ref.scatter(want[n], want[n + 1], used, page, hkv, D, *o.mxfp8_quantize(x.reshape(M, -1)))
+    for got, w, old, name in zip(host(cache), want, arrays, ("k codes", "k scales", "v codes", "v scales")):
+        assert np.array_equal(got, w), name
+    if hq:
+        got = y_to_f32(q_out)
+        assert np.array_equal(got[~left_out, : hq * D], o.bf16_round(q.reshape(M, -1))[~left_out])
+        assert np.all(got[left_out] == 7.0) and np.all(got[:, hq * D:] == 7.0)
+
+
+def _transforms(B, rng, hkv, D, form, clip=True):
+    width = hkv * D
+    G = (np.eye(4) + 0.05 * rng.standard_normal((4, 4))).astype(np.float32)
+    P = (np.eye(8) + 0.05 * rng.standard_normal((width // 32, 8, 8))).astype(np.float32)
+    c = rng.uniform(0.85, 1.0, width // 32).astype(np.float32) if clip else None
+    T = o.kron_blocks(G, P)
+    if form == "kron":
+        return B.Transform(width, G, P, c), T, c
+    return B.Transform.general(width, dense=T.astype(np.float32), clip=c), T.astype(np.float32).astype(np.float64), c
+
+
+@pytest.mark.parametrize("M,hq,hkv,D,page,rot,inter,dtype", [c for c in APPEND if c[0] > 1])
+@pytest.mark.parametrize("form", ["kron", "dense"])
+def test_append_with_transforms(B, M, hq, hkv, D, page, rot, inter, dtype, form):
+    """Codes against the 64-bit transform: an element may sit on the other side of a rounding border only if the
+    exact value is within the transform's accuracy (2^-20 sum |x| |T|) of it."""
+    import torch
+    rng = np.random.default_rng(M + hq + D + rot + 1)
+    (q, k, v), (qd, kd, vd), positions, slots, pages = append_case(rng, M, hq, hkv, D, page, rot, dtype)
+    arrays, cache = make_cache(B, rng, pages, page, hkv, D)
+    tk, Tk, ck = _transforms(B, rng, hkv, D, form)
+    tv, Tv, cv = _transforms(B, rng, hkv, D, form)
+    table = ref.rope_table(1000, rot) if rot else None
+    q_out = B.batq_kv_paged_append(cache, kd, vd, dev(slots), positions=dev(positions) if rot else None, q=qd if hq else None,
+                                   rope=dev(table) if rot else None, interleaved=inter, tk=tk, tv=tv)
+    torch.cuda.synchronize()
+    left_out = ((positions < 0) | (positions >= 1000)) if rot else np.zeros(M, bool)
+    if rot:
+        at = np.where(left_out, 0, positions)
+        q, k = ref.rotate(q, table, at, rot, inter), ref.rotate(k, table, at, rot, inter)
+    live = ~left_out & (slots >= 0) & (slots < pages * page)
+    got = host(cache)
+    for n, x, T, c in ((0, k, Tk, ck), (2, v, Tv, cv)):
+        x = x.reshape(M, -1).astype(np.float64)
+        y, absy = o.apply_blocks(x, T), o.apply_blocks(np.abs(x), np.abs(T))
+        want_c, want_s = o.mxfp8_quantize(y.astype(np.float32), c)
+        gc = got[n][slots[live] // page, :, slots[live] % page].reshape(live.sum(), -1)
+        gs = got[n + 1][slots[live] // page, :, :, slots[live] % page].reshape(live.sum(), -1)
+        assert np.mean(gc != want_c[live]) <= 1e-3 and np.mean(gs != want_s[live]) <= 1e-3
+        val = o.dequantize_fp8(gc, gs)
+        y, absy = y[live], absy[live]
+        lim = np.repeat(np.abs(y).reshape(len(y), -1, 32).max(-1) * c, 32, 1)
+        unit = np.repeat(np.exp2(gs.astype(np.float64) - 127), 32, 1)
+        clipped = np.clip(np.clip(y, -lim, lim), -448 * unit, 448 * unit)
+        step = np.maximum(np.exp2(np.floor(np.log2(np.maximum(np.abs(clipped), 1e-300))) - 3), unit * 2.0 ** -9)
+        assert np.all(np.abs(val - clipped) <= step / 2 + 2.0 ** -19 * np.repeat(absy.reshape(len(y), -1, 32).max(-1), 32, 1))
+        # nothing else was touched
+        mask = np.ones(got[n].shape, bool)
+        mask[slots[live] // page, :, slots[live] % page] = False
+        assert np.array_equal(got[n][mask], arrays[n][mask])
+    if hq:
+        Tq = np.repeat(o.inverse_transpose_blocks(Tk).reshape(hkv, -1, 32, 32), hq // hkv, 0).reshape(-1, 32, 32)
+        x = q.reshape(M, -1).astype(np.float64)
+        y, absy = o.apply_blocks(x, Tq), o.apply_blocks(np.abs(x), np.abs(Tq))
+        d = np.abs(y_to_f32(q_out).astype(np.float64) - y)
+        assert np.all((d <= 2.0 ** -8 * np.abs(y) + 2.0 ** -19 * absy)[~left_out])
+
+
+@pytest.mark.parametrize("kind", ["kron", "minmax", "clip only"])
+def test_append_without_rotation_writes_the_bytes_of_batq_kv_append(B, kind):
+    """One sequence in page order: the rows of the paged cache hold what the row-window cache holds, byte for byte."""
+    import torch
+    rng = np.random.default_rng(5)
+    M, hkv, D, page = 150, 2, 128, 32
+    width = hkv * D
+    bits, _ = ref.bf16_values(rng, M, width)
+    X = to_dev(bits, "bf16")
+    if kind == "kron":
+        t, _, _ = _transforms(B, rng, hkv, D, "kron")
+    elif kind == "clip only":
+        t = B.Transform(width, None, None, rng.uniform(0.7, 1.0, width // 32).astype(np.float32))
+    else:
+        lo, hi = (rng.uniform(0.7, 1.0, width // 32).astype(np.float32) for _ in range(2))
+        t = B.Transform.general(width, outer=np.eye(4, dtype=np.float32) * 1.25,
+                                inner=(np.eye(8) + 0.05 * rng.standard_normal((width // 32, 8, 8))), clip_min=lo, clip_max=hi)
+    cache = B.PagedCache(-(-M // page), page, hkv, D)
+    for lo, hi in ((0, 1), (1, 40), (40, M)):               # in pieces of any size
+        B.batq_kv_paged_append(cache, X[lo:hi], X[lo:hi], torch.arange(lo, hi, device="cuda"), tk=t, tv=t)
+    codes = torch.zeros(B.batq_code8_bytes(M, width), dtype=torch.uint8, device="cuda")
+    scales = torch.zeros(B.batq_scale_bytes(M, width), dtype=torch.uint8, device="cuda")
+    B.batq_kv_append(t, X, codes, scales, 0, M, bits=8)
+    rc, rs = B.batq_codes8_to_rowmajor(codes, M, width), B.batq_scales_to_rowmajor(scales, M, width)
+    torch.cuda.synchronize()
+    for c, s in ((cache.k_codes, cache.k_scales), (cache.v_codes, cache.v_scales)):
+        assert torch.equal(c.permute(0, 2, 1, 3).reshape(-1, width)[:M], rc)
+        assert torch.equal(s.permute(0, 3, 1, 2).reshape(-1, width // 32)[:M], rs)
+
+
+def test_append_token_by_token_equals_one_call(B):
+    import torch
+    rng = np.random.default_rng(8)
+    M, hq, hkv, D, page = 70, 4, 2, 128, 16
+    X = to_dev(ref.bf16_values(rng, M, (hq + 2 * hkv) * D)[0], "bf16")
+    q, k, v = X.split((hq * D, hkv * D, hkv * D), 1)
+    tk, _, _ = _transforms(B, rng, hkv, D, "kron")
+    table, slots = dev(ref.rope_table(4000, D)), torch.randperm(6 * page, device="cuda")[:M]
+    pos = torch.arange(M, device="cuda", dtype=torch.int32) + 3900
+    a, b = B.PagedCache(6, page, hkv, D), B.PagedCache(6, page, hkv, D)
+    qa = B.batq_kv_paged_append(a, k, v, slots, pos, q=q, rope=table, tk=tk)
+    qb = torch.zeros_like(qa)
+    for m in range(M):
+        B.batq_kv_paged_append(b, k[m:m + 1], v[m:m + 1], slots[m:m + 1], pos[m:m + 1], q=q[m:m + 1], q_out=qb[m:m + 1],
+                               rope=table, tk=tk)
+    torch.cuda.synchronize()
+    assert torch.equal(qa, qb)
+    for x, y in zip(host(a), host(b)):
+        assert np.array_equal(x, y)
+
+
+# ---------------------------------------------------------------------------------------- attention
+def attend_case(rng, B, lens, qs, hq, hkv, D, page, spare=0):
+    lens, qs = np.array(lens), np.array(qs)
+    per = -(-lens // page)
+    pages = int(per.sum()) + 2
+    arrays, cache = make_cache(B, rng, pages, page, hkv, D)
+    order = rng.permutation(pages)
+    table = np.full((len(lens), max(1, int(per.max()))), -7, np.int32)
+    filled = np.zeros(pages, np.int64)
+    at = 0
+    for b in range(len(lens)):
+        mine = order[at: at + per[b]]
+        at += per[b]
+        table[b, : per[b]] = mine
+        filled[mine] = np.minimum(page, lens[b] - page * np.arange(per[b]))
+    # what no token was written to holds NaN codes and NaN scales
+    empty = np.arange(page)[None] >= filled[:, None]
+    for n in (0, 2):
+        arrays[n][np.broadcast_to(empty[:, None, :, None], arrays[n].shape)] = 0x7F
+        arrays[n + 1][np.broadcast_to(empty[:, None, None, :], arrays[n + 1].shape)] = 255
+    cache = B.PagedCache(pages, page, hkv, D, tensors=[dev(a) for a in arrays])
+    cu = np.concatenate([[0], np.cumsum(qs)]).astype(np.int32)
+    T = int(cu[-1]) + spare
+    bits, q = ref.bf16_values(rng, T, hq * D)
+    with np.errstate(invalid="ignore"):
+        kv, vv = ref.cache_values(arrays[0], arrays[1]), ref.cache_values(arrays[2], arrays[3])
+    return cache, (kv, vv), to_dev(bits, "bf16"), q.reshape(T, hq, D).astype(np.float64), cu, lens.astype(np.int32), table, T
+
+
+def run_attention(B, cache, qd, cu, lens, table, T, hq, max_q=None, max_kv=None, **kw):
+    import torch
+    D = cache.head_dim
+    out = torch.full((T, hq * D + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((T, hq), 7.0, dtype=torch.float32, device="cuda")
+    max_q = int(np.diff(cu).max()) if max_q is None else max_q
+    max_kv = int(max(lens)) if max_kv is None else max_kv
+    B.batq_paged_attention(cache, qd, dev(cu), dev(lens), dev(table), max_q, max_kv, out=out[:, : hq * D], lse=lse, **kw)
+    torch.cuda.synchronize()
+    got = y_to_f32(out).astype(np.float64)
+    assert np.all(got[:, hq * D:] == 7.0)
+    assert np.all(got[cu[-1]:, : hq * D] == 7.0) and bool((lse[int(cu[-1]):] == 7.0).all())
+    return got[:, : hq * D].reshape(T, hq, D), lse.cpu().numpy().astype(np.float64)
+
+
+ATTEND = [
+    # lens, query counts, q heads, kv heads, D, page, window
+    ([1], [1], 1, 1, 64, 16, 0),
+    ([64], [1], 4, 1, 128, 16, 0),
+    ([1, 15, 16, 17, 63, 64, 65, 129], [1] * 8, 8, 2, 128, 16, 0),
+    ([0, 5, 0, 300], [1, 1, 2, 1], 7, 1, 128, 32, 0),
+    ([700, 3, 1025], [1, 1, 1], 28, 4, 64, 64, 0),
+    ([513, 40], [3, 2], 8, 4, 64, 256, 0),
+    ([200, 90], [5, 7], 6, 2, 128, 16, 33),
+    ([1000], [1], 16, 1, 128, 128, 64),
+    ([333], [333], 3, 3, 64, 32, 0),
+    ([290], [290], 8, 1, 128, 16, 0),
+    ([130, 64, 257, 1], [130, 1, 100, 1], 14, 2, 128, 64, 0),
+    ([200, 140], [70, 140], 4, 4, 128, 32, 1),
+    ([500], [129], 2, 1, 64, 16, 100),
+    ([300, 20], [10, 20], 32, 1, 64, 16, 0),
+    ([77], [40], 40, 1, 128, 16, 0),
+    ([5, 9], [9, 20], 4, 2, 64, 16, 0),                     # more queries than tokens: the first ones see nothing
+]
+
+
+@pytest.mark.parametrize("lens,qs,hq,hkv,D,page,window", ATTEND)
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention(B, lens, qs, hq, hkv, D, page, window, causal):
+    rng = np.random.default_rng(sum(lens) + sum(qs) + hq)
+    cache, (kv, vv), qd, q, cu, lens, table, T = attend_case(rng, B, lens, qs, hq, hkv, D, page, spare=3)
+    got, lse = run_attention(B, cache, qd, cu, lens, table, T, hq, causal=causal, window=window)
+    want = ref.attention(kv, vv, q, cu, lens, table, page, D ** -0.5, causal, window, T)
+    ref.assert_attention(got, lse, want)
+
+
+def test_attention_of_long_sequences(B):
+    """Long enough for every way of cutting a sequence into parts: one against the reference, and each against a
+    batch of which it is a part."""
+    import torch
+    rng = np.random.default_rng(3)
+    hq, hkv, D, page = 8, 2, 128, 64
+    cache, (kv, vv), qd, q, cu, lens, table, T = attend_case(rng, B, [20000, 9, 7001, 1, 15000], [1, 1, 4, 1, 2], hq, hkv, D, page)
+    got, lse = run_attention(B, cache, qd, cu, lens, table, T, hq)
+    ref.assert_attention(got, lse, ref.attention(kv, vv, q, cu, lens, table, page, D ** -0.5, True, 0, T))
+    for b in range(5):
+        one = np.array([0, cu[b + 1] - cu[b]], np.int32)
+        alone, _ = run_attention(B, cache, qd[cu[b]: cu[b + 1]], one, lens[b: b + 1], table[b: b + 1], int(one[1]), hq)
+        ref.assert_attention(alone, None, tuple(x[cu[b]: cu[b + 1]] for x in ref.attention(kv, vv, q, cu, lens, table, page, D ** -0.5, True, 0, T)))
+
+
+def test_attention_of_a_long_chunk(B):
+    """A prompt's later chunk: many queries over a long context, next to decoding sequences."""
+    rng = np.random.default_rng(4)
+    hq, hkv, D, page = 4, 1, 64, 16
+    cache, (kv, vv), qd, q, cu, lens, table, T = attend_case(rng, B, [3000, 1500, 2500], [70, 1, 300], hq, hkv, D, page)
+    for window in (0, 700):
+        got, lse = run_attention(B, cache, qd, cu, lens, table, T, hq, window=window)
+        ref.assert_attention(got, lse, ref.attention(kv, vv, q, cu, lens, table, page, D ** -0.5, True, window, T))
+
+
+def test_attention_does_not_trust_its_lists(B):
+    """Pages outside the cache, lengths past the table or max_kv, rows outside q: none of it takes part."""
+    rng = np.random.default_rng(6)
+    hq, hkv, D, page = 4, 2, 128, 16
+    cache, (kv, vv), qd, q, cu, lens, table, T = attend_case(rng, B, [100, 40, 64, 90], [1, 3, 20, 1], hq, hkv, D, page, spare=2)
+    table[0, 2], table[2, 0], table[2, 3], table[1, 0] = -1, 10 ** 6, -2 ** 31, 2 ** 31 - 1
+    table[3, :] = -1                                        # a sequence without any page
+    got, lse = run_attention(B, cache, qd, cu, lens, table, T, hq, max_kv=128)
+    ref.assert_attention(got, lse, ref.attention(kv, vv, q, cu, lens, table, page, D ** -0.5, True, 0, T))
+    # lengths: past the table's width, negative
+    longer = lens.copy()
+    longer[0], longer[1] = 10 ** 9, -5
+    eff = np.array([table.shape[1] * page, 0, 64, 90])
+    got, lse = run_attention(B, cache, qd, cu, longer, table, T, hq, max_kv=10 ** 6)
+    full = np.nan_to_num(kv), np.nan_to_num(vv)
+    t2 = table.copy()
+    t2[0] = np.where((table[0] >= 0), table[0], -1)
+    want = ref.attention(*full, q, cu, eff, t2, page, D ** -0.5, True, 0, T)
+    rows = slice(int(cu[1]), int(cu[4]))                    # (sequence 0 now reads places that nothing was written to)
+    ref.assert_attention(got[rows], lse[rows], tuple(x[rows] for x in want))
+    # row lists: a decreasing one and one past the end leave their rows alone
+    for broken in ([0, 1, 4, 24, 10 ** 6], [0, 1, 4, 24, 3], [0, -1, 4, 24, 25]):
+        broken = np.array(broken, np.int32)
+        import torch
+        out = torch.full((T, hq * D), 7.0, dtype=torch.bfloat16, device="cuda")
+        B.batq_paged_attention(cache, qd, dev(broken), dev(lens), dev(table), 20, 128, out=out)
+        torch.cuda.synchronize()
+        got = y_to_f32(out).astype(np.float64).reshape(T, hq, D)
+        assert np.all(got[25:] == 7.0)
+        sel = slice(4, 24)
+        ref.assert_attention(got[sel], None, tuple(x[sel] for x in ref.attention(kv, vv, q, cu, lens, table, page, D ** -0.5, True, 0, T)))
+
+
+@pytest.mark.parametrize("max_q,max_kv", [(1, 64), (3, 50), (64, 0)])
+def test_attention_bounds_cut_a_sequence(B, max_q, max_kv):
+    import torch
+    rng = np.random.default_rng(7)
+    hq, hkv, D, page = 4, 2, 64, 16
+    cache, (kv, vv), qd, q, cu, lens, table, T = attend_case(rng, B, [64, 50], [5, 6], hq, hkv, D, page)
+    out = torch.full((T, hq * D), 7.0, dtype=torch.bfloat16, device="cuda")
+    B.batq_paged_attention(cache, qd, dev(cu), dev(lens), dev(table), max_q, max_kv, out=out)
+    torch.cuda.synchronize()
+    got = y_to_f32(out).astype(np.float64).reshape(T, hq, D)
+    want = ref.attention(np.nan_to_num(kv), np.nan_to_num(vv), q, cu, np.minimum(lens, max_kv), table, page, D ** -0.5, True, 0, T)
+    for b in range(2):
+        n = min(max_q, int(cu[b + 1] - cu[b]))
+        sel = slice(int(cu[b]), int(cu[b]) + n)
+        ref.assert_attention(got[sel], None, tuple(x[sel] for x in want))
+        assert np.all(got[int(cu[b]) + n: int(cu[b + 1])] == 7.0)
+
+
+def test_attention_with_extreme_scores(B):
+    """One key that carries everything, scores of +-1000, equal keys, and a scale of its own."""
+    import torch
+    rng = np.random.default_rng(9)
+    hq, hkv, D, page = 2, 1, 64, 16
+    for n, qn in ((200, 1), (200, 100)):
+        cache, (kv, vv), qd, q, cu, lens, table, T = attend_case(rng, B, [n], [qn], hq, hkv, D, page)
+        kc, ks = cache.k_codes.cpu().numpy(), cache.k_scales.cpu().numpy()
+        ks[...] = np.where(ks == 255, 255, ks + 6)
+        kc[table[0, 3], 0, 5] = 0x38
+        ks[table[0, 3], 0, :, 5] = 133
+        cache = B.PagedCache(cache.num_pages, page, hkv, D, tensors=[dev(kc), dev(ks), cache.v_codes, cache.v_scales])
+        with np.errstate(invalid="ignore"):
+            kv = ref.cache_values(kc, ks)
+        for scale in (D ** -0.5, 1.0, 1e-3):
+            got, lse = run_attention(B, cache, qd, cu, lens, table, T, hq, scale=scale)
+            ref.assert_attention(got, lse, ref.attention(kv, vv, q, cu, lens, table, page, scale, True, 0, T))
+
+
+def test_attention_past_four_gigabytes(B):
+    """Offsets into the code arrays beyond 32 bits: two pages at either end of a pool of 4.3 GB per array."""
+    import torch
+    rng = np.random.default_rng(10)
+    hq, hkv, D, page = 4, 1, 128, 256
+    pages = (1 << 32) // (page * D) + 2000
+    cache = B.PagedCache(pages, page, hkv, D)
+    L = 300
+    ids = np.array([[pages - 1, 3]], np.int32)
+    X = to_dev(ref.bf16_values(rng, L, 2 * D)[0], "bf16")
+    t = np.arange(L)
+    slots = ids[0].astype(np.int64)[t // page] * page + t % page
+    B.batq_kv_paged_append(cache, X[:, :D], X[:, D:], dev(slots))
+    bits, q = ref.bf16_values(rng, 2, hq * D)
+    lens, cu = np.array([L], np.int32), np.array([0, 2], np.int32)
+    got, lse = run_attention(B, cache, to_dev(bits, "bf16"), cu, lens, ids, 2, hq)
+    small = [a[torch.tensor(ids[0].astype(np.int64), device="cuda")].cpu().numpy() for a in (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)]
+    kv, vv = ref.cache_values(small[0], small[1]), ref.cache_values(small[2], small[3])
+    x = X[:, :D].float().cpu().numpy()
+    # the keys are there: half a step of 3 mantissa bits is |x| / 16; of a block whose maximum is a = (1.75 .. 2) 2^f the
+    # elements above 448 2^(f - 8) = 1.75 2^f saturate, which takes at most (2 - 1.75) / 2 = 1 / 8 of them; the smallest
+    # step of a block with a < 8 is 2^(2 - 8 - 9)
+    assert bool(np.all(np.abs(kv[:, 0].reshape(-1, D)[:L] - x) <= np.abs(x) / 8 + 2.0 ** -15))
+    ref.assert_attention(got, lse, ref.attention(kv, vv, q.reshape(2, hq, D).astype(np.float64), cu, lens, np.array([[0, 1]]), page, D ** -0.5, True, 0, 2))
+
+
+def test_attention_is_repeatable_and_runs_on_a_side_stream_and_in_graphs(B):
+    """Same bits on another stream and from replays of two graphs that share one workspace, with eager work and a
+    moved cache state in between (lengths live on the device)."""
+    import torch
+    rng = np.random.default_rng(11)
+    hq, hkv, D, page = 8, 2, 128, 16
+    cache, (kv, vv), qd, q, cu, lens, table, T = attend_case(rng, B, [5000, 333, 1], [1, 1, 1], hq, hkv, D, page)
+    dcu, dlens, dtable = dev(cu), dev(lens), dev(table)
+    n = B.batq_paged_attention_workspace(cache, hq, 3, T, 1, 5000)
+    ws = torch.full((max(n, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+    args = (dcu, dlens, dtable, 1, 5000)
+    want = B.batq_paged_attention(cache, qd, *args, workspace=ws)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        o2 = B.batq_paged_attention(cache, qd, *args, workspace=ws)
+    side.synchronize()
+    assert torch.equal(o2, want)
+    outs, graphs = [torch.zeros_like(want) for _ in range(2)], [torch.cuda.CUDAGraph() for _ in range(2)]
+    for g, oo in zip(graphs, outs):
+        with torch.cuda.graph(g, stream=side):
+            B.batq_paged_attention(cache, qd, *args, out=oo, workspace=ws)
+    for rep in range(3):
+        dlens.copy_(torch.tensor([5000 - 1000 * rep, 333 - rep, 1], dtype=torch.int32))
+        want = B.batq_paged_attention(cache, qd, *args)
+        junk = torch.randn(300, 300, device="cuda") @ torch.randn(300, 300, device="cuda")
+        for oo in outs:
+            oo.zero_()
+        torch.cuda.synchronize()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(oo, want) for oo in outs), rep
+        assert bool(torch.isfinite(junk).all())
+
+
+# ---------------------------------------------------------------------------------------- together
+@pytest.mark.parametrize("transforms", [False, True])
+def test_a_serving_step_end_to_end(B, transforms):
+    """Fused projection (W4A8) with adapters, append, attention, the way back through T_v^-1: two sequences are
+    prefilled and then decoded in a captured step that is replayed at moving positions (they live on the device)."""
+    import torch
+    rng = np.random.default_rng(12)
+    K, hq, hkv, D, page = 256, 4, 2, 64, 16
+    N = (hq + 2 * hkv) * D
+    w = bi.make_small(8, K, N, seed=2, dtype="bf16")
+    t = B.Transform(K, w.G, w.P, w.clip)
+    wh = B.batq_prepare_weight(t, to_dev(w.W, "bf16"))
+    A = to_dev(ref.bf16_values(rng, 2, 8, K, scale=K ** -0.5)[0], "bf16")
+    Bm = to_dev(ref.bf16_values(rng, 2, N, 8, scale=8 ** -0.5)[0], "bf16")
+    tk = tv = to = None
+    if transforms:
+        tk, tv = _transforms(B, rng, hkv, D, "kron", clip=False)[0], None
+        G = (np.eye(4) + 0.05 * rng.standard_normal((4, 4))).astype(np.float32)
+        P = (np.eye(8) + 0.05 * rng.standard_normal((hkv, D // 32, 8, 8))).astype(np.float32)
+        tv = B.Transform(hkv * D, G, P.reshape(-1, 8, 8), None)
+        to = B.Transform(hq * D, G, np.repeat(P, hq // hkv, 0).reshape(-1, 8, 8), None)
+    cache = B.PagedCache(12, page, hkv, D)
+    rope = dev(ref.rope_table(200, D))
+    order = rng.permutation(12)
+    table = np.stack([order[:6], order[6:]]).astype(np.int32)
+    dtable = dev(table)
+    lens0, steps = np.array([37, 20]), 14
+    tokens = to_dev(ref.bf16_values(rng, 2, 80, K)[0], "bf16")       # inputs of both sequences
+
+    def slots_of(b, p):
+        return table[b][p // page].astype(np.int64) * page + p % page
+
+    def layer(X, index, slots, pos, cu, lens, max_q, out=None, work=None):
+        Y = B.batq_linear_a8w4(t, wh, X, torch.bfloat16)
+        Y = B.batq_lora_add(X, A, Bm, index, Y, out=Y)
+        q, k, v = Y.split((hq * D, hkv * D, hkv * D), 1)
+        qr = B.batq_kv_paged_append(cache, k, v, slots, pos, q=q, rope=rope, tk=tk, tv=tv)
+        oo = B.batq_paged_attention(cache, qr, cu, lens, dtable, max_q, 96, out=out)
+        return Y, (oo if to is None else B.batq_transform_apply(to, oo, B.APPLY_INVERSE))
+
+    # what the cache should stand for, kept on the side in fp32 from the same projection outputs
+    kept = [[], []]
+
+    def check(Y, out, rows):
+        Yf, got = y_to_f32(Y), y_to_f32(out).astype(np.float64).reshape(len(rows), hq, D)
+        tab = ref.rope_table(200, D)
+        for r, (b, p) in enumerate(rows):
+            q, k, v = np.split(Yf[r], [hq * D, (hq + hkv) * D])
+            kept[b].append((ref.rotate(k.reshape(1, hkv, D), tab, [p], D, False)[0], v.reshape(hkv, D)))
+        for r, (b, p) in enumerate(rows):
+            q = ref.rotate(Yf[r, : hq * D].reshape(1, hq, D), tab, [p], D, False)[0].astype(np.float64)
+            kk = np.stack([x for x, _ in kept[b][: p + 1]]).astype(np.float64)
+            vv = np.stack([x for _, x in kept[b][: p + 1]]).astype(np.float64)
+            for h in range(hq):
+                s = kk[:, h // 2] @ q[h] / np.sqrt(D)
+                pr = np.exp(s - s.max())
+                pr /= pr.sum()
+                want = pr @ vv[:, h // 2]
+                # keys and values carry 4 significant bits (2^-4 of an element, more of small ones in a block): scores
+                # move by about 2^-4 |q| |k| / sqrt(D) and outputs with them; a wrong rotation, page or head is off by 1
+                bound = 0.35 * np.sqrt((vv[:, h // 2] ** 2).mean())
+                assert np.sqrt(((got[r, h] - want) ** 2).mean()) <= bound, (r, b, p, h)
+
+    rows = [(b, p) for b in range(2) for p in range(lens0[b])]
+    X = torch.cat([tokens[b, : lens0[b]] for b in range(2)])
+    Y, out = layer(X, dev(np.array([b for b, _ in rows], np.int32)), dev(np.array([slots_of(b, p) for b, p in rows])),
+                   dev(np.array([p for _, p in rows], np.int32)), dev(np.array([0, lens0[0], lens0.sum()], np.int32)),
+                   dev(lens0.astype(np.int32)), int(lens0.max()))
+    torch.cuda.synchronize()
+    check(Y, out, rows)
+    # the decode step, captured once
+    sX = torch.zeros((2, K), dtype=torch.bfloat16, device="cuda")
+    index, cu = dev(np.array([0, 1], np.int32)), dev(np.array([0, 1, 2], np.int32))
+    slots, pos, lens = dev(np.zeros(2, np.int64) - 1), dev(np.zeros(2, np.int32)), dev(np.ones(2, np.int32))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        layer(sX, index, slots, pos, cu, lens, 1)           # first calls outside the capture (slots -1: nothing is written)
+    side.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        gY, gout = layer(sX, index, slots, pos, cu, lens, 1)
+    for step in range(steps):
+        p = lens0 + step
+        sX.copy_(torch.stack([tokens[b, int(p[b])] for b in range(2)]))
+        slots.copy_(dev(np.array([slots_of(b, p[b]) for b in range(2)])))
+        pos.copy_(dev(p.astype(np.int32)))
+        lens.copy_(dev((p + 1).astype(np.int32)))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        check(gY, gout, [(b, int(p[b])) for b in range(2)])

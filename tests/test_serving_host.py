@@ -1,0 +1,117 @@
+"""Refusals of the serving calls: every argument is looked at on the host, before any device is touched."""
+import ctypes as C
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def B():
+    import paper_2603_16590_amd as b
+    return b
+
+
+class Cache(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("num_pages", "page_size", "kv_heads", "head_dim")] + \
+               [(n, C.c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales")]
+
+
+class Rope(C.Structure):
+    _fields_ = [("table", C.c_void_p)] + [(n, C.c_int) for n in ("positions", "rotary_dim", "interleaved")]
+
+
+class Batch(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("cu_q", "kv_len", "page_table")] + \
+               [(n, C.c_int) for n in ("batch", "table_width", "total_q", "max_q", "max_kv")]
+
+
+P = 1 << 20                                                 # an aligned address that is never followed
+
+
+def cache(**kw):
+    return Cache(**{**dict(num_pages=4, page_size=16, kv_heads=2, head_dim=64, k_codes=P, k_scales=P, v_codes=P, v_scales=P), **kw})
+
+
+def test_sizes(B):
+    f, g = B.lib.batq_kv_paged_code_bytes, B.lib.batq_kv_paged_scale_bytes
+    assert f(4, 16, 2, 64) == 4 * 16 * 2 * 64 and g(4, 16, 2, 64) == 4 * 16 * 2 * 2
+    assert f(1 << 20, 256, 8, 128) == 1 << 38               # past 32 bits
+    for bad in ((0, 16, 2, 64), (4, 8, 2, 64), (4, 24, 2, 64), (4, 512, 2, 64), (4, 16, 0, 64), (4, 16, 2, 96), (-1, 16, 2, 128)):
+        assert f(*bad) == 0 and g(*bad) == 0
+    w = B.lib.batq_lora_workspace
+    assert w(4, 64, 64, 8, 1) % 4 == 0
+    for bad in ((-1, 64, 64, 8, 1), (4, 48, 64, 8, 1), (4, 64, 0, 8, 1), (4, 64, 64, 12, 1), (4, 64, 64, 136, 1), (4, 64, 64, 8, 0)):
+        assert w(*bad) == 0
+
+
+def append(B, c, rope=None, q=None, ldq=0, q_heads=0, q_out=None, ldqo=0, k=P, ldk=128, v=P, ldv=128, dt=1, pos=P, slots=P, M=4, tk=None):
+    return B.lib.batq_kv_paged_append(C.byref(c) if c is not None else None, tk, None, C.byref(rope) if rope is not None else None,
+                                      q, ldq, q_heads, q_out, ldqo, k, ldk, v, ldv, dt, pos, slots, M, None)
+
+
+def test_append_refusals(B):
+    ok = cache()
+    assert append(B, None) == 1
+    for kw, want in ((dict(head_dim=96), 4), (dict(page_size=24), 2), (dict(num_pages=0), 2), (dict(kv_heads=0), 2),
+                     (dict(k_codes=None), 1), (dict(v_scales=None), 1), (dict(k_scales=P + 8), 2)):
+        assert append(B, cache(**kw)) == want, kw
+    for kw, want in ((dict(dt=2), 3), (dict(M=-1), 2), (dict(ldk=127), 2), (dict(ldv=120), 2), (dict(k=None), 1), (dict(v=None), 1),
+                     (dict(slots=None), 1), (dict(slots=P + 4), 2), (dict(k=P + 2), 2), (dict(ldk=132), 2),
+                     (dict(q_heads=3), 2), (dict(q_heads=-2), 2), (dict(q=P, q_heads=0), 1),
+                     (dict(q_heads=2, ldq=128, ldqo=128, q_out=P), 1), (dict(q_heads=2, ldq=128, ldqo=128, q=P), 1),
+                     (dict(q_heads=2, ldq=120, ldqo=128, q=P, q_out=2 * P), 2), (dict(q_heads=2, ldq=128, ldqo=120, q=P, q_out=2 * P), 2),
+                     (dict(q_heads=2, ldq=128, ldqo=128, q=P, q_out=P), 2), (dict(q_heads=2, ldq=128, ldqo=132, q=P, q_out=2 * P), 2)):
+        assert append(B, ok, **kw) == want, kw
+    for r, want in ((Rope(None, 10, 64, 0), 1), (Rope(P, 0, 64, 0), 2), (Rope(P, 10, 24, 0), 2), (Rope(P, 10, 80, 0), 2),
+                    (Rope(P, 10, 0, 0), 2), (Rope(P + 4, 10, 64, 0), 2)):
+        assert append(B, ok, rope=r) == want
+    assert append(B, ok, rope=Rope(P, 10, 64, 0), pos=None) == 1
+    assert append(B, ok, rope=Rope(P, 10, 64, 0), pos=P + 2) == 2
+    assert append(B, ok, M=0, k=None, v=None, slots=None) == 0
+
+
+def attend(B, c, q=P, ldq=256, q_heads=4, scale=0.1, window=0, out=2 * P, ldo=256, lse=None, ws=None, wsb=0, **kw):
+    b = Batch(**{**dict(cu_q=P, kv_len=P, page_table=P, batch=2, table_width=3, total_q=5, max_q=4, max_kv=48), **kw})
+    return B.lib.batq_paged_attention(C.byref(c) if c is not None else None, C.byref(b), q, ldq, q_heads, scale, 1, window, out, ldo,
+                                      lse, ws, wsb, None)
+
+
+def test_attention_refusals(B):
+    ok = cache()
+    assert attend(B, None) == 1
+    assert B.lib.batq_paged_attention(C.byref(ok), None, P, 256, 4, 0.1, 1, 0, 2 * P, 256, None, None, 0, None) == 1
+    assert attend(B, cache(head_dim=32)) == 4 and attend(B, cache(page_size=0)) == 2 and attend(B, cache(v_codes=None)) == 1
+    for kw, want in ((dict(q_heads=3), 2), (dict(q_heads=0), 2), (dict(q_heads=2 * 130), 2), (dict(ldq=255), 2), (dict(ldo=200), 2),
+                     (dict(ldq=260), 2), (dict(batch=-1), 2), (dict(total_q=-1), 2), (dict(max_q=-1), 2), (dict(max_kv=-1), 2),
+                     (dict(table_width=-1), 2), (dict(window=-1), 2), (dict(scale=0.0), 2), (dict(scale=float("nan")), 2),
+                     (dict(scale=float("inf")), 2), (dict(q=None), 1), (dict(out=None), 1), (dict(cu_q=None), 1), (dict(kv_len=None), 1),
+                     (dict(page_table=None), 1), (dict(q=P + 2), 2), (dict(out=P), 2), (dict(cu_q=P + 2), 2), (dict(lse=P + 1), 2),
+                     (dict(ws=P + 16), 2), (dict(total_q=1 << 30), 2)):
+        assert attend(B, ok, **kw) == want, kw
+    for kw in (dict(batch=0), dict(total_q=0), dict(max_q=0)):
+        assert attend(B, ok, **{**kw, "q": None, "out": None}) == 0
+    assert B.lib.batq_paged_attention_workspace(None, 4, 1, 1, 1, 100) == 0
+    assert B.lib.batq_paged_attention_workspace(C.byref(ok), 3, 1, 1, 1, 100) == 0
+
+
+def lora(B, X=P, xdt=1, M=4, K=64, ldx=64, A=P, Bm=P, N=40, rank=8, n=2, scales=P, index=P, base=P, ldb=40, out=2 * P, ldo=40, ydt=1, ws=P, wsb=1 << 20):
+    return B.lib.batq_lora_add(X, xdt, M, K, ldx, A, Bm, N, rank, n, scales, index, base, ldb, out, ldo, ydt, ws, wsb, None)
+
+
+def test_lora_refusals(B):
+    for kw, want in ((dict(xdt=5), 3), (dict(ydt=-1), 3), (dict(M=-1), 2), (dict(K=48), 2), (dict(K=0), 2), (dict(N=0), 2), (dict(rank=4), 2),
+                     (dict(rank=20), 2), (dict(rank=136), 2), (dict(n=0), 2), (dict(ldx=63), 2), (dict(ldx=68), 2), (dict(ldb=39), 2),
+                     (dict(ldo=39), 2), (dict(X=None), 1), (dict(A=None), 1), (dict(Bm=None), 1), (dict(index=None), 1), (dict(out=None), 1),
+                     (dict(X=P + 8), 2), (dict(A=P + 2), 2), (dict(Bm=P + 2), 2), (dict(index=P + 2), 2), (dict(scales=P + 2), 2),
+                     (dict(out=P + 1), 2), (dict(base=P + 1), 2), (dict(ws=P + 64), 2), (dict(out=P), 2), (dict(base=2 * P, ldb=48), 2)):
+        assert lora(B, **kw) == want, kw
+    assert lora(B, M=0, X=None, A=None, Bm=None, index=None, out=None) == 0
+
+
+def test_binding_refusals(B):
+    torch = pytest.importorskip("torch")
+    with pytest.raises(ValueError):
+        B.PagedCache(4, 24, 2, 64)
+    with pytest.raises(ValueError):
+        B.batq_lora_add(torch.zeros(2, 64), torch.zeros(1, 8, 32).bfloat16(), torch.zeros(1, 4, 8).bfloat16(), torch.zeros(2, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        B.batq_lora_add(torch.zeros(2, 32), torch.zeros(1, 8, 32), torch.zeros(1, 4, 8).bfloat16(), torch.zeros(2, dtype=torch.int32))
