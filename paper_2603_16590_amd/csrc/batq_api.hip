@@ -918,9 +918,11 @@ static batq_status check_attention_dims(const batq_paged_cache* c, int q_heads, 
     if (!c) return BATQ_ERR_NULL;
     if (batq_status st = check_paged_dims(c->num_pages, c->page_size, c->kv_heads, c->head_dim); st != BATQ_OK) return st;
     if (q_heads < 1 || q_heads % c->kv_heads != 0 || q_heads / c->kv_heads > 128) return BATQ_ERR_SHAPE;
-    if (batch < 0 || batch > (1 << 20) || total_q < 0 || max_q < 0 || max_kv < 0 ||
+    if (batch < 0 || batch > (1 << 20) || total_q < 0 || max_q < 0 || max_kv < 0 || max_kv > (1 << 30) ||
         (int64_t)total_q * q_heads > INT32_MAX || (int64_t)max_q * q_heads > INT32_MAX)
         return BATQ_ERR_SHAPE;
+    // workgroups are numbered with 32 bits: the shortest parts are 256 tokens
+    if ((int64_t)batch * c->kv_heads * (max_kv / 256 + 2) > INT32_MAX) return BATQ_ERR_SHAPE;
     return BATQ_OK;
 }
 
