@@ -14,6 +14,7 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -28,11 +29,13 @@ struct AttnArgs {
     int causal, window;
     float scale;                                            // times log2 e: scores are kept in units of ln 2
     // sequences of at most few_rows rows (query tokens x heads of a group) belong to attend_few, the others to
-    // attend_rows; parts of few_len tokens
+    // attend_many; parts of few_len and many_len tokens
     int few_rows, few_len, max_parts;
     int part_rows;                                          // rows of a (sequence, key head) that partial results have room for
     float* part_o;                                          // [sequence][key head][row][part][D]: sums with the part's own maximum
     float* part_ml;                                         // [sequence][key head][row][part][2]: maximum, sum of the weights
+    int many_len, many_parts;
+    float *many_o, *many_ml;                                // likewise [row of q][query head][part]
 };
 
 // Sequence b as the kernels take it: nothing in the lists is trusted.
@@ -55,11 +58,15 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
     return s;
 }
 
-// Parts of part_len tokens that a sequence is cut into (counted from its first visible token's block of 64; at least one,
-// which writes the zeros of rows that see nothing).
-__device__ __forceinline__ int live_parts(const Seq& s, int part_len) {
-    return max(1, (s.t_hi - (s.t_lo & ~63) + part_len - 1) / part_len);
+// Tokens [lo, hi) that some row of a workgroup sees, and the parts of part_len tokens that they are cut into (counted
+// from the block of 64 with the first of them; at least one, which writes the zeros of rows that see nothing).
+struct TokenRange {
+    int lo, hi;
+};
+__device__ __forceinline__ int range_parts(const TokenRange& t, int part_len) {
+    return max(1, (t.hi - (t.lo & ~63) + part_len - 1) / part_len);
 }
+__device__ __forceinline__ int live_parts(const Seq& s, int part_len) { return range_parts(TokenRange{s.t_lo, s.t_hi}, part_len); }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -328,11 +335,49 @@ attend_few(const AttnArgs a) {
     }
 }
 
-// Joins the parts of sequences that were cut, in part order: one wave per row of a (sequence, key head).
+// Joins the parts of a row, in part order, by one wave; `at` is the row's first part.
+template <int D>
+__device__ __forceinline__ void join_row(const AttnArgs& a, const float* part_o, const float* part_ml, size_t at, int parts,
+                                         size_t row, int head) {
+    const int lane = threadIdx.x & 63;
+    float top = -INFINITY;
+    for (int p = lane; p < parts; p += 64) top = __builtin_fmaxf(top, part_ml[2 * (at + p)]);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) top = __builtin_fmaxf(top, shuffle_xor(top, d));
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f, v[D / 64] = {};
+    for (int p0 = 0; p0 < parts; p0 += 64) {
+        const int p = p0 + lane;
+        const float f = p < parts ? exp2_(part_ml[2 * (at + p)] - ref) : 0.0f;
+        sum += p < parts ? f * part_ml[2 * (at + p) + 1] : 0.0f;
+        const int count = min(64, parts - p0);
+        for (int j0 = 0; j0 < count; j0 += 8) {             // eight loads in flight; past the end: the last part, weight 0
+            float x[8][D / 64];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int c = 0; c < D / 64; ++c) x[j][c] = part_o[(at + p0 + min(j0 + j, count - 1)) * D + lane * (D / 64) + c];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float fj = j0 + j < count ? __shfl(f, j0 + j) : 0.0f;
+#pragma unroll
+                for (int c = 0; c < D / 64; ++c) v[c] = __builtin_fmaf(fj, x[j][c], v[c]);
+            }
+        }
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) sum += shuffle_xor(sum, d);
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    __bf16* o = reinterpret_cast<__bf16*>(a.out + row * a.ldo + (size_t)head * D + lane * (D / 64));
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) o[c] = (__bf16)(v[c] * inv);
+    if (a.lse && lane == 0) a.lse[row * a.q_heads + head] = sum > 0.0f ? (top + __log2f(sum)) * 0.69314718055994531f : -INFINITY;
+}
+
+// One wave per row of a (sequence, key head) of few rows.
 template <int D>
 __global__ void __launch_bounds__(256)
-join_parts(const AttnArgs a) {
-    const int lane = threadIdx.x & 63;
+join_few(const AttnArgs a) {
     const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t bh = unit / a.part_rows;
     const int r = (int)(unit - bh * a.part_rows), h = (int)(bh % a.kv_heads), b = (int)(bh / a.kv_heads);
@@ -340,108 +385,320 @@ join_parts(const AttnArgs a) {
     const Seq s = sequence(a, b);
     const int rows = s.n * a.group;
     if (r >= rows || rows > a.few_rows) return;
-    const size_t row = (size_t)s.begin + r / a.group;
-    const int head = h * a.group + r % a.group;
     const int parts = live_parts(s, a.few_len);
     if (parts == 1) return;
-    const size_t at = (size_t)unit * a.max_parts;
-    float top = -INFINITY;
-    for (int p = lane; p < parts; p += 64) top = __builtin_fmaxf(top, a.part_ml[2 * (at + p)]);
-#pragma unroll
-    for (int d = 32; d; d >>= 1) top = __builtin_fmaxf(top, shuffle_xor(top, d));
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, v[D / 64] = {};
-    for (int p0 = 0; p0 < parts; p0 += 64) {
-        const int p = p0 + lane;
-        const float f = p < parts ? exp2_(a.part_ml[2 * (at + p)] - ref) : 0.0f;
-        const float w = p < parts ? f * a.part_ml[2 * (at + p) + 1] : 0.0f;
-        sum += w;
-        const int count = min(64, parts - p0);
-#pragma unroll 8
-        for (int j = 0; j < count; ++j) {
-            const float fj = __shfl(f, j);
-#pragma unroll
-            for (int c = 0; c < D / 64; ++c) v[c] = __builtin_fmaf(fj, a.part_o[(at + p0 + j) * D + lane * (D / 64) + c], v[c]);
-        }
-    }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) sum += shuffle_xor(sum, d);
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-    uint16_t* o = a.out + row * a.ldo + (size_t)head * D + lane * (D / 64);
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c) reinterpret_cast<__bf16*>(o)[c] = (__bf16)(v[c] * inv);
-    if (a.lse && lane == 0) a.lse[row * a.q_heads + head] = sum > 0.0f ? (top + __log2f(sum)) * 0.69314718055994531f : -INFINITY;
+    join_row<D>(a, a.part_o, a.part_ml, (size_t)unit * a.max_parts, parts, (size_t)s.begin + r / a.group, h * a.group + r % a.group);
 }
 
-// One wave per (row of q, query head): a lane takes a key of 64 at a time, then a channel (or two) of the values.
+// Many query rows to a key head (prompts, chunks of prompts): bound by the matrix pipe, the exponentials and LDS reads.
+// A workgroup of eight waves takes 256 rows (row = query token * group + head of the group) of one (sequence, key head), 32
+// to a wave, and walks the visible tokens in tiles of 64.  The codes of the next tile are requested while this one is
+// worked on, converted once for all eight waves and written to LDS as bf16:
+//   keys    [64][D] in chunks of 8 channels, values transposed, [D][64] in chunks of 8 tokens (chunk 2j + h of tokens
+//           16j + 4h .. + 3 and 16j + 8 + 4h .. + 3: those whose weights lane half h holds); a chunk's place in its row is
+//           XORed with the row's number so that 16 lanes that read a chunk of 16 rows reach all banks
+//   scores  result element r of 32-token tile x in lane (n, h) = (l % 32, l / 32) is row n, token 32x + 8 (r / 4) + 4h + r % 4
+// The weights are rounded to bf16 once (2^-8 at most): two terms would add half of the products again.  The reference
+// of the exponentials moves only when a row's maximum has grown by more than 2^8, which spares most rescalings of O.
+constexpr int kManyRows = 256;
+
 template <int D>
-__global__ void __launch_bounds__(64)
-attend_rows(const AttnArgs a) {
-    __shared__ float sq[D];
-    const int lane = threadIdx.x, row = blockIdx.x, head = blockIdx.y, kvh = head / a.group;
-    int b = 0, begin = 0, end = 0;
-    for (; b < a.batch; ++b) {
-        begin = a.cu_q[b], end = a.cu_q[b + 1];
-        if (begin >= 0 && row >= begin && row < end && end <= a.total_q) break;
+__device__ __forceinline__ int k_place(int row, int chunk) { return D == 128 ? chunk ^ (row & 15) : chunk ^ ((row >> 1) & 7); }
+__device__ __forceinline__ int v_place(int row, int chunk) { return chunk ^ (((row >> 1) ^ (row >> 4)) & 7); }
+
+template <int D>
+constexpr int many_lds() { return 4 * 64 * D * 2 + 2 * 16; }   // two buffers of keys and values, which 16-token groups exist
+
+// Tokens that some row of a sequence's 256-row tile sees.
+__device__ __forceinline__ TokenRange tile_tokens(const AttnArgs& a, const Seq& s, int tile) {
+    const int i0 = tile * kManyRows / a.group, i1 = (min(s.n * a.group, (tile + 1) * kManyRows) - 1) / a.group;
+    TokenRange t;
+    t.hi = a.causal ? max(0, min(s.len, s.first_pos + i1 + 1)) : s.len;
+    t.lo = a.window ? min(t.hi, max(0, s.first_pos + i0 - a.window + 1)) : 0;
+    return t;
+}
+
+// The sequence and 256-row tile of workgroup tile `x`, last ones first (they see the most tokens); b < 0: none.
+__device__ __forceinline__ void find_tile(const AttnArgs& a, int x, int* b, int* tile) {
+    const int lane = threadIdx.x & 63;
+    auto tiles_of = [&](int i) {
+        if (i >= a.batch) return 0;
+        const Seq s = sequence(a, i);
+        const int rows = s.n * a.group;
+        return rows > a.few_rows ? (rows + kManyRows - 1) / kManyRows : 0;
+    };
+    int total = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 64) {
+        int c = tiles_of(b0 + lane);
+#pragma unroll
+        for (int d = 32; d; d >>= 1) c += __shfl_xor(c, d);
+        total += c;
     }
-    if (b == a.batch || row - begin >= a.max_q || min(end - begin, a.max_q) * a.group <= a.few_rows) return;
-    int64_t width = (int64_t)a.table_width << a.page_shift;
-    const int len = (int)min((int64_t)max(0, min(a.kv_len[b], a.max_kv)), width);
-    const int pos = len - (end - begin) + (row - begin);
-    const int t1 = a.causal ? min(len, pos + 1) : len;
-    const int t0 = a.window ? max(0, pos - a.window + 1) : 0;
-    for (int i = lane; i < D; i += 64) sq[i] = bf16_bits_to_float(a.q[(size_t)row * a.ldq + (size_t)head * D + i]);
-    __syncthreads();
-    float m = -INFINITY, l = 0.0f, o[D / 64] = {};
-    const int page_mask = (1 << a.page_shift) - 1;
-    for (int t = t0 & ~63; t < t1; t += 64) {
-        const int tt = t + lane;
-        float s = -INFINITY;
-        if (tt >= t0 && tt < t1) {
-            const int page = a.page_table[(size_t)b * a.table_width + (tt >> a.page_shift)];
-            if (page >= 0 && page < a.num_pages) {
-                const int64_t ph = (int64_t)page * a.kv_heads + kvh;
-                const uint8_t* kc = a.k_codes + (((ph << a.page_shift) + (tt & page_mask)) * D);
-                s = 0.0f;
-                for (int blk = 0; blk < D / 32; ++blk) {
-                    const float sc = scale_operand(a.k_scales[((ph * (D / 32) + blk) << a.page_shift) + (tt & page_mask)]);
-                    for (int i = 0; i < 8; ++i) {
-                        const uint32_t w = reinterpret_cast<const uint32_t*>(kc + blk * 32)[i];
-                        const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, sc, false);
-                        const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, sc, true);
-                        const float* qq = sq + blk * 32 + 4 * i;
-                        s += lo[0] * qq[0] + lo[1] * qq[1] + hi[0] * qq[2] + hi[1] * qq[3];
+    *b = -1, *tile = 0;
+    int left = total - 1 - x;                               // the tile's number from the front
+    if (left < 0) return;
+    for (int b0 = 0; b0 < a.batch; b0 += 64) {
+        const int c = tiles_of(b0 + lane);
+        int sum = c;                                        // inclusive prefix sum over the lanes
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int v = __shfl_up(sum, d);
+            if (lane >= d) sum += v;
+        }
+        const uint64_t past = __ballot(sum > left);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            *b = __builtin_amdgcn_readfirstlane(b0 + l);
+            *tile = __builtin_amdgcn_readfirstlane(left - __shfl(sum - c, l));
+            return;
+        }
+        left -= __shfl(sum, 63);
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(512, 2)
+attend_many(const AttnArgs a) {
+    constexpr int kU = D / 16, kCb = D / 32, kHalf = 64 * D * 2;
+    extern __shared__ __align__(16) uint8_t lds[];
+    uint8_t* const s_k = lds;                               // [2][64][D] bf16
+    uint8_t* const s_v = lds + 2 * kHalf;                   // [2][D][64] bf16
+    uint8_t* const s_ok = lds + 4 * kHalf;                  // [2][4]: whether the page of 16 tokens exists
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 31, hh = lane >> 5;
+    const int h = blockIdx.x % a.kv_heads, xp = blockIdx.x / a.kv_heads;
+    const int part = xp % a.many_parts;
+    int b, tile;
+    find_tile(a, xp / a.many_parts, &b, &tile);
+    if (b < 0) return;
+    const Seq s = sequence(a, b);
+    const int rows = s.n * a.group, row0 = tile * kManyRows;
+    const TokenRange range = tile_tokens(a, s, tile);
+    const int parts = range_parts(range, a.many_len);
+    if (part >= parts) return;
+    const int t_begin = (range.lo & ~63) + part * a.many_len, t_end = min(range.hi, t_begin + a.many_len);
+
+    // this lane's row
+    const int r = row0 + wave * 32 + n, i = r / a.group;
+    const bool live = r < rows;
+    const int head = h * a.group + (live ? r - i * a.group : 0);
+    const size_t row = (size_t)(s.begin + (live ? i : 0));
+    bf16x8 qf[kU];
+    {
+        const uint16_t* p = a.q + row * a.ldq + (size_t)head * D + 8 * hh;
+#pragma unroll
+        for (int u = 0; u < kU; ++u) qf[u] = *reinterpret_cast<const bf16x8*>(p + 16 * u);
+    }
+    const int pos = s.first_pos + i;
+    const int row_hi = !live ? 0 : a.causal ? min(s.len, pos + 1) : s.len;
+    const int row_lo = a.window ? max(0, pos - a.window + 1) : 0;
+    // the wave's rows: [some_lo, some_hi) is seen by some, [all_lo, all_hi) by all of them
+    const int wr0 = row0 + wave * 32, wr1 = min(rows, wr0 + 32) - 1;
+    const bool wave_live = wr0 < rows;
+    const int wp0 = s.first_pos + wr0 / a.group, wp1 = s.first_pos + wr1 / a.group;
+    const int some_hi = !wave_live ? 0 : a.causal ? min(s.len, wp1 + 1) : s.len, some_lo = a.window ? max(0, wp0 - a.window + 1) : 0;
+    const int all_hi = a.causal ? min(s.len, wp0 + 1) : s.len, all_lo = a.window ? max(0, wp1 - a.window + 1) : 0;
+
+    // staging: a thread converts 16 channels of a key and a 4 x 4 tile of values (D = 64: one or the other)
+    const int32_t* table = a.page_table + (size_t)b * a.table_width;
+    const int page_mask = (1 << a.page_shift) - 1, last_page = max(0, (s.len - 1) >> a.page_shift);
+    constexpr int kKc = D / 16;                             // 16-channel chunks of a key
+    const int id = D == 128 ? tid : tid & 255;
+    const bool do_k = D == 128 || tid < 256, do_v = D == 128 || tid >= 256;
+    const int k_tok = id / kKc, k_c = id % kKc;
+    const int v_quad = id / (D / 4), v_c = id % (D / 4);    // tokens 4 v_quad .. + 3, channels 4 v_c .. + 3
+    auto entry = [&](int t) { return table[min(t >> a.page_shift, last_page)]; };
+    u32x4 kw = {};
+    uint32_t kscale = 0, vw[4] = {}, vscale = 0;
+    bool k_ok = false, v_ok = false;
+    auto request = [&](int t, int kp, int vp) {
+        if (do_k) {
+            k_ok = (uint32_t)kp < (uint32_t)a.num_pages;
+            const int64_t ph = (int64_t)(k_ok ? kp : 0) * a.kv_heads + h;
+            const int off = (t + k_tok) & page_mask;
+            kw = *reinterpret_cast<const u32x4*>(a.k_codes + ((ph << a.page_shift) + off) * D + k_c * 16);
+            kscale = a.k_scales[((ph * (D / 32) + k_c / 2) << a.page_shift) + off];
+        }
+        if (do_v) {
+            v_ok = (uint32_t)vp < (uint32_t)a.num_pages;
+            const int64_t ph = (int64_t)(v_ok ? vp : 0) * a.kv_heads + h;
+            const int off = (t + 4 * v_quad) & page_mask;
+            const uint8_t* p = a.v_codes + ((ph << a.page_shift) + off) * D + v_c * 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vw[e] = *reinterpret_cast<const uint32_t*>(p + e * D);
+            vscale = *reinterpret_cast<const uint32_t*>(a.v_scales + ((ph * (D / 32) + v_c / 8) << a.page_shift) + off);
+        }
+    };
+    auto stage = [&](int t, int buf) {                      // the requested tile (first token t) into LDS
+        if (do_k) {
+            const float sc = scale_operand(kscale);
+            uint8_t* row_k = s_k + buf * kHalf + k_tok * (D * 2);
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                *reinterpret_cast<u32x4*>(row_k + k_place<D>(k_tok, 2 * k_c + e) * 16) =
+                    u32x4{cvt_lo(kw[2 * e], sc), cvt_hi(kw[2 * e], sc), cvt_lo(kw[2 * e + 1], sc), cvt_hi(kw[2 * e + 1], sc)};
+            if (k_c == 0 && (k_tok & 15) == 0) s_ok[buf * 4 + k_tok / 16] = k_ok;
+        }
+        if (do_v) {
+            // places that nobody sees may hold anything: a weight of zero must stay a product of zero
+            if (!v_ok || t < range.lo || t + 64 > s.len) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int tok = t + 4 * v_quad + e;
+                    if (!(v_ok && tok >= range.lo && tok < s.len)) {
+                        vw[e] = 0u;
+                        vscale = (vscale & ~(0xFFu << (8 * e))) | (127u << (8 * e));
                     }
                 }
-                s *= a.scale * 0.69314718055994531f;
+            }
+            uint32_t lo[4], hi[4];                          // [token] channels 0, 1 and 2, 3
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float sc = scale_byte(vscale, e);
+                lo[e] = cvt_lo(vw[e], sc), hi[e] = cvt_hi(vw[e], sc);
+            }
+            const int chunk = 2 * (v_quad >> 2) + (v_quad & 1), half = (v_quad >> 1) & 1;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const uint32_t* w = c < 2 ? lo : hi;
+                const u32x2 q = c & 1 ? u32x2{high_halves(w[0], w[1]), high_halves(w[2], w[3])} : u32x2{low_halves(w[0], w[1]), low_halves(w[2], w[3])};
+                const int ch = 4 * v_c + c;
+                *reinterpret_cast<u32x2*>(s_v + buf * kHalf + ch * 128 + v_place(ch, chunk) * 16 + half * 8) = q;
             }
         }
-        float mx = s;
-        for (int d = 32; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-        if (mx == -INFINITY) continue;
-        const float m2 = fmaxf(m, mx), f = expf(m - m2), p = expf(s - m2);
-        float sum = p;
-        for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-        l = l * f + sum;
-        m = m2;
-        for (int i = 0; i < D / 64; ++i) o[i] *= f;
-        for (int j = 0; j < 64; ++j) {
-            const float pj = __shfl(p, j);
-            const int u = t + j;
-            if (pj == 0.0f) continue;                       // (places that take no part may hold anything)
-            const int page = a.page_table[(size_t)b * a.table_width + (u >> a.page_shift)];
-            const int64_t ph = (int64_t)page * a.kv_heads + kvh;
-            for (int i = 0; i < D / 64; ++i) {
-                const int c = i * 64 + lane;
-                const uint32_t w = a.v_codes[((ph << a.page_shift) + (u & page_mask)) * D + c];
-                const float sc = scale_operand(a.v_scales[((ph * (D / 32) + c / 32) << a.page_shift) + (u & page_mask)]);
-                o[i] += pj * __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, sc, false)[0];
-            }
-        }
+    };
+
+    float m = -INFINITY, l = 0.0f;
+    v16f o[kCb];
+#pragma unroll
+    for (int c = 0; c < kCb; ++c) o[c] = v16f{};
+
+    int kp = 0, vp = 0;
+    if (t_begin < t_end) {
+        request(t_begin, entry(t_begin + k_tok), entry(t_begin + 4 * v_quad));
+        kp = entry(t_begin + 64 + k_tok), vp = entry(t_begin + 64 + 4 * v_quad);
+        stage(t_begin, 0);
     }
-    for (int i = 0; i < D / 64; ++i)
-        a.out[(size_t)row * a.ldo + (size_t)head * D + i * 64 + lane] = (uint16_t)float_to_bf16_bits(l > 0.0f ? o[i] / l : 0.0f);
-    if (a.lse && lane == 0) a.lse[(size_t)row * a.q_heads + head] = l > 0.0f ? m + logf(l) : -INFINITY;
+    __syncthreads();
+    int buf = 0;
+    for (int t = t_begin; t < t_end; t += 64, buf ^= 1) {
+        const bool more = t + 64 < t_end;
+        if (more) {
+            request(t + 64, kp, vp);
+            kp = entry(t + 128 + k_tok), vp = entry(t + 128 + 4 * v_quad);
+        }
+        if (t < some_hi && t + 64 > some_lo) {              // wave-uniform
+            v16f sc[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                sc[x] = v16f{};
+                const uint8_t* row_k = s_k + buf * kHalf + (32 * x + n) * (D * 2);
+#pragma unroll
+                for (int u = 0; u < kU; ++u) {
+                    const bf16x8 kf = *reinterpret_cast<const bf16x8*>(row_k + k_place<D>(32 * x + n, 2 * u + hh) * 16);
+                    sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[u], sc[x], 0, 0, 0);
+                }
+            }
+            const uint32_t ok = *reinterpret_cast<const uint32_t*>(s_ok + buf * 4);
+            if (t < all_lo || t + 64 > all_hi || ok != 0x01010101u) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int at = 32 * x + 8 * (e >> 2) + 4 * hh + (e & 3), tok = t + at;
+                        const bool there = (ok >> (8 * (2 * x + (e >> 3)))) & 1u;
+                        if (!(there && tok >= row_lo && tok < row_hi)) sc[x][e] = -INFINITY;
+                    }
+            }
+            float mx = sc[0][0];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) mx = __builtin_fmaxf(mx, sc[x][e]);
+            mx = __builtin_fmaxf(mx, shuffle_xor(mx, 32)) * a.scale;
+            if (__ballot(mx > m + 8.0f)) {
+                const float m2 = __builtin_fmaxf(m, mx);
+                const float f = m2 == -INFINITY ? 0.0f : exp2_(m - m2);
+                l *= f;
+#pragma unroll
+                for (int c = 0; c < kCb; ++c) o[c] *= f;
+                m = m2;
+            }
+            const float ref = m == -INFINITY ? 0.0f : m;
+            bf16x8 pf[4];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float p = exp2_(__builtin_fmaf(sc[x][e], a.scale, -ref));
+                    l += p;
+                    pf[2 * x + (e >> 3)][e & 7] = (__bf16)p;
+                }
+#pragma unroll
+            for (int c = 0; c < kCb; ++c) {
+                const uint8_t* row_v = s_v + buf * kHalf + (32 * c + n) * 128;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bf16x8 vf = *reinterpret_cast<const bf16x8*>(row_v + v_place(32 * c + n, 2 * j + hh) * 16);
+                    o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[j], o[c], 0, 0, 0);
+                }
+            }
+        }
+        if (more) stage(t + 64, buf ^ 1);
+        __syncthreads();
+    }
+    if (!live || i >= s.n) return;
+    l += shuffle_xor(l, 32);
+    // element e of o[c] is channel 32c + 8 (e / 4) + 4h + e % 4
+    if (parts == 1) {
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        uint16_t* p = a.out + row * a.ldo + (size_t)head * D + 4 * hh;
+#pragma unroll
+        for (int c = 0; c < kCb; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+                *reinterpret_cast<bf16x4*>(p + 32 * c + 8 * e) =
+                    bf16x4{(__bf16)(o[c][4 * e] * inv), (__bf16)(o[c][4 * e + 1] * inv), (__bf16)(o[c][4 * e + 2] * inv), (__bf16)(o[c][4 * e + 3] * inv)};
+            }
+        if (a.lse && hh == 0) a.lse[row * a.q_heads + head] = l > 0.0f ? (m + __log2f(l)) * 0.69314718055994531f : -INFINITY;
+    } else {
+        const size_t at = (row * a.q_heads + head) * a.many_parts + part;
+        float* p = a.many_o + at * D + 4 * hh;
+#pragma unroll
+        for (int c = 0; c < kCb; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) *reinterpret_cast<f32x4*>(p + 32 * c + 8 * e) = f32x4{o[c][4 * e], o[c][4 * e + 1], o[c][4 * e + 2], o[c][4 * e + 3]};
+        if (hh == 0) a.many_ml[2 * at] = m, a.many_ml[2 * at + 1] = l;
+    }
+}
+
+// One wave per (row of q, query head) of sequences with many rows.
+template <int D>
+__global__ void __launch_bounds__(256)
+join_many(const AttnArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row = (int)(unit / a.q_heads), head = (int)(unit % a.q_heads);
+    if (row >= a.total_q) return;
+    int b = -1;                                             // the row's sequence: lanes look at 64 of them at a time
+    for (int b0 = 0; b0 < a.batch && b < 0; b0 += 64) {
+        bool mine = false;
+        if (b0 + lane < a.batch) {
+            const int begin = a.cu_q[b0 + lane], end = a.cu_q[b0 + lane + 1];
+            mine = begin >= 0 && end <= a.total_q && row >= begin && row < end;
+        }
+        const uint64_t found = __ballot(mine);
+        if (found) b = b0 + __builtin_ctzll(found);
+    }
+    if (b < 0) return;
+    const Seq s = sequence(a, b);
+    const int rows = s.n * a.group, i = row - s.begin;
+    if (i >= s.n || rows <= a.few_rows) return;
+    const TokenRange t = tile_tokens(a, s, (i * a.group + head % a.group) / kManyRows);
+    const int parts = range_parts(t, a.many_len);
+    if (parts == 1) return;
+    join_row<D>(a, a.many_o, a.many_ml, ((size_t)row * a.q_heads + head) * a.many_parts, parts, (size_t)row, head);
 }
 
 }  // namespace
@@ -450,17 +707,19 @@ namespace {
 
 struct Plan {
     int few_rows, few_len, max_parts, part_rows;
-    bool few, rows;                                         // which kernels run
+    int many_tiles, many_len, many_parts;
+    bool few, many;                                         // which kernels run
 };
 
-// Part length: enough workgroups for two to a compute unit (four where a sequence is long), at least 256 tokens (a
-// block for each wave) and at most 1024, so that the longest of ragged sequences does not outlast the others.
-Plan plan(int group, int kv_heads, int batch, int max_q, int max_kv, int compute_units) {
+// Part length of attend_few: enough workgroups for two to a compute unit (four where a sequence is long), at least 256
+// tokens (a block for each wave) and at most 1024, so that the longest of ragged sequences does not outlast the others.
+// attend_many cuts the tokens only where its row tiles are fewer than the compute units.
+Plan plan(int group, int kv_heads, int batch, int total_q, int max_q, int max_kv, int compute_units) {
     Plan p = {};
     const int64_t rows = (int64_t)max_q * group;
-    p.rows = rows > 32;
-    p.few = !p.rows || batch > 1;
-    p.few_rows = !p.few ? 0 : p.rows ? 16 : rows > 16 ? 32 : 16;
+    p.many = rows > 32;
+    p.few = !p.many || batch > 1;
+    p.few_rows = !p.few ? 0 : p.many ? 16 : rows > 16 ? 32 : 16;
     p.part_rows = (int)(rows < p.few_rows ? rows : p.few_rows);
     const int64_t tokens = (int64_t)batch * kv_heads * max_kv;
     int64_t len = (tokens / (4 * compute_units) + 255) & ~int64_t(255);
@@ -469,36 +728,57 @@ Plan plan(int group, int kv_heads, int batch, int max_q, int max_kv, int compute
     p.few_len = (int)len;
     p.max_parts = p.few ? (int)((max_kv + 63 + len - 1) / len) : 1;
     if (p.max_parts < 1) p.max_parts = 1;
+    p.many_parts = 1, p.many_len = 1 << 30;
+    if (p.many) {
+        p.many_tiles = (int)((int64_t)total_q * group / kManyRows + batch);
+        const int64_t groups = (int64_t)((int64_t)total_q * group / kManyRows + 1) * kv_heads;
+        if (groups < compute_units) {
+            int64_t n = 2 * compute_units / groups;
+            const int64_t most = (max_kv + 511) / 512;      // at least 512 tokens to a part
+            if (n > most) n = most;
+            if (n > 1) {
+                p.many_len = (int)(((max_kv + n - 1) / n + 63) & ~int64_t(63));
+                p.many_parts = (max_kv + 63 + p.many_len - 1) / p.many_len;
+            }
+        }
+    }
     return p;
 }
 
-int64_t part_units(const Plan& p, int batch, int kv_heads) { return p.max_parts > 1 ? (int64_t)batch * kv_heads * p.part_rows : 0; }
+// Partial results: rows x parts of attend_few, then of attend_many.
+int64_t few_units(const Plan& p, int batch, int kv_heads) { return p.max_parts > 1 ? (int64_t)batch * kv_heads * p.part_rows * p.max_parts : 0; }
+int64_t many_units(const Plan& p, int total_q, int q_heads) { return p.many_parts > 1 ? (int64_t)total_q * q_heads * p.many_parts : 0; }
 
 template <int D>
-hipError_t launch_attention(const AttnArgs& a, const Plan& p, hipStream_t stream) {
+hipError_t launch_attention(const AttnArgs& a, const Plan& p, int dev, hipStream_t stream) {
+    if (p.many) {
+        if (hipError_t e = ensure_dynamic_lds<&attend_many<D>>(dev, many_lds<D>()); e != hipSuccess) return e;
+        attend_many<D><<<(unsigned)p.many_tiles * p.many_parts * a.kv_heads, 512, many_lds<D>(), stream>>>(a);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
     if (p.few) {
         const unsigned units = (unsigned)a.batch * a.kv_heads * p.max_parts;
         if (p.few_rows == 16) attend_few<D, 1><<<units, 256, 0, stream>>>(a);
         else attend_few<D, 2><<<units, 256, 0, stream>>>(a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    if (p.rows) {
-        attend_rows<D><<<dim3(a.total_q, a.q_heads), 64, 0, stream>>>(a);
+    if (p.max_parts > 1) {
+        join_few<D><<<((unsigned)a.batch * a.kv_heads * p.part_rows + 3) / 4, 256, 0, stream>>>(a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    if (const int64_t units = part_units(p, a.batch, a.kv_heads)) {
-        join_parts<D><<<(unsigned)((units + 3) / 4), 256, 0, stream>>>(a);
-        return hipGetLastError();
+    if (p.many_parts > 1) {
+        join_many<D><<<((unsigned)a.total_q * a.q_heads + 3) / 4, 256, 0, stream>>>(a);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
 }  // namespace
 
-size_t paged_attention_workspace_bytes(const batq_paged_cache& c, int q_heads, int batch, int, int max_q, int max_kv,
+size_t paged_attention_workspace_bytes(const batq_paged_cache& c, int q_heads, int batch, int total_q, int max_q, int max_kv,
                                        int compute_units) {
-    const Plan p = plan(q_heads / c.kv_heads, c.kv_heads, batch, max_q, max_kv, compute_units);
-    return (size_t)part_units(p, batch, c.kv_heads) * p.max_parts * (c.head_dim + 2) * 4;
+    const Plan p = plan(q_heads / c.kv_heads, c.kv_heads, batch, total_q, max_q, max_kv, compute_units);
+    return (size_t)(few_units(p, batch, c.kv_heads) + many_units(p, total_q, q_heads)) * (c.head_dim + 2) * 4;
 }
 
 hipError_t launch_paged_attention(const batq_paged_cache& c, const batq_paged_batch& b, const void* q, int64_t ldq,
@@ -508,7 +788,7 @@ hipError_t launch_paged_attention(const batq_paged_cache& c, const batq_paged_ba
     hipError_t e = hipGetDevice(&dev);
     const int cus = e == hipSuccess ? device_compute_units(dev, &e) : 0;
     if (e != hipSuccess) return e;
-    const Plan p = plan(q_heads / c.kv_heads, c.kv_heads, b.batch, b.max_q, b.max_kv, cus);
+    const Plan p = plan(q_heads / c.kv_heads, c.kv_heads, b.batch, b.total_q, b.max_q, b.max_kv, cus);
     AttnArgs a = {};
     a.q = static_cast<const uint16_t*>(q), a.ldq = ldq, a.ldo = ldo, a.out = static_cast<uint16_t*>(out), a.lse = lse;
     a.k_codes = c.k_codes, a.k_scales = c.k_scales, a.v_codes = c.v_codes, a.v_scales = c.v_scales;
@@ -518,9 +798,13 @@ hipError_t launch_paged_attention(const batq_paged_cache& c, const batq_paged_ba
     a.q_heads = q_heads, a.kv_heads = c.kv_heads, a.group = q_heads / c.kv_heads;
     a.causal = causal, a.window = window, a.scale = scale * 1.4426950408889634f;
     a.few_rows = p.few_rows, a.few_len = p.few_len, a.max_parts = p.max_parts, a.part_rows = p.part_rows;
+    a.many_len = p.many_len, a.many_parts = p.many_parts;
+    const size_t few = (size_t)few_units(p, b.batch, c.kv_heads), many = (size_t)many_units(p, b.total_q, q_heads);
     a.part_o = static_cast<float*>(workspace);
-    a.part_ml = a.part_o ? a.part_o + (size_t)part_units(p, b.batch, c.kv_heads) * p.max_parts * c.head_dim : nullptr;
-    return c.head_dim == 64 ? launch_attention<64>(a, p, stream) : launch_attention<128>(a, p, stream);
+    a.part_ml = a.part_o + few * c.head_dim;
+    a.many_o = a.part_ml + few * 2;
+    a.many_ml = a.many_o + many * c.head_dim;
+    return c.head_dim == 64 ? launch_attention<64>(a, p, dev, stream) : launch_attention<128>(a, p, dev, stream);
 }
 
 }  // namespace batq
