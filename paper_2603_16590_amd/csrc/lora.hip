@@ -14,6 +14,8 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+constexpr int kMaxParts = 8;                                // of K
+
 struct LoraArgs {
     const void* X;
     const uint16_t *A, *B;
@@ -26,7 +28,7 @@ struct LoraArgs {
     int M, K, N, rank, adapters;
     int slots;                                              // workgroups that share a tile's adapters
     int parts, part_k;                                      // parts of K and their length (a multiple of 256)
-    int blocks_n;                                           // columns of a workgroup of expand_kernel, in blocks of 256
+    int tile_rows, groups_n;                                // row tiles of a workgroup of expand_kernel, workgroups beside each other
     int vec;                                                // base and out rows allow 16-byte accesses
 };
 
@@ -36,117 +38,136 @@ __device__ __forceinline__ int adapter_of(const LoraArgs& a, int m) {
     return i >= 0 && i < a.adapters ? i : -1;
 }
 
-// Calls f(adapter) for each `slot`-th, (slot + slots)-th, ... distinct value of the tile's rows [row0, row0 + count), in
-// the order of first appearance; count <= 64.  Wave-uniform.
+// Calls f(adapter) for each `slot`-th, (slot + slots)-th, ... distinct adapter of a tile of 16 rows, in the order of first
+// appearance; lane l holds the adapter of row l % 16 (-1: none, -2: no such row).  Wave-uniform.
 template <typename F>
-__device__ __forceinline__ void for_adapters(const LoraArgs& a, int row0, int count, int slot, F f) {
-    const int lane = threadIdx.x & 63;
-    const int mine = lane < count ? adapter_of(a, row0 + lane) : -2;
-    uint64_t left = __ballot(lane < count);
+__device__ __forceinline__ void for_adapters(const LoraArgs& a, int mine, int slot, F f) {
+    uint64_t left = __ballot(mine != -2) & 0xFFFFu;
     for (int n = 0; left; ++n) {
         const int id = __builtin_amdgcn_readlane(mine, __builtin_ctzll(left));
         left &= ~__ballot(mine == id);
-        if (n % a.slots == slot) f(id);
+        if (n == slot || (n > slot && (n - slot) % a.slots == 0)) f(id);
     }
 }
 
-// Sixteen consecutive elements as bf16 operands (k-slots 0..7 and 8..15), in `Terms` terms whose sum is the element.
+// Eight consecutive elements as bf16 operands in `Terms` terms whose sum is the element.
 template <int Terms>
-__device__ __forceinline__ void load16(const uint16_t* p, bf16x8 (&x)[Terms][2]) {
-    x[0][0] = reinterpret_cast<const bf16x8*>(p)[0], x[0][1] = reinterpret_cast<const bf16x8*>(p)[1];
+__device__ __forceinline__ void terms8(const uint16_t*, const f32x4* w, bf16x8 (&x)[Terms]) {
+    x[0] = __builtin_bit_cast(bf16x8, w[0]);
 }
 template <int Terms>
-__device__ __forceinline__ void load16(const float* p, bf16x8 (&x)[Terms][2]) {
+__device__ __forceinline__ void terms8(const float*, const f32x4* w, bf16x8 (&x)[Terms]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const f32x4 v = reinterpret_cast<const f32x4*>(p)[i];
+    for (int e = 0; e < 8; ++e) {
+        float r = w[e >> 2][e & 3];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float r = v[e];
-#pragma unroll
-            for (int t = 0; t < Terms; ++t) {
-                const __bf16 b = (__bf16)r;
-                x[t][i >> 1][4 * (i & 1) + e] = b;
-                r -= (float)b;
-            }
+        for (int t = 0; t < Terms; ++t) {
+            x[t][e] = (__bf16)r;
+            r -= (float)x[t][e];
         }
     }
 }
 
-// h[m][j] = sum over a part of K of X[m][k] A_a[j][k].  A workgroup takes (row tile of 16 RG rows, adapters of a slot, part
-// of K); its four waves split the part and are added through LDS in wave order.  Lane (i, g) = (l % 16, l / 16) loads
-// k = 16g .. 16g + 15 of every 64 for its row of A (i: rank index) and of X: whole 128-byte lines over two instructions.
-template <typename XT, int RG, int JT>
-__global__ void __launch_bounds__(256)
+// A wave's piece of a matrix in LDS: Rows rows of 64 elements, requested with 16-byte loads whose neighbouring lanes take
+// neighbouring 16 bytes of a row (operands loaded straight into registers would have every lane in another row: with
+// rows 8 KiB apart, four times slower), the 16-byte chunks of a row XORed with the row's number so that 16 lanes
+// that read a chunk of 16 rows reach all banks.
+template <typename T, int Rows>
+struct Piece {
+    static constexpr int kChunks = 4 * (int)sizeof(T);      // of a row
+    static constexpr int kRowsAtOnce = 64 / kChunks, kLoads = Rows / kRowsAtOnce, kBytes = Rows * kChunks * 16;
+    f32x4 w[kLoads];
+    __device__ static int place(int row, int chunk) { return row * kChunks + (kChunks == 16 ? chunk ^ (row & 15) : chunk ^ ((row >> 1) & 7)); }
+    // element 64 of row r at rows(r) + k; lanes whose chunk lies behind `left` elements get zeros
+    template <typename F>
+    __device__ __forceinline__ void request(F rows, int k, int left) {
+        const int lane = threadIdx.x & 63, c = lane % kChunks, e = c * (16 / (int)sizeof(T));
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const T* p = rows(i * kRowsAtOnce + lane / kChunks) + k;
+            w[i] = e < left ? *reinterpret_cast<const f32x4*>(p + e) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+    }
+    __device__ __forceinline__ void store(f32x4* lds) const {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) lds[place(i * kRowsAtOnce + lane / kChunks, lane % kChunks)] = w[i];
+    }
+    // elements 8 c .. 8 c + 7 of a row
+    template <int Terms>
+    __device__ static void operand(const f32x4* lds, int row, int c, bf16x8 (&x)[Terms]) {
+        f32x4 v[kChunks / 8];
+#pragma unroll
+        for (int i = 0; i < kChunks / 8; ++i) v[i] = lds[place(row, c * (kChunks / 8) + i)];
+        terms8<Terms>(static_cast<const T*>(nullptr), v, x);
+    }
+};
+
+template <typename XT, int JT, int W>
+constexpr int shrink_lds() { return W * (Piece<XT, 16>::kBytes + Piece<uint16_t, 16 * JT>::kBytes); }   // (the sums need less)
+
+// h[m][j] = sum over a part of K of X[m][k] A_a[j][k].  A workgroup takes (16 rows, adapters of a slot, part of K); its W
+// waves split the part into W ranges and are added through LDS in wave order.  A wave works on 64 k at a time, out of
+// its own pieces of LDS, while the next 64 are on their way to registers.  Bound: the stream of X (many rows), the latency
+// of index, loads and sums in a row (few).
+template <typename XT, int JT, int W>
+__global__ void __launch_bounds__(64 * W)
 shrink_kernel(const LoraArgs a) {
     constexpr int kTerms = sizeof(XT) == 4 ? 3 : 1;
-    __shared__ f32x4 s_acc[3][RG * JT][64];
+    using PX = Piece<XT, 16>;
+    using PA = Piece<uint16_t, 16 * JT>;
+    extern __shared__ __align__(16) uint8_t s_raw[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane & 15, g = lane >> 4;
-    const int slot = blockIdx.x % a.slots, tile = blockIdx.x / a.slots, part = blockIdx.y;
-    const int row0 = tile * 16 * RG, count = min(16 * RG, a.M - row0);
-    const int k0 = part * a.part_k, k1 = min(a.K, k0 + a.part_k);
-    for_adapters(a, row0, count, slot, [&](int id) {
+    const int part = blockIdx.x % a.parts, ts = blockIdx.x / a.parts, slot = ts % a.slots, row0 = ts / a.slots * 16;
+    const int share = a.part_k / W, k0 = part * a.part_k + wave * share, k1 = min(a.K, k0 + share);
+    f32x4* const s_x = reinterpret_cast<f32x4*>(s_raw + wave * (PX::kBytes + PA::kBytes));
+    f32x4* const s_a = s_x + PX::kBytes / 16;
+    f32x4* const s_acc = reinterpret_cast<f32x4*>(s_raw);   // [W - 1][JT][64], when the pieces are used up
+    auto x_row = [&](int r) { return static_cast<const XT*>(a.X) + (size_t)min(row0 + r, a.M - 1) * a.ldx; };
+    const int mine = row0 + i < a.M ? adapter_of(a, row0 + i) : -2;
+    for_adapters(a, mine, slot, [&](int id) {
         if (id < 0) return;
-        const uint16_t* ap[JT];
+        auto a_row = [&](int j) { return a.A + ((size_t)id * a.rank + min(j, a.rank - 1)) * a.K; };
+        f32x4 acc[JT];
 #pragma unroll
-        for (int j = 0; j < JT; ++j) ap[j] = a.A + ((size_t)id * a.rank + min(16 * j + i, a.rank - 1)) * a.K + 16 * g;
-        const XT* xp[RG];
+        for (int j = 0; j < JT; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        PX px;
+        PA pa;
+        if (k0 < k1) px.request(x_row, k0, k1 - k0), pa.request(a_row, k0, k1 - k0);
+        for (int k = k0; k < k1; k += 64) {
+            // (a wave's LDS operations are carried out in order: the last step's reads come before these writes)
+            px.store(s_x);
+            pa.store(s_a);
+            if (k + 64 < k1) px.request(x_row, k + 64, k1 - k - 64), pa.request(a_row, k + 64, k1 - k - 64);
 #pragma unroll
-        for (int r = 0; r < RG; ++r) xp[r] = static_cast<const XT*>(a.X) + (size_t)min(row0 + 16 * r + i, a.M - 1) * a.ldx + 16 * g;
-        f32x4 acc[RG][JT];
+            for (int e = 0; e < 2; ++e) {
+                bf16x8 x[kTerms];
+                PX::template operand<kTerms>(s_x, i, 4 * e + g, x);
 #pragma unroll
-        for (int r = 0; r < RG; ++r)
+                for (int j = 0; j < JT; ++j) {
+                    bf16x8 aw[1];
+                    PA::template operand<1>(s_a, 16 * j + i, 4 * e + g, aw);
 #pragma unroll
-            for (int j = 0; j < JT; ++j) acc[r][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        auto step = [&](int k, bool inside) {               // K is a multiple of 32: the last 64 may be half there
-            bf16x8 aw[JT][1][2];
-#pragma unroll
-            for (int j = 0; j < JT; ++j) {
-                load16<1>(ap[j] + (inside ? k : 0), aw[j]);
-                if (!inside) aw[j][0][0] = bf16x8{}, aw[j][0][1] = bf16x8{};
+                    for (int t = kTerms - 1; t >= 0; --t) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aw[0], x[t], acc[j], 0, 0, 0);
+                }
             }
-#pragma unroll
-            for (int r = 0; r < RG; ++r) {
-                bf16x8 x[kTerms][2];
-                load16<kTerms>(xp[r] + (inside ? k : 0), x);
-                if (!inside)
-#pragma unroll
-                    for (int t = 0; t < kTerms; ++t) x[t][0] = bf16x8{}, x[t][1] = bf16x8{};
-#pragma unroll
-                for (int j = 0; j < JT; ++j)
-#pragma unroll
-                    for (int t = kTerms - 1; t >= 0; --t)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aw[j][0][e], x[t][e], acc[r][j], 0, 0, 0);
-            }
-        };
-        // (a lane whose 16 elements lie behind K reads the row's first ones instead and multiplies zeros)
-        for (int k = k0 + 64 * wave; k < k1; k += 256) {
-            if (k + 64 <= k1) step(k, true);
-            else step(k, k + 16 * g < k1);
         }
-        __syncthreads();                                    // (the previous adapter's sums have been read)
+        __syncthreads();                                    // every wave is done with its pieces
         if (wave > 0)
 #pragma unroll
-            for (int r = 0; r < RG; ++r)
-#pragma unroll
-                for (int j = 0; j < JT; ++j) s_acc[wave - 1][r * JT + j][lane] = acc[r][j];
+            for (int j = 0; j < JT; ++j) s_acc[((wave - 1) * JT + j) * 64 + lane] = acc[j];
         __syncthreads();
-        if (wave > 0) return;
-#pragma unroll
-        for (int r = 0; r < RG; ++r) {
-            const int m = row0 + 16 * r + i;
-            const bool live = 16 * r + i < count && adapter_of(a, min(m, a.M - 1)) == id;
+        if (wave == 0)
 #pragma unroll
             for (int j = 0; j < JT; ++j) {
-                f32x4 v = acc[r][j];
+                f32x4 v = acc[j];
 #pragma unroll
-                for (int w = 0; w < 3; ++w) v += s_acc[w][r * JT + j][lane];
+                for (int w = 0; w < W - 1; ++w) v += s_acc[(w * JT + j) * 64 + lane];
                 const int at = 16 * j + 4 * g;              // the rank is a multiple of 8
-                if (live && at < a.rank) *reinterpret_cast<f32x4*>(a.h + ((size_t)part * a.M + m) * a.rank + at) = v;
+                if (mine == id && at < a.rank) *reinterpret_cast<f32x4*>(a.h + ((size_t)part * a.M + row0 + i) * a.rank + at) = v;
             }
-        }
+        __syncthreads();                                    // the sums have been read: the pieces may be written again
     });
 }
 
@@ -154,200 +175,223 @@ __device__ __forceinline__ float value(float x) { return x; }
 __device__ __forceinline__ float value(uint16_t x) { return bf16_bits_to_float(x); }
 __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put(uint16_t* p, float x) { *reinterpret_cast<__bf16*>(p) = (__bf16)x; }
-// Sixteen elements with 16-byte accesses.
-__device__ __forceinline__ void read16(const float* p, float (&v)[16]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const f32x4 x = reinterpret_cast<const f32x4*>(p)[i];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[4 * i + e] = x[e];
+// C neighbouring columns of a row (16 or 8 bytes) as they lie in memory.
+template <typename T, int C>
+struct Cols {
+    typedef uint32_t words __attribute__((ext_vector_type(C * (int)sizeof(T) / 4)));
+    words w;
+    __device__ __forceinline__ float at(int c) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[c]);
+        else return __uint_as_float(c & 1 ? w[c / 2] & 0xFFFF0000u : w[c / 2] << 16);
     }
-}
-__device__ __forceinline__ void read16(const uint16_t* p, float (&v)[16]) {
+    __device__ __forceinline__ void set(const float (&v)[C]) {
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const bf16x8 x = reinterpret_cast<const bf16x8*>(p)[i];
+            for (int c = 0; c < C; ++c) w[c] = __float_as_uint(v[c]);
+        } else {
+            typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[8 * i + e] = (float)x[e];
+            for (int c = 0; c < C; c += 2) w[c / 2] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)v[c], (__bf16)v[c + 1]});
+        }
     }
-}
-__device__ __forceinline__ void write16(float* p, const float (&v)[16]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) reinterpret_cast<f32x4*>(p)[i] = f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
-}
-__device__ __forceinline__ void write16(uint16_t* p, const float (&v)[16]) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        bf16x8 x;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (__bf16)v[8 * i + e];
-        reinterpret_cast<bf16x8*>(p)[i] = x;
-    }
-}
+};
 
-// Eight-element chunks of the contraction: the rank's chunks of h's first bf16 term, then of the second and the third
-// (their sum is h to 24 bits), padded to whole instructions of four chunks with zeros.
-__device__ __forceinline__ int chunk_steps(int rank) { return (3 * (rank / 8) + 3) / 4; }
-__host__ __device__ inline int h_pitch(int rank) { return ((3 * (rank / 8) + 3) / 4) * 64 + 16; }   // bytes of a row in LDS
-
-// out = base + s h B^T.  A workgroup takes (row tile of 16 RG rows, adapters of a slot, 256 blocks_n columns); a wave takes 64
-// columns at a time.  Lane (i, g) ends with columns 16g .. 16g + 15 of row i (the columns of the four instructions of a
-// step are numbered that way): 128 contiguous bytes of bf16 per row.
-template <typename YT, int RG>
-__global__ void __launch_bounds__(256)
+// out = base + s h B^T.  A wave takes 16 C columns and tile_rows tiles of 16 rows, one after the other, and keeps the
+// adapter's B for its columns in registers (G groups of 32 rank indexes) until a row wants another adapter.  Column t of the C
+// instructions of a tile is column C i + t in lane (i, g) = (l % 16, l / 16): a lane ends with C neighbouring columns of
+// rows 4g .. 4g + 3, 16 lanes with a contiguous piece of a row.  h is taken as three bf16 terms (24 bits).  The sums start
+// from base, which is requested a tile ahead.  Bound: base in, out out.
+template <typename YT, int G, int P>
+__global__ void __launch_bounds__(256, P > 1 ? (G == 4 ? 1 : 2) : G == 1 ? 4 : 2)
 expand_kernel(const LoraArgs a) {
-    extern __shared__ __align__(16) uint8_t s_h[];
+    constexpr int C = 4, kWide = 16 * C;                    // columns of a lane, of a wave
+    typedef Cols<YT, C> V;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int i = lane & 15, g = lane >> 4;
-    const int slot = blockIdx.x % a.slots, tile = blockIdx.x / a.slots;
-    const int row0 = tile * 16 * RG, count = min(16 * RG, a.M - row0);
-    const int n_begin = blockIdx.y * a.blocks_n * 256, n_end = (int)min((int64_t)a.N, (int64_t)n_begin + a.blocks_n * 256);
-    const int chunks = a.rank / 8, steps = chunk_steps(a.rank), pitch = h_pitch(a.rank);
-    for_adapters(a, row0, count, slot, [&](int id) {
-        if (id < 0 && a.base == a.out) return;              // nothing to add, nothing to copy
-        if (id >= 0) {
-            const float s = a.scales ? a.scales[id] : 1.0f;
-            __syncthreads();                                // (the previous adapter's h has been read)
-            for (int c = threadIdx.x; c < 16 * RG * chunks; c += 256) {
-                const int r = c / chunks, ch = c - r * chunks;
-                const bool live = r < count && adapter_of(a, row0 + r) == id;       // other rows of h may hold anything
-                float v[8] = {};
-                if (live)
-                    for (int p = 0; p < a.parts; ++p) {
-                        const float* hp = a.h + ((size_t)p * a.M + row0 + r) * a.rank + 8 * ch;
+    const int y = blockIdx.x % a.groups_n, ts = blockIdx.x / a.groups_n, slot = ts % a.slots, tile0 = ts / a.slots * a.tile_rows;
+    const int n0 = (y * 4 + wave) * kWide, n = n0 + C * i;
+    if (n0 >= a.N) return;
+    const bool whole = a.vec && n0 + kWide <= a.N;          // wave-uniform
+    const int chunks = a.rank / 8, tiles = (a.M + 15) / 16, tile1 = min(tiles, tile0 + a.tile_rows);
+    auto base_row = [&](int m) { return static_cast<const YT*>(a.base) + (size_t)min(m, a.M - 1) * a.ldb; };   // (past the end: the last row again)
+    auto request = [&](int tile, V (&v)[4]) {
+        if (a.base && whole)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] += hp[e];
+            for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const V*>(base_row(tile * 16 + 4 * g + e) + n);
+    };
+    auto adapters = [&](int tile) { return tile * 16 + i < a.M ? adapter_of(a, tile * 16 + i) : -2; };
+    bf16x8 bw[G][C];
+    float s = 0.0f;
+    int loaded = -1;
+    V next[4];
+    if (tile0 < tile1) request(tile0, next);
+    int mine_next = tile0 < tile1 ? adapters(tile0) : -2;
+    for (int tile = tile0; tile < tile1; ++tile) {
+        const int row0 = tile * 16, mine = mine_next;
+        V now[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) now[e] = next[e];
+        if (tile + 1 < tile1) {
+            request(tile + 1, next);
+            mine_next = adapters(tile + 1);
+        }
+        for_adapters(a, mine, slot, [&](int id) {
+            if (id < 0 && a.base == a.out) return;          // nothing to add, nothing to copy
+            f32x4 acc[C];                                   // [column][row]
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int t = 0; t < C; ++t) acc[t][e] = a.base && whole ? now[e].at(t) : 0.0f;
+            if (id >= 0) {
+                if (id != loaded) {
+                    loaded = id;
+                    s = a.scales ? a.scales[id] : 1.0f;
+#pragma unroll
+                    for (int q = 0; q < G; ++q)
+#pragma unroll
+                        for (int t = 0; t < C; ++t)
+                            bw[q][t] = *reinterpret_cast<const bf16x8*>(a.B + ((size_t)id * a.N + min(n + t, a.N - 1)) * a.rank + 8 * min(4 * q + g, chunks - 1));
+                }
+#pragma unroll
+                for (int q = 0; q < G; ++q) {
+                    float v[8] = {};
+                    if (mine == id && 4 * q + g < chunks) { // (other rows of h may hold anything)
+                        const float* hp = a.h + (size_t)(row0 + i) * a.rank + 8 * (4 * q + g);
+                        const size_t step = (size_t)a.M * a.rank;
+                        f32x4 h0[P], h1[P];                 // all parts in flight (past the last one: the last one again)
+#pragma unroll
+                        for (int p = 0; p < P; ++p) {
+                            const f32x4* from = reinterpret_cast<const f32x4*>(hp + (P > 1 ? min(p, a.parts - 1) : 0) * step);
+                            h0[p] = from[0], h1[p] = from[1];
+                        }
+#pragma unroll
+                        for (int p = 0; p < P; ++p)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                v[e] += P == 1 || p < a.parts ? h0[p][e] : 0.0f;
+                                v[4 + e] += P == 1 || p < a.parts ? h1[p][e] : 0.0f;
+                            }
                     }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= s;
-#pragma unroll
-                for (int t = 0; t < 3; ++t) {
-                    bf16x8 x;
+                    bf16x8 h[3];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        x[e] = (__bf16)v[e];
-                        v[e] -= (float)x[e];
+                        float r = v[e] * s;
+#pragma unroll
+                        for (int t = 0; t < 3; ++t) {
+                            h[t][e] = (__bf16)r;
+                            r -= (float)h[t][e];
+                        }
                     }
-                    *reinterpret_cast<bf16x8*>(s_h + r * pitch + (t * chunks + ch) * 16) = x;
+#pragma unroll
+                    for (int e = 2; e >= 0; --e)
+#pragma unroll
+                        for (int t = 0; t < C; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[e], bw[q][t], acc[t], 0, 0, 0);
                 }
             }
-            for (int c = threadIdx.x; c < 16 * RG * (4 * steps - 3 * chunks); c += 256) {
-                const int pad = 4 * steps - 3 * chunks, r = c / pad;
-                *reinterpret_cast<bf16x8*>(s_h + r * pitch + (3 * chunks + c - r * pad) * 16) = bf16x8{};
-            }
-            __syncthreads();
-        }
-        for (int n0 = n_begin + 64 * wave; n0 < n_end; n0 += 256) {
-            f32x4 acc[RG][4];
 #pragma unroll
-            for (int r = 0; r < RG; ++r)
+            for (int e = 0; e < 4; ++e) {
+                if (__shfl(mine, 4 * g + e) != id) continue;
+                YT* o = static_cast<YT*>(a.out) + (size_t)(row0 + 4 * g + e) * a.ldo + n;
+                float v[C];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) acc[r][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            if (id >= 0) {
-                const uint16_t* bp[4];                      // instruction t's row 4q + e is column 16q + 4t + e
-#pragma unroll
-                for (int t = 0; t < 4; ++t) bp[t] = a.B + ((size_t)id * a.N + min(n0 + 16 * (i >> 2) + 4 * t + (i & 3), a.N - 1)) * a.rank;
-                for (int st = steps - 1; st >= 0; --st) {   // smallest terms first
-                    const int rc = (4 * st + g) % chunks;
-                    bf16x8 bw[4];
-#pragma unroll
-                    for (int t = 0; t < 4; ++t) bw[t] = *reinterpret_cast<const bf16x8*>(bp[t] + 8 * rc);
-#pragma unroll
-                    for (int r = 0; r < RG; ++r) {
-                        const bf16x8 hw = *reinterpret_cast<const bf16x8*>(s_h + (16 * r + i) * pitch + (4 * st + g) * 16);
-#pragma unroll
-                        for (int t = 0; t < 4; ++t) acc[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[t], hw, acc[r][t], 0, 0, 0);
-                    }
-                }
-            }
-            const int n = n0 + 16 * g;
-#pragma unroll
-            for (int r = 0; r < RG; ++r) {
-                const int m = row0 + 16 * r + i;
-                if (16 * r + i >= count || adapter_of(a, m) != id || n >= a.N) continue;
-                const YT* b = a.base ? static_cast<const YT*>(a.base) + (size_t)m * a.ldb + n : nullptr;
-                YT* o = static_cast<YT*>(a.out) + (size_t)m * a.ldo + n;
-                float v[16];
-                if (a.vec && n + 16 <= a.N) {
-                    if (b) read16(b, v);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) v[e] = (b ? v[e] : 0.0f) + acc[r][e >> 2][e & 3];
-                    write16(o, v);
+                for (int t = 0; t < C; ++t) v[t] = acc[t][e];
+                if (whole) {
+                    V w;
+                    w.set(v);
+                    *reinterpret_cast<V*>(o) = w;
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (n + e < a.N) put(o + e, (b ? value(b[e]) : 0.0f) + acc[r][e >> 2][e & 3]);
+                    for (int t = 0; t < C; ++t)
+                        if (n + t < a.N) put(o + t, (a.base ? value(base_row(row0 + 4 * g + e)[n + t]) : 0.0f) + v[t]);
                 }
             }
-        }
-    });
+        });
+    }
 }
 
-// How a call is cut.  Row tiles: 16 rows where there are few (decoding: a tile's adapters are spread over workgroups), else
-// 64 (32 of large ranks, whose sums fill the registers).  Parts of K: two workgroups to a compute unit if the rows of a tile
-// share one or two adapters, at least 256 to a part.
+// How a call is cut.  Few rows (decoding): a tile's adapters are spread over workgroups, and K is cut into parts so that
+// there are about two workgroups to a compute unit if the rows of a tile share one or two adapters, at least 256 to a part.
+// Many rows: whole rows of X to a workgroup, so that h is written and read once.
 struct Plan {
-    int rg, tiles, slots, parts, part_k;
+    int tiles, slots, parts, part_k;
+    bool few;
 };
-Plan plan(int M, int K, int rank, int adapters) {
+Plan plan(int M, int K, int adapters) {
     Plan p;
-    p.rg = M <= 512 ? 1 : rank > 64 ? 2 : 4;
-    p.tiles = (int)(((int64_t)M + 16 * p.rg - 1) / (16 * p.rg));
-    p.slots = p.rg == 1 ? 16 : 4;
+    p.few = M <= 512;
+    p.tiles = (int)(((int64_t)M + 15) / 16);
+    p.slots = p.few ? 64 / p.tiles : 1;
+    if (p.slots > 16) p.slots = 16;
     if (p.slots > adapters + 1) p.slots = adapters + 1;     // (rows without an adapter count as one)
-    int n = 512 / (p.rg == 1 ? 2 * p.tiles : p.tiles);
+    if (p.slots < 1) p.slots = 1;
+    int n = p.few ? 256 / p.tiles : 1;
     if (n > (K + 255) / 256) n = (K + 255) / 256;
-    if (n > 16) n = 16;
-    if (n < 1) n = 1;
-    p.part_k = ((K + n - 1) / n + 255) & ~255;
+    if (n > kMaxParts) n = kMaxParts;
+    p.part_k = (int)((((int64_t)K + n - 1) / n + 511) & ~int64_t(511));     // whole steps of 64 for each of 8 waves
+    if (n > 1) p.part_k = ((K + n - 1) / n + 255) & ~255;
     p.parts = (K + p.part_k - 1) / p.part_k;
     return p;
 }
 
+template <typename XT, int JT, int W>
+hipError_t launch_shrink(const LoraArgs& a, unsigned grid, int dev, hipStream_t stream) {
+    constexpr int lds = shrink_lds<XT, JT, W>();
+    if constexpr (lds > 65536)
+        if (hipError_t e = ensure_dynamic_lds<&shrink_kernel<XT, JT, W>>(dev, lds); e != hipSuccess) return e;
+    shrink_kernel<XT, JT, W><<<grid, 64 * W, lds, stream>>>(a);
+    return hipGetLastError();
+}
 template <typename XT>
-void shrink(const LoraArgs& a, int rg, dim3 grid, hipStream_t stream) {
-    if (a.rank > 64) rg == 1 ? shrink_kernel<XT, 1, 8><<<grid, 256, 0, stream>>>(a) : shrink_kernel<XT, 2, 8><<<grid, 256, 0, stream>>>(a);
-    else if (a.rank > 32) rg == 1 ? shrink_kernel<XT, 1, 4><<<grid, 256, 0, stream>>>(a) : shrink_kernel<XT, 4, 4><<<grid, 256, 0, stream>>>(a);
-    else if (a.rank > 16) rg == 1 ? shrink_kernel<XT, 1, 2><<<grid, 256, 0, stream>>>(a) : shrink_kernel<XT, 4, 2><<<grid, 256, 0, stream>>>(a);
-    else rg == 1 ? shrink_kernel<XT, 1, 1><<<grid, 256, 0, stream>>>(a) : shrink_kernel<XT, 4, 1><<<grid, 256, 0, stream>>>(a);
+hipError_t shrink(const LoraArgs& a, bool few, unsigned grid, int dev, hipStream_t stream) {
+    if (a.rank > 64) return launch_shrink<XT, 8, 4>(a, grid, dev, stream);
+    if (a.rank > 32) return few ? launch_shrink<XT, 4, 4>(a, grid, dev, stream) : launch_shrink<XT, 4, 8>(a, grid, dev, stream);
+    if (a.rank > 16) return few ? launch_shrink<XT, 2, 4>(a, grid, dev, stream) : launch_shrink<XT, 2, 8>(a, grid, dev, stream);
+    return few ? launch_shrink<XT, 1, 4>(a, grid, dev, stream) : launch_shrink<XT, 1, 8>(a, grid, dev, stream);
 }
 
+template <typename YT, int G>
+hipError_t launch_expand(LoraArgs& a, const Plan& p, hipStream_t stream) {
+    // tiles of a workgroup: as many as leave eight workgroups to a compute unit; workgroups are numbered with 32 bits
+    a.groups_n = (int)(((int64_t)a.N + 255) / 256);
+    const int64_t units = (int64_t)p.tiles * p.slots * a.groups_n;
+    int64_t t = p.few ? 1 : (int64_t)p.tiles * a.groups_n / 2048;
+    if (t > 32) t = 32;
+    if (t < units / (1 << 30) + 1) t = units / (1 << 30) + 1;
+    a.tile_rows = (int)t;
+    const unsigned grid = (unsigned)((p.tiles + t - 1) / t * p.slots * a.groups_n);
+    if (p.parts > 1) expand_kernel<YT, G, kMaxParts><<<grid, 256, 0, stream>>>(a);
+    else expand_kernel<YT, G, 1><<<grid, 256, 0, stream>>>(a);
+    return hipGetLastError();
+}
 template <typename YT>
-void expand(const LoraArgs& a, int rg, dim3 grid, hipStream_t stream) {
-    if (rg == 1) expand_kernel<YT, 1><<<grid, 256, 16 * h_pitch(a.rank), stream>>>(a);
-    else if (rg == 2) expand_kernel<YT, 2><<<grid, 256, 32 * h_pitch(a.rank), stream>>>(a);
-    else expand_kernel<YT, 4><<<grid, 256, 64 * h_pitch(a.rank), stream>>>(a);
+hipError_t expand(LoraArgs& a, const Plan& p, hipStream_t stream) {
+    if (a.rank <= 32) return launch_expand<YT, 1>(a, p, stream);
+    if (a.rank <= 64) return launch_expand<YT, 2>(a, p, stream);
+    return launch_expand<YT, 4>(a, p, stream);
 }
 
 }  // namespace
 
 size_t lora_workspace_bytes(int M, int K, int, int rank, int adapters) {
-    return M > 0 ? (size_t)plan(M, K, rank, adapters).parts * M * rank * 4 : 0;
+    return M > 0 ? (size_t)plan(M, K, adapters).parts * M * rank * 4 : 0;
 }
 
 hipError_t launch_lora_add(const void* X, batq_dtype xdtype, int M, int K, int64_t ldx, const void* A, const void* B,
                            int N, int rank, int adapters, const float* scales, const int32_t* index, const void* base,
                            int64_t ldb, void* out, int64_t ldo, batq_dtype ydtype, void* workspace, hipStream_t stream) {
-    const Plan p = plan(M, K, rank, adapters);
+    int dev = 0;
+    if (hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
+    const Plan p = plan(M, K, adapters);
     LoraArgs a = {};
     a.X = X, a.A = static_cast<const uint16_t*>(A), a.B = static_cast<const uint16_t*>(B), a.scales = scales, a.index = index;
     a.base = base, a.out = out, a.h = static_cast<float*>(workspace), a.ldx = ldx, a.ldb = ldb, a.ldo = ldo;
     a.M = M, a.K = K, a.N = N, a.rank = rank, a.adapters = adapters, a.slots = p.slots, a.parts = p.parts, a.part_k = p.part_k;
     const int64_t size = ydtype == BATQ_BF16 ? 2 : 4;
     a.vec = ((uintptr_t)out | (uintptr_t)base | (uintptr_t)(ldo * size) | (uintptr_t)(base ? ldb * size : 0)) % 16 == 0;
-    const dim3 grid((unsigned)p.tiles * p.slots, p.parts);
-    if (xdtype == BATQ_BF16) shrink<uint16_t>(a, p.rg, grid, stream);
-    else shrink<float>(a, p.rg, grid, stream);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    // columns of a workgroup: h is read again for each of them, so as many as leave four workgroups to a compute unit
-    const int blocks = (int)(((int64_t)N + 255) / 256);
-    a.blocks_n = p.rg == 1 ? 1 : (int)(((int64_t)p.tiles * blocks + 1023) / 1024);
-    if (a.blocks_n > blocks) a.blocks_n = blocks;
-    if (a.blocks_n < (blocks + 65534) / 65535) a.blocks_n = (blocks + 65534) / 65535;      // grid.y
-    const dim3 wide((unsigned)p.tiles * p.slots, (blocks + a.blocks_n - 1) / a.blocks_n);
-    if (ydtype == BATQ_BF16) expand<uint16_t>(a, p.rg, wide, stream);
-    else expand<float>(a, p.rg, wide, stream);
-    return hipGetLastError();
+    const unsigned grid = (unsigned)p.tiles * p.slots * p.parts;
+    if (hipError_t e = xdtype == BATQ_BF16 ? shrink<uint16_t>(a, p.few, grid, dev, stream) : shrink<float>(a, p.few, grid, dev, stream); e != hipSuccess)
+        return e;
+    return ydtype == BATQ_BF16 ? expand<uint16_t>(a, p, stream) : expand<float>(a, p, stream);
 }
 
 }  // namespace batq
