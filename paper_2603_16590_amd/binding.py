@@ -639,25 +639,45 @@ class _PagedBatch(C.Structure):
                 ("max_q", _i), ("max_kv", _i)]
 
 
-def _on_current_device(*tensors):
-    """The library launches on the current device and the current stream of it: every tensor has to live there."""
+# Checks of the serving calls' tensors.  They are most of the host time of a small call: each property is asked for once.
+# The library launches on the current device and its current stream, so every tensor has to live there.
+def _device() -> int:
     import torch
-    dev = torch._C._cuda_getDevice()
-    for t in tensors:
-        if t is not None and not (t.is_cuda and t.get_device() == dev):
-            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+    try:
+        return torch._C._cuda_getDevice()
+    except RuntimeError:                                    # no GPU here: no tensor is on device -2
+        return -2
 
 
-def _rows(t, width: int, what: str) -> int:
-    """The row pitch of a 2-D tensor of `width` columns with unit column stride."""
-    if t.dim() != 2 or t.shape[1] != width or (t.stride(1) != 1 and width > 1):
-        raise ValueError(f"{what}: expected [rows, {width}] with unit column stride, got {tuple(t.shape)} with strides {t.stride()}")
-    return t.stride(0) if t.shape[0] > 1 else max(width, t.stride(0))
+def _elsewhere(t, dev: int, what: str):
+    return ValueError(f"{what} is on {t.device}, the current device is cuda:{dev}")
 
 
-def _list(t, dtype, shape, what: str):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+def _rows(t, rows: int, width: int, dtype, dev: int, what: str) -> int:
+    """The row pitch of a [rows, width] tensor with unit column stride."""
+    if t.dtype is not dtype or t.shape != (rows, width):
+        raise ValueError(f"{what}: expected {dtype} [{rows}, {width}], got {t.dtype} {tuple(t.shape)}")
+    ld, unit = t.stride()
+    if unit != 1 and width > 1:
+        raise ValueError(f"{what}: expected unit column stride, got {t.stride()}")
+    if t.get_device() != dev:                               # (-1 for host memory)
+        raise _elsewhere(t, dev, what)
+    return ld if rows > 1 else max(width, ld)
+
+
+def _list(t, dtype, shape, dev: int, what: str) -> int:
+    """The address of a contiguous tensor."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if t.get_device() != dev:
+        raise _elsewhere(t, dev, what)
+    return t.data_ptr()
+
+
+def _scratch(t, dev: int) -> int:
+    if t.get_device() != dev or not t.is_contiguous():
+        raise ValueError("workspace: expected a contiguous tensor on the current device")
+    return t.data_ptr()
 
 
 class PagedCache:
@@ -673,14 +693,15 @@ class PagedCache:
         codes, scales = (num_pages, kv_heads, page_size, head_dim), (num_pages, kv_heads, head_dim // 32, page_size)
         if tensors is None:
             tensors = [torch.zeros(s, dtype=torch.uint8, device="cuda") for s in (codes, scales, codes, scales)]
+        self.device = _device()
         for t, shape in zip(tensors, (codes, scales, codes, scales)):
-            _list(t, torch.uint8, shape, "cache")
-        _on_current_device(*tensors)
+            _list(t, torch.uint8, shape, self.device, "cache")
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = tensors
         self._d = _CacheDesc(num_pages, page_size, kv_heads, head_dim, *(t.data_ptr() for t in tensors))
 
-    @property
-    def desc(self):
+    def desc(self, dev: int):
+        if dev != self.device:
+            raise _elsewhere(self.k_codes, dev, "cache")
         return C.byref(self._d)
 
 
@@ -690,44 +711,34 @@ def batq_kv_paged_append(cache: PagedCache, k, v, slots, positions=None, q=None,
     values of M tokens into the cache at ``slots`` (int64 [M], outside the cache: not written), and rotate and transform
     their queries.  k, v: [M, kv_heads * head_dim], q: [M, q_heads * head_dim] or None.  Returns q_out (bf16)."""
     import torch
-    D, M = cache.head_dim, k.shape[0]
+    dev, D, M, dtype = _device(), cache.head_dim, k.shape[0], k.dtype
     width = cache.kv_heads * D
-    ldk, ldv = _rows(k, width, "k"), _rows(v, width, "v")
-    if v.shape[0] != M or v.dtype != k.dtype:
-        raise ValueError("k and v differ in rows or type")
-    _list(slots, torch.int64, (M,), "slots")
-    r = None
+    ldk, ldv = _rows(k, M, width, dtype, dev, "k"), _rows(v, M, width, dtype, dev, "v")
+    p_slots = _list(slots, torch.int64, (M,), dev, "slots")
+    r = p_pos = p_q = p_q_out = None
     if rope is not None:
-        if positions is None:
-            raise ValueError("a rotation needs positions")
-        if rope.dim() != 2:
-            raise ValueError("rope: expected [positions, rotary_dim]")
-        _list(rope, torch.float32, rope.shape, "rope")
-        _list(positions, torch.int32, (M,), "positions")
-        r = C.byref(_Rope(rope.data_ptr(), rope.shape[0], rope.shape[1], int(interleaved)))
+        if positions is None or rope.dim() != 2:
+            raise ValueError("a rotation needs positions, and a table [positions, rotary_dim]")
+        rows, rot = rope.shape
+        r = C.byref(_Rope(_list(rope, torch.float32, (rows, rot), dev, "rope"), rows, rot, interleaved))
+        p_pos = _list(positions, torch.int32, (M,), dev, "positions")
     q_heads = ldq = ldq_out = 0
     if q is not None:
-        q_heads = q.shape[1] // D
-        ldq = _rows(q, q_heads * D, "q")
-        if q.shape[0] != M or q.dtype != k.dtype:
-            raise ValueError("q and k differ in rows or type")
+        q_heads = q.shape[-1] // D
+        ldq = _rows(q, M, q_heads * D, dtype, dev, "q")
         if q_out is None:
             q_out = torch.empty((M, q_heads * D), dtype=torch.bfloat16, device=q.device)
-        ldq_out = _rows(q_out, q_heads * D, "q_out")
-        if q_out.shape[0] != M or q_out.dtype != torch.bfloat16:
-            raise ValueError("q_out: expected bf16 with the rows of q")
-    _on_current_device(cache.k_codes, k, v, slots, positions if r is not None else None, rope, q, q_out)
-    _check(lib.batq_kv_paged_append(cache.desc, tk.handle if tk is not None else None, tv.handle if tv is not None else None, r,
-                                    q.data_ptr() if q is not None else None, ldq, q_heads,
-                                    q_out.data_ptr() if q is not None else None, ldq_out, k.data_ptr(), ldk, v.data_ptr(), ldv,
-                                    _dtype_code(k), positions.data_ptr() if r is not None else None, slots.data_ptr(), M,
-                                    _stream()), "batq_kv_paged_append")
+        ldq_out = _rows(q_out, M, q_heads * D, torch.bfloat16, dev, "q_out")
+        p_q, p_q_out = q.data_ptr(), q_out.data_ptr()
+    _check(lib.batq_kv_paged_append(cache.desc(dev), None if tk is None else tk.handle, None if tv is None else tv.handle, r, p_q,
+                                    ldq, q_heads, p_q_out, ldq_out, k.data_ptr(), ldk, v.data_ptr(), ldv, _dtype_code(k), p_pos,
+                                    p_slots, M, torch._C._cuda_getCurrentRawStream(dev)), "batq_kv_paged_append")
     return q_out
 
 
 def batq_paged_attention_workspace(cache: PagedCache, q_heads: int, batch: int, total_q: int, max_q: int, max_kv: int) -> int:
     """Bytes of scratch for batq_paged_attention calls within these bounds on the current device."""
-    return int(lib.batq_paged_attention_workspace(cache.desc, q_heads, batch, total_q, max_q, max_kv))
+    return int(lib.batq_paged_attention_workspace(C.byref(cache._d), q_heads, batch, total_q, max_q, max_kv))
 
 
 def batq_paged_attention(cache: PagedCache, q, cu_q, kv_len, page_table, max_q: int, max_kv: int, scale: Optional[float] = None,
@@ -736,31 +747,26 @@ def batq_paged_attention(cache: PagedCache, q, cu_q, kv_len, page_table, max_q: 
     its last tokens) over the cache.  cu_q, kv_len: int32 [batch + 1], [batch]; page_table: int32 [batch, width].
     scale: 1 / sqrt(head_dim) if None.  lse: fp32 [total_q, q_heads] to be filled, or None.  Returns out (bf16)."""
     import torch
-    if q.dim() != 2 or q.dtype != torch.bfloat16:
-        raise ValueError("q: expected bf16 [total_q, q_heads * head_dim]")
-    T, q_heads = q.shape[0], q.shape[1] // cache.head_dim
-    ldq, batch = _rows(q, q_heads * cache.head_dim, "q"), kv_len.shape[0]
-    _list(cu_q, torch.int32, (batch + 1,), "cu_q")
-    _list(kv_len, torch.int32, (batch,), "kv_len")
-    if page_table.dim() != 2:
-        raise ValueError("page_table: expected [batch, width]")
-    _list(page_table, torch.int32, (batch, page_table.shape[1]), "page_table")
+    if q.dim() != 2 or page_table.dim() != 2:
+        raise ValueError("expected q [total_q, q_heads * head_dim] and page_table [batch, width]")
+    dev, D = _device(), cache.head_dim
+    T, width = q.shape
+    batch, table_width = page_table.shape
+    q_heads = width // D
+    ldq = _rows(q, T, q_heads * D, torch.bfloat16, dev, "q")
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    ldo = _rows(out, q.shape[1], "out")
-    if out.shape[0] != T or out.dtype != torch.bfloat16:
-        raise ValueError("out: expected bf16 with the rows of q")
-    if lse is not None:
-        _list(lse, torch.float32, (T, q_heads), "lse")
+        out = torch.empty((T, width), dtype=torch.bfloat16, device=q.device)
+    ldo = _rows(out, T, width, torch.bfloat16, dev, "out")
     if workspace is None:
         n = batq_paged_attention_workspace(cache, q_heads, batch, T, max_q, max_kv)
         workspace = torch.empty((max(n, 16),), dtype=torch.uint8, device=q.device)
-    _on_current_device(cache.k_codes, q, cu_q, kv_len, page_table, out, lse, workspace)
-    b = _PagedBatch(cu_q.data_ptr(), kv_len.data_ptr(), page_table.data_ptr(), batch, page_table.shape[1], T, max_q, max_kv)
-    _check(lib.batq_paged_attention(cache.desc, C.byref(b), q.data_ptr(), ldq, q_heads,
-                                    cache.head_dim ** -0.5 if scale is None else scale, int(causal), window, out.data_ptr(), ldo,
-                                    lse.data_ptr() if lse is not None else None, workspace.data_ptr(),
-                                    workspace.numel() * workspace.element_size(), _stream()), "batq_paged_attention")
+    b = _PagedBatch(_list(cu_q, torch.int32, (batch + 1,), dev, "cu_q"), _list(kv_len, torch.int32, (batch,), dev, "kv_len"),
+                    _list(page_table, torch.int32, (batch, table_width), dev, "page_table"), batch, table_width, T, max_q, max_kv)
+    _check(lib.batq_paged_attention(cache.desc(dev), C.byref(b), q.data_ptr(), ldq, q_heads, D ** -0.5 if scale is None else scale,
+                                    causal, window, out.data_ptr(), ldo,
+                                    None if lse is None else _list(lse, torch.float32, (T, q_heads), dev, "lse"),
+                                    _scratch(workspace, dev), workspace.nbytes, torch._C._cuda_getCurrentRawStream(dev)),
+           "batq_paged_attention")
     return out
 
 
@@ -775,26 +781,21 @@ def batq_lora_add(X, A, B, index, base=None, scales=None, out=None, out_dtype=No
     import torch
     if A.dim() != 3 or B.dim() != 3:
         raise ValueError("A, B: expected [adapters, rank, K] and [adapters, N, rank]")
+    dev = _device()
     n, rank, K = A.shape
     N, M = B.shape[1], X.shape[0]
-    ldx = _rows(X, K, "X")
-    _list(A, torch.bfloat16, (n, rank, K), "A")
-    _list(B, torch.bfloat16, (n, N, rank), "B")
-    _list(index, torch.int32, (M,), "index")
-    if scales is not None:
-        _list(scales, torch.float32, (n,), "scales")
+    ldx = _rows(X, M, K, X.dtype, dev, "X")
     if out is None:
         out = torch.empty((M, N), dtype=base.dtype if base is not None else out_dtype or torch.bfloat16, device=X.device)
-    ldo, ldb = _rows(out, N, "out"), N
-    if out.shape[0] != M or (base is not None and (base.shape[0] != M or base.dtype != out.dtype)):
-        raise ValueError("base and out: expected [M, N] of one type")
+    ldo = ldb = _rows(out, M, N, out.dtype, dev, "out")
+    p_base = None
     if base is not None:
-        ldb = _rows(base, N, "base")
+        ldb, p_base = _rows(base, M, N, out.dtype, dev, "base"), base.data_ptr()
     if workspace is None:
         workspace = torch.empty((max(batq_lora_workspace(M, K, N, rank, n), 16),), dtype=torch.uint8, device=X.device)
-    _on_current_device(X, A, B, index, scales, base, out, workspace)
-    _check(lib.batq_lora_add(X.data_ptr(), _dtype_code(X), M, K, ldx, A.data_ptr(), B.data_ptr(), N, rank, n,
-                             scales.data_ptr() if scales is not None else None, index.data_ptr(),
-                             base.data_ptr() if base is not None else None, ldb, out.data_ptr(), ldo, _dtype_code(out),
-                             workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream()), "batq_lora_add")
+    _check(lib.batq_lora_add(X.data_ptr(), _dtype_code(X), M, K, ldx, _list(A, torch.bfloat16, (n, rank, K), dev, "A"),
+                             _list(B, torch.bfloat16, (n, N, rank), dev, "B"), N, rank, n,
+                             None if scales is None else _list(scales, torch.float32, (n,), dev, "scales"),
+                             _list(index, torch.int32, (M,), dev, "index"), p_base, ldb, out.data_ptr(), ldo, _dtype_code(out),
+                             _scratch(workspace, dev), workspace.nbytes, torch._C._cuda_getCurrentRawStream(dev)), "batq_lora_add")
     return out
