@@ -889,7 +889,7 @@ batq_status batq_kv_paged_append(const batq_paged_cache* cache, const batq_trans
     if (batq_status st = check_paged_cache(cache); st != BATQ_OK) return st;
     if (!dtype_ok(xdtype)) return BATQ_ERR_DTYPE;
     const int D = cache->head_dim, width = cache->kv_heads * D;
-    if (M < 0 || ldk < width || ldv < width || q_heads < 0 || q_heads > (1 << 19) || q_heads % cache->kv_heads != 0)
+    if (M < 0 || M > (1 << 30) || ldk < width || ldv < width || q_heads < 0 || q_heads > (1 << 19) || q_heads % cache->kv_heads != 0)
         return BATQ_ERR_SHAPE;
     if (q_heads > 0 && (ldq < (int64_t)q_heads * D || ldq_out < (int64_t)q_heads * D)) return BATQ_ERR_SHAPE;
     if ((tk && tk->K != width) || (tv && tv->K != width)) return BATQ_ERR_MISMATCH;

@@ -11,6 +11,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+constexpr int kFewUnits = 2048;                             // (32 tokens, block) units up to which append_few serves
+
 struct AppendArgs {
     const void *q, *k, *v;
     int64_t ldq, ldk, ldv;                                  // elements
@@ -25,6 +27,7 @@ struct AppendArgs {
     int64_t num_slots;
     int table_rows, rotary_dim, interleaved;
     int M, q_heads, kv_heads, group, page_shift;
+    int tiles_wg;                                           // append_many: 32-token tiles of a workgroup
 };
 
 __device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
@@ -89,93 +92,45 @@ __device__ __forceinline__ bf16x8 to_bf16(const float* x) {
     return r;
 }
 
-// One wave per (32 tokens, MX block of a query, key or value head).  Lane l holds channels 16 (l / 32) .. + 15 of the
-// block for token l % 32, before the transform and after it: the operand order of the 32x32x16 matrix instruction
-// (the handle's split operands are stored so that its results come in the same order).
-template <typename XT, int D>
-__global__ void __launch_bounds__(256)
-append_kernel(const AppendArgs a) {
-    constexpr int kBlocks = D / 32;
-    const int lane = threadIdx.x & 63, l32 = lane & 31, kg = lane >> 5;
-    const int per_tile = (a.q_heads + 2 * a.kv_heads) * kBlocks;
-    const int tiles = (a.M + 31) >> 5;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (unit >= (int64_t)tiles * per_tile) return;          // wave-uniform
-    const int tile = (int)(unit / per_tile);
-    int hb = (int)(unit - (int64_t)tile * per_tile);        // head * kBlocks + block, queries first
-    int kind = 0;                                           // 0 query, 1 key, 2 value
-    if (hb >= a.q_heads * kBlocks) {
-        hb -= a.q_heads * kBlocks;
-        kind = 1;
-        if (hb >= a.kv_heads * kBlocks) hb -= a.kv_heads * kBlocks, kind = 2;
-    }
-    const int head = hb / kBlocks, b = hb % kBlocks;
-    const int m = tile * 32 + l32, mm = min(m, a.M - 1);    // rows past the end repeat the last one: computed, not stored
-    bool live = m < a.M;
-    const float* row = nullptr;
-    if (a.table && kind != 2) {
-        const int p = a.positions[mm];
-        const bool inside = p >= 0 && p < a.table_rows;
-        live = live && inside;
-        row = a.table + (size_t)(inside ? p : 0) * a.rotary_dim;
-    } else if (a.table) {
-        const int p = a.positions[mm];
-        live = live && p >= 0 && p < a.table_rows;
-    }
-    const XT* src = kind == 0 ? static_cast<const XT*>(a.q) + (size_t)mm * a.ldq
-                  : kind == 1 ? static_cast<const XT*>(a.k) + (size_t)mm * a.ldk
-                              : static_cast<const XT*>(a.v) + (size_t)mm * a.ldv;
-    float y[16];
-    load_rotated8<XT>(src + (size_t)head * D, b * 32 + 16 * kg, a, row, *reinterpret_cast<float(*)[8]>(y));
-    load_rotated8<XT>(src + (size_t)head * D, b * 32 + 16 * kg + 8, a, row, *reinterpret_cast<float(*)[8]>(y + 8));
+// What a wave works on: a block of a head.
+enum Kind { kQuery, kKey, kValue };
 
-    const int blk = (kind == 0 ? head / a.group : head) * kBlocks + b;      // block of the transform
-    const uint4* op = kind == 0 ? a.tq : kind == 1 ? a.tk : a.tv;
-    if (op) {
-        // y = h + m + l in bf16 terms, T = t0 + t1 + t2 likewise: the six products that matter at 24 bits are summed in
-        // fp32, smallest first (bf16 input that was not rotated has m = l = 0: the quantiser's own three products)
-        bf16x8 t[6];
+// The transform of 16 channels a lane (operand order of the 32x32x16 matrix instruction, see below), in place.
+// y = h + m + l in bf16 terms, T = t0 + t1 + t2 likewise: the six products that matter at 24 bits are summed in fp32,
+// smallest first (bf16 input that was not rotated, `exact`, has m = l = 0: the quantiser's own three products).
+__device__ __forceinline__ void transform16(float (&y)[16], const bf16x8 (&t)[6], bool exact) {
+    bf16x8 xs[3][2];
 #pragma unroll
-        for (int i = 0; i < 6; ++i) t[i] = __builtin_bit_cast(bf16x8, op[(size_t)blk * 384 + i * 64 + lane]);
-        const bool exact = sizeof(XT) == 2 && !row;         // wave-uniform
-        bf16x8 xs[3][2];
+    for (int h = 0; h < 2; ++h) {
+        float r[8];
+        xs[0][h] = to_bf16(y + 8 * h);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float r[8];
-            xs[0][h] = to_bf16(y + 8 * h);
+        for (int i = 0; i < 8; ++i) r[i] = y[8 * h + i] - (float)xs[0][h][i];
+        xs[1][h] = to_bf16(r);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) r[i] = y[8 * h + i] - (float)xs[0][h][i];
-            xs[1][h] = to_bf16(r);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) r[i] -= (float)xs[1][h][i];
-            xs[2][h] = to_bf16(r);
-        }
-        v16f acc = {};
-        auto product = [&](int xt, int tt) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t[tt * 2 + h], xs[xt][h], acc, 0, 0, 0);
-        };
-        if (!exact) {
-            product(2, 0);
-            product(1, 1);
-        }
-        product(0, 2);
-        if (!exact) product(1, 0);
-        product(0, 1);
-        product(0, 0);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) y[r] = acc[r];
+        for (int i = 0; i < 8; ++i) r[i] -= (float)xs[1][h][i];
+        xs[2][h] = to_bf16(r);
     }
+    v16f acc = {};
+    auto product = [&](int xt, int tt) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(t[tt * 2 + h], xs[xt][h], acc, 0, 0, 0);
+    };
+    if (!exact) {
+        product(2, 0);
+        product(1, 1);
+    }
+    product(0, 2);
+    if (!exact) product(1, 0);
+    product(0, 1);
+    product(0, 0);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) y[r] = acc[r];
+}
 
-    if (kind == 0) {
-        if (!live) return;
-        uint16_t* o = a.q_out + (size_t)m * a.ldq_out + (size_t)hb * 32 + 16 * kg;
-        *reinterpret_cast<bf16x8*>(o) = to_bf16(y);
-        *reinterpret_cast<bf16x8*>(o + 8) = to_bf16(y + 8);
-        return;
-    }
-    const float* clip = kind == 1 ? a.clip_k : a.clip_v;
-    const float* clip_max = kind == 1 ? a.clip_k_max : a.clip_v_max;
+// Clips and quantises the lane's half of block blk; returns the codes, and the scale byte in *scale.
+__device__ __forceinline__ uint4 quantise16(float (&y)[16], const float* clip, const float* clip_max, int blk, uint32_t* scale) {
+    const int lane = threadIdx.x & 63;
     auto other_half = [&](float x) -> float {
         return __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute((lane ^ 32) << 2, __builtin_bit_cast(int, x)));
     };
@@ -203,14 +158,330 @@ append_kernel(const AppendArgs a) {
     const uint32_t sb = e8m0_of_bound_fp8(bound);
     const float sc = scale_operand(sb);
     const uint2 o0 = encode8_fp8(y, bound, sb, sc), o1 = encode8_fp8(y + 8, bound, sb, sc);
+    *scale = sb;
+    return uint4{o0.x, o0.y, o1.x, o1.y};
+}
+
+// Head number `head` of a token's queries, keys and values, in that order.
+__device__ __forceinline__ Kind kind_of(const AppendArgs& a, int* head) {
+    if (*head < a.q_heads) return kQuery;
+    *head -= a.q_heads;
+    if (*head < a.kv_heads) return kKey;
+    *head -= a.kv_heads;
+    return kValue;
+}
+
+// Few tokens (decoding): a chain of latencies.  One wave per (32 tokens, MX block of a head).  Lane l holds channels
+// 16 (l / 32) .. + 15 of the block for token l % 32, before the transform and after it (the handle's split operands are
+// stored so that the matrix instruction's results come in the order of its operands).
+template <typename XT, int D>
+__global__ void __launch_bounds__(256)
+append_few(const AppendArgs a) {
+    constexpr int kBlocks = D / 32;
+    const int lane = threadIdx.x & 63, l32 = lane & 31, kg = lane >> 5;
+    const int per_tile = (a.q_heads + 2 * a.kv_heads) * kBlocks;
+    const int tiles = (a.M + 31) >> 5;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (unit >= (int64_t)tiles * per_tile) return;          // wave-uniform
+    const int tile = (int)(unit / per_tile), hb = (int)(unit - (int64_t)tile * per_tile), b = hb % kBlocks;
+    int head = hb / kBlocks;
+    const Kind kind = kind_of(a, &head);
+    const int m = tile * 32 + l32, mm = min(m, a.M - 1);    // rows past the end repeat the last one: computed, not stored
+    bool live = m < a.M;
+    const float* row = nullptr;
+    if (a.table) {
+        const int p = a.positions[mm];
+        const bool inside = p >= 0 && p < a.table_rows;
+        live = live && inside;
+        if (kind != kValue) row = a.table + (size_t)(inside ? p : 0) * a.rotary_dim;
+    }
     const int64_t slot = a.slots[mm];
+    const XT* src = kind == kQuery ? static_cast<const XT*>(a.q) + (size_t)mm * a.ldq
+                  : kind == kKey   ? static_cast<const XT*>(a.k) + (size_t)mm * a.ldk
+                                   : static_cast<const XT*>(a.v) + (size_t)mm * a.ldv;
+    const int blk = (kind == kQuery ? head / a.group : head) * kBlocks + b;     // block of the transform
+    const uint4* op = kind == kQuery ? a.tq : kind == kKey ? a.tk : a.tv;
+    bf16x8 t[6];
+    if (op)
+#pragma unroll
+        for (int i = 0; i < 6; ++i) t[i] = __builtin_bit_cast(bf16x8, op[(size_t)blk * 384 + i * 64 + lane]);
+    float y[16];
+    load_rotated8<XT>(src + (size_t)head * D, b * 32 + 16 * kg, a, row, *reinterpret_cast<float(*)[8]>(y));
+    load_rotated8<XT>(src + (size_t)head * D, b * 32 + 16 * kg + 8, a, row, *reinterpret_cast<float(*)[8]>(y + 8));
+    if (op) transform16(y, t, sizeof(XT) == 2 && !row);
+
+    if (kind == kQuery) {
+        if (!live) return;
+        uint16_t* o = a.q_out + (size_t)m * a.ldq_out + (size_t)head * D + b * 32 + 16 * kg;
+        *reinterpret_cast<bf16x8*>(o) = to_bf16(y);
+        *reinterpret_cast<bf16x8*>(o + 8) = to_bf16(y + 8);
+        return;
+    }
+    uint32_t sb;
+    const uint4 codes = kind == kKey ? quantise16(y, a.clip_k, a.clip_k_max, blk, &sb) : quantise16(y, a.clip_v, a.clip_v_max, blk, &sb);
     if (!live || slot < 0 || slot >= a.num_slots) return;
-    const int64_t page = slot >> a.page_shift, off = slot & ((1 << a.page_shift) - 1);
-    uint8_t* codes = kind == 1 ? a.k_codes : a.v_codes;
-    uint8_t* scales = kind == 1 ? a.k_scales : a.v_scales;
-    const int64_t ph = page * a.kv_heads + head;
-    *reinterpret_cast<uint4*>(codes + (((ph << a.page_shift) + off) * D + b * 32 + 16 * kg)) = uint4{o0.x, o0.y, o1.x, o1.y};
-    if (kg == 0) scales[((ph * kBlocks + b) << a.page_shift) + off] = (uint8_t)sb;
+    const int64_t off = slot & ((1 << a.page_shift) - 1), ph = (slot >> a.page_shift) * a.kv_heads + head;
+    *reinterpret_cast<uint4*>((kind == kKey ? a.k_codes : a.v_codes) + (((ph << a.page_shift) + off) * D + b * 32 + 16 * kg)) = codes;
+    if (kg == 0) (kind == kKey ? a.k_scales : a.v_scales)[((ph * kBlocks + b) << a.page_shift) + off] = (uint8_t)sb;
+}
+
+// Orders a wave's own LDS accesses across its lanes (they are carried out in order; this keeps the compiler to it).
+__device__ __forceinline__ void wave_lds_order() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+template <typename XT, int D>
+constexpr int many_lds() { return 4 * 2 * 32 * D * (int)sizeof(XT) + 32 * 512; }    // two tiles a wave, a tile's rows of the table
+
+// Many tokens (prompts): bound by the streams in and out, and close behind them the vector instructions.  One wave per
+// head and range of 32-token tiles: the head's split operands stay in registers.  Rows go to LDS by LDS-direct loads, a
+// tile ahead, with neighbouring lanes in the same row, and results leave from the places that their inputs have been read
+// from.  A 16-byte chunk's place in its row is XORed with the row's number, so that a lane's address for chunk c is
+// (its row's address) ^ 16 c.  The four waves of a workgroup share the tile's cosines and sines.  For rotations whose
+// pairs a lane holds (interleaved, or whole blocks apart); arithmetic as in append_few, same bits.
+template <typename XT, int D>
+__global__ void __launch_bounds__(256, sizeof(XT) == 4 && D == 128 ? 1 : 2)
+append_many(const AppendArgs a) {
+    constexpr int kBlocks = D / 32, kSize = (int)sizeof(XT), kCh = D * kSize / 16, kRows = 64 / kCh, kLoads = 32 / kRows, kTile = 32 * kCh * 16;
+    constexpr int kQCh = D / 8, kCCh = D / 16;              // 16-byte chunks of a row of queries out, of codes
+    extern __shared__ __align__(16) uint8_t s_raw[];
+    typedef __attribute__((address_space(3))) uint8_t lds_byte;
+    int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint8_t* const s_x = s_raw + wave * 2 * kTile;
+    uint8_t* const s_t = s_raw + 4 * 2 * kTile;             // [32][128] floats
+    const uint32_t x_lds = (uint32_t)(uintptr_t)(lds_byte*)s_raw + wave * 2 * kTile;
+    const int heads = a.q_heads + 2 * a.kv_heads, head_groups = (heads + 3) / 4;
+    int head = blockIdx.x % head_groups * 4 + wave;
+    const bool busy = head < heads;                         // (the others keep the workgroup's barriers)
+    if (!busy) head = 0;
+    const Kind kind = kind_of(a, &head);
+    const int tiles = (a.M + 31) >> 5, tile0 = (int)(blockIdx.x / head_groups) * a.tiles_wg, tile1 = min(tiles, tile0 + a.tiles_wg);
+    const uint4* op = kind == kQuery ? a.tq : kind == kKey ? a.tk : a.tv;
+    const int blk0 = (kind == kQuery ? head / a.group : head) * kBlocks;
+    const float* clip = kind == kKey ? a.clip_k : a.clip_v;
+    const float* clip_max = kind == kKey ? a.clip_k_max : a.clip_v_max;
+    const XT* src = (kind == kQuery ? static_cast<const XT*>(a.q) : kind == kKey ? static_cast<const XT*>(a.k) : static_cast<const XT*>(a.v)) + (size_t)head * D;
+    const int64_t ld = kind == kQuery ? a.ldq : kind == kKey ? a.ldk : a.ldv;
+    const bool rotated = a.table && kind != kValue;
+    const int rot = rotated ? a.rotary_dim : 0, half = rot >> 1;
+    bf16x8 t[kBlocks][6];
+    if (op)
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int i = 0; i < 6; ++i) t[b][i] = __builtin_bit_cast(bf16x8, op[(size_t)(blk0 + b) * 384 + i * 64 + lane]);
+    // byte address of row r's chunk 0 (XOR 16 c: chunk c) among rows of `ch` chunks
+    auto at = [](int r, int ch) { return r * ch * 16 + (ch == 8 ? (r >> 1) & 7 : r & 15) * 16; };
+    auto request = [&](int tile, int buf) {                 // (rows past the end repeat the last one)
+        const uint8_t* from = reinterpret_cast<const uint8_t*>(src + (size_t)tile * 32 * ld);
+        const int rows_left = a.M - 1 - tile * 32;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int r = i * kRows + lane / kCh;           // this lane's 16 bytes of LDS hold chunk (place) ^ (the row's XOR)
+            const int c = (lane % kCh) ^ (at(r, kCh) / 16 % kCh);
+            const uint32_t voff = (uint32_t)min(r, rows_left) * (uint32_t)(ld * kSize) + (uint32_t)c * 16;
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+                         :: "v"(voff), "s"(from), "s"(x_lds + (uint32_t)(buf * kTile + i * 1024)) : "memory");
+        }
+    };
+    // the tile's rows of the table: thread i moves chunks i, i + 256, ... of rotary_dim / 4 a row
+    const int t_chunks = a.table ? a.rotary_dim / 4 : 1;
+    u32x4 tw[4] = {};
+    int pos[4] = {};
+    auto positions = [&](int tile) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int r = (x * 256 + (int)threadIdx.x) / t_chunks;
+            pos[x] = r < 32 ? a.positions[min(tile * 32 + r, a.M - 1)] : 0;
+        }
+    };
+    auto request_table = [&]() {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int i = x * 256 + (int)threadIdx.x;
+            if (i < 32 * t_chunks)
+                tw[x] = *(reinterpret_cast<const u32x4*>(a.table + (size_t)(pos[x] >= 0 && pos[x] < a.table_rows ? pos[x] : 0) * a.rotary_dim) + i % t_chunks);
+        }
+    };
+    // a tile's slots and positions are asked for a tile ahead (the table's positions two): in the loop nothing is waited
+    // for but the one wait at its top
+    auto slot_of = [&](int tile) { return kind == kQuery ? (int64_t)0 : a.slots[min(tile * 32 + (lane & 31), a.M - 1)]; };
+    auto position_of = [&](int tile) { return a.table ? a.positions[min(tile * 32 + (lane & 31), a.M - 1)] : 0; };
+    if (a.table) {
+        positions(tile0);
+        request_table();
+        positions(min(tile0 + 1, tiles - 1));
+    }
+    int64_t next_slot = slot_of(tile0);                     // (every workgroup has a tile)
+    int next_pos = position_of(tile0);
+    if (busy) request(tile0, 0);
+    for (int tile = tile0, buf = 0; tile < tile1; ++tile, buf ^= 1) {
+        // opaque here: otherwise every LDS address of a tile is kept in a register of its own across the tiles
+        asm volatile("" : "+v"(lane));
+        const int l32 = lane & 31, kg = lane >> 5, m = tile * 32 + l32;
+        __builtin_amdgcn_s_waitcnt(0x0F70);                 // vmcnt(0): the tile has landed
+        asm volatile("" ::: "memory");
+        const int64_t slot = next_slot;
+        const bool there = m < a.M && (!a.table || (next_pos >= 0 && next_pos < a.table_rows));
+        const bool live = there && slot >= 0 && slot < a.num_slots;
+        if (a.table) {
+            __syncthreads();                                // the last tile's angles have been used
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int i = x * 256 + (int)threadIdx.x, r = i / t_chunks;
+                if (i < 32 * t_chunks) *reinterpret_cast<u32x4*>(s_t + (at(r, 32) ^ ((i - r * t_chunks) * 16))) = tw[x];
+            }
+            if (tile + 1 < tile1) {
+                request_table();
+                positions(min(tile + 2, tiles - 1));
+            }
+            __syncthreads();
+        }
+        if (tile + 1 < tile1) {
+            next_slot = slot_of(tile + 1), next_pos = position_of(tile + 1);
+            if (busy) request(tile + 1, buf ^ 1);
+        }
+        if (!busy) continue;
+        const int64_t off = slot & ((1 << a.page_shift) - 1), ph = (slot >> a.page_shift) * a.kv_heads + head;
+        uint8_t* const x_at = s_x + buf * kTile;
+        const int own = at(l32, kCh) ^ (kg * 16 * kSize), t_at = at(l32, 32);    // channels 16 kg ..: XOR 32 b kSize: of block b
+        auto block16 = [&](int b, float (&x)[16]) {         // channels 16 kg .. + 15 of block b of this lane's token
+#pragma unroll
+            for (int i = 0; i < kSize; ++i) {
+                const u32x4 v = *reinterpret_cast<const u32x4*>(x_at + (own ^ (32 * kSize * b + 16 * i)));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (kSize == 4) x[4 * i + e] = __uint_as_float(v[e]);
+                    else x[8 * i + 2 * e] = __uint_as_float(v[e] << 16), x[8 * i + 2 * e + 1] = __uint_as_float(v[e] & 0xFFFF0000u);
+                }
+            }
+        };
+        auto angles4 = [&](int j, float (&x)[4]) {          // entries j .. j + 3 of this lane's row of the table
+            const u32x4 v = *reinterpret_cast<const u32x4*>(s_t + (t_at ^ (4 * j)));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(v[i]);
+        };
+        auto interleaved16 = [&](float (&y)[16], int b) {   // (rotary_dim is a multiple of 16)
+            const int c0 = 32 * b + 16 * kg;
+            if (c0 >= rot) return;
+#pragma unroll
+            for (int i = 0; i < 16; i += 8) {
+                float c[4], s[4];
+                angles4((c0 + i) >> 1, c);
+                angles4(half + ((c0 + i) >> 1), s);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = y[i + 2 * e], r = y[i + 2 * e + 1];
+                    y[i + 2 * e] = rot_first(p, r, c[e], s[e]);
+                    y[i + 2 * e + 1] = rot_second(p, r, c[e], s[e]);
+                }
+            }
+        };
+        auto finish = [&](float (&y)[16], const bf16x8 (&tb)[6], int b) {
+            if (op) transform16(y, tb, kSize == 2 && !rotated);
+            if (kind == kQuery) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) *reinterpret_cast<bf16x8*>(x_at + (own ^ (32 * kSize * b + 16 * h))) = to_bf16(y + 8 * h);
+            } else {
+                uint32_t sb;
+                const uint4 codes = quantise16(y, clip, clip_max, blk0 + b, &sb);
+                *reinterpret_cast<uint4*>(x_at + (own ^ (32 * kSize * b))) = codes;
+                if (live && kg == 0) (kind == kKey ? a.k_scales : a.v_scales)[((ph * kBlocks + b) << a.page_shift) + off] = (uint8_t)sb;
+            }
+            __builtin_amdgcn_sched_barrier(0);              // block by block: interleaved, they would not fit the registers
+        };
+        auto pair = [&](const bf16x8 (&t0)[6], const bf16x8 (&t1)[6], int b0, int b1) {     // two blocks
+            float y0[16], y1[16];
+            block16(b0, y0);
+            if (!rotated || a.interleaved) {
+                if (rotated) interleaved16(y0, b0);
+                finish(y0, t0, b0);
+                block16(b1, y1);
+                if (rotated) interleaved16(y1, b1);
+                finish(y1, t1, b1);
+                return;
+            }
+            block16(b1, y1);
+            if (32 * b0 < half)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    float c[4], s[4];
+                    angles4(32 * b0 + 16 * kg + i, c);
+                    angles4(half + 32 * b0 + 16 * kg + i, s);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = y0[i + e], r = y1[i + e];
+                        y0[i + e] = rot_first(p, r, c[e], s[e]);
+                        y1[i + e] = rot_second(p, r, c[e], s[e]);
+                    }
+                }
+            finish(y0, t0, b0);
+            finish(y1, t1, b1);
+        };
+        if constexpr (kBlocks == 2) {
+            pair(t[0], t[1], 0, 1);
+        } else if (half == 64) {
+            pair(t[0], t[2], 0, 2);
+            pair(t[1], t[3], 1, 3);
+        } else {
+            pair(t[0], t[1], 0, 1);
+            pair(t[2], t[3], 2, 3);
+        }
+        wave_lds_order();
+        // rows out: lane l moves chunk l % kQCh (kCCh) of row l / kQCh, from where its lane put it; what the row's own lane
+        // knows about it is shuffled over
+        if (kind == kQuery) {
+#pragma unroll
+            for (int i = 0; i < kQCh / 2; ++i) {
+                const int r = i * (64 / kQCh) + lane / kQCh, c = lane % kQCh;
+                const u32x4 v = *reinterpret_cast<const u32x4*>(x_at + (at(r, kCh) ^ ((c >> 1 & 1) * 16 * kSize) ^ ((c >> 2) * 32 * kSize + (c & 1) * 16)));
+                if (__shfl((int)there, r)) store16_through(a.q_out + (size_t)(tile * 32 + r) * a.ldq_out + (size_t)head * D + c * 8, v);
+            }
+        } else {
+            const int64_t to = live ? ((ph << a.page_shift) + off) * D : -1;
+#pragma unroll
+            for (int i = 0; i < kCCh / 2; ++i) {
+                const int r = i * (64 / kCCh) + lane / kCCh, c = lane % kCCh;
+                const u32x4 v = *reinterpret_cast<const u32x4*>(x_at + (at(r, kCh) ^ ((c & 1) * 16 * kSize) ^ ((c >> 1) * 32 * kSize)));
+                const int64_t from = (int64_t)(((uint64_t)(uint32_t)__shfl((int)(to >> 32), r) << 32) | (uint32_t)__shfl((int)to, r));
+                if (from >= 0) *reinterpret_cast<u32x4*>((kind == kKey ? a.k_codes : a.v_codes) + from + c * 16) = v;
+            }
+        }
+        wave_lds_order();
+    }
+}
+
+template <typename XT, int D>
+hipError_t launch_append(AppendArgs& a, hipStream_t stream) {
+    const int tiles = (int)(((int64_t)a.M + 31) / 32), heads = a.q_heads + 2 * a.kv_heads;
+    const int64_t units = (int64_t)tiles * heads * (D / 32);
+    // append_many: pairs of a rotation in one lane, and rows of a tile within 32-bit offsets
+    const int64_t ld = a.ldq > a.ldk ? (a.ldq > a.ldv ? a.ldq : a.ldv) : (a.ldk > a.ldv ? a.ldk : a.ldv);
+    const bool fits = (!a.table || a.interleaved || a.rotary_dim % 64 == 0) && ld * (int64_t)sizeof(XT) < (int64_t(1) << 26);
+    if (units <= kFewUnits || !fits) {
+        append_few<XT, D><<<(unsigned)((units + 3) / 4), 256, 0, stream>>>(a);
+        return hipGetLastError();
+    }
+    int dev = 0;
+    if (hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
+    hipError_t e;
+    const int cus = device_compute_units(dev, &e);
+    if (e != hipSuccess) return e;
+    constexpr int lds = many_lds<XT, D>();
+    if constexpr (lds > 65536)
+        if (e = ensure_dynamic_lds<&append_many<XT, D>>(dev, lds); e != hipSuccess) return e;
+    // tiles of a workgroup: two workgroups to a compute unit at a time, in whole rounds
+    const int groups = (heads + 3) / 4;
+    int64_t n = ((int64_t)tiles * groups + 2 * cus - 1) / (2 * cus);
+    while (n < 16 && (tiles + n - 1) / n * groups > 2 * cus) ++n;
+    if (n > 16) n = 16;
+    a.tiles_wg = (int)n;
+    const int64_t grid = (tiles + n - 1) / n * groups;
+    append_many<XT, D><<<(unsigned)grid, 256, lds, stream>>>(a);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -236,16 +507,8 @@ hipError_t launch_kv_paged_append(const batq_paged_cache& c, const batq_transfor
     a.num_slots = (int64_t)c.num_pages * c.page_size;
     a.q_heads = q_heads, a.kv_heads = c.kv_heads, a.group = q_heads ? q_heads / c.kv_heads : 1;
     a.page_shift = __builtin_ctz((unsigned)c.page_size);
-    const int64_t units = (int64_t)((M + 31) / 32) * (q_heads + 2 * c.kv_heads) * (c.head_dim / 32);
-    const dim3 grid((unsigned)((units + 3) / 4)), block(256);
-    if (xdtype == BATQ_BF16) {
-        if (c.head_dim == 64) append_kernel<uint16_t, 64><<<grid, block, 0, stream>>>(a);
-        else append_kernel<uint16_t, 128><<<grid, block, 0, stream>>>(a);
-    } else {
-        if (c.head_dim == 64) append_kernel<float, 64><<<grid, block, 0, stream>>>(a);
-        else append_kernel<float, 128><<<grid, block, 0, stream>>>(a);
-    }
-    return hipGetLastError();
+    if (xdtype == BATQ_BF16) return c.head_dim == 64 ? launch_append<uint16_t, 64>(a, stream) : launch_append<uint16_t, 128>(a, stream);
+    return c.head_dim == 64 ? launch_append<float, 64>(a, stream) : launch_append<float, 128>(a, stream);
 }
 
 }  // namespace batq

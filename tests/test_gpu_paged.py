@@ -204,6 +204,34 @@ def test_append_token_by_token_equals_one_call(B):
         assert np.array_equal(x, y)
 
 
+@pytest.mark.parametrize("dtype,D,rot,inter", [("bf16", 128, 128, False), ("bf16", 64, 48, False), ("f32", 128, 64, True), ("f32", 64, 32, False)])
+def test_append_of_many_tokens_equals_pieces(B, dtype, D, rot, inter):
+    """A long call and its pieces (other kernels, other tiles) leave the same bytes and the same queries."""
+    import torch
+    rng = np.random.default_rng(13)
+    M, hq, hkv, page = 2100, 6, 3, 64
+    X = torch.randn((M, (hq + 2 * hkv) * D), device="cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    q, k, v = X.split((hq * D, hkv * D, hkv * D), 1)
+    tk, _, _ = _transforms(B, rng, hkv, D, "kron")
+    tv, _, _ = _transforms(B, rng, hkv, D, "dense")
+    table, slots = dev(ref.rope_table(4000, rot)), torch.randperm(40 * page, device="cuda")[:M]
+    slots[5], slots[1000] = -1, 10 ** 12
+    pos = torch.randint(0, 4000, (M,), device="cuda", dtype=torch.int32)
+    pos[7], pos[2000] = -1, 4000
+    for t in ((tk, tv), (None, None)):
+        a, b = B.PagedCache(40, page, hkv, D), B.PagedCache(40, page, hkv, D)
+        qa = torch.full((M, hq * D), 7.0, dtype=torch.bfloat16, device="cuda")
+        qb = qa.clone()
+        B.batq_kv_paged_append(a, k, v, slots, pos, q=q, q_out=qa, rope=table, interleaved=inter, tk=t[0], tv=t[1])
+        for lo in range(0, M, 111):
+            s = slice(lo, min(M, lo + 111))
+            B.batq_kv_paged_append(b, k[s], v[s], slots[s], pos[s], q=q[s], q_out=qb[s], rope=table, interleaved=inter, tk=t[0], tv=t[1])
+        torch.cuda.synchronize()
+        assert torch.equal(qa, qb) and bool((qa[7] == 7.0).all()) and bool((qa[2000] == 7.0).all())
+        for x, y in zip(host(a), host(b)):
+            assert np.array_equal(x, y)
+
+
 # ---------------------------------------------------------------------------------------- attention
 def attend_case(rng, B, lens, qs, hq, hkv, D, page, spare=0):
     lens, qs = np.array(lens), np.array(qs)
