@@ -83,18 +83,18 @@ __device__ __forceinline__ float scale_byte(uint32_t w, int i) { return scale_op
 __device__ __forceinline__ float shuffle_xor(float x, int d) { return __shfl_xor(x, d); }
 
 // Few query rows to a key head (decoding, short drafts): bound by the stream of codes.  A workgroup takes one part of one
-// (sequence, key head); its four waves take blocks of 64 tokens in turn, each with its own running maximum, and are
+// (sequence, key head); its four waves take blocks of 32 tokens in turn, each with its own running maximum, and are
 // joined at the end.  Rows: query token i and head j of the group are row i * group + j of NT tiles of 16.
-//   keys     lane (m, g) = (l % 16, l / 16) loads channels [g D/4, (g + 1) D/4) of tokens 4m .. 4m + 3 straight into the
-//            operand of S^T's tile t = 0..3 (tokens 4m + t): the order in which a product runs over channels is free, so a
-//            lane's 16 bytes are contiguous, and its scales of the four tokens are one dword.
-//   scores   result element r of tile t in lane (n, g) is row n and token 16g + 4r + t
-//   values   lane (m, g) loads channels [m D/16, (m + 1) D/16) of tokens 16g .. 16g + 15, converts them with their tokens'
+//   keys     lane (m, g) = (l % 16, l / 16) loads channels [g D/4, (g + 1) D/4) of tokens 2m and 2m + 1 straight into the
+//            operands of S^T's tiles 0 and 1: the order in which a product runs over channels is free, so a lane's
+//            16 bytes are contiguous, and its scales of the two tokens are one 16-bit word
+//   scores   result element r of tile t in lane (n, g) is row n and token 8g + 2r + t
+//   values   lane (m, g) loads channels [m D/16, (m + 1) D/16) of tokens 8g .. 8g + 7, converts them with their tokens'
 //            scales and turns pairs of tokens by 2 x 2; tile j of O^T has channels m D/16 + j
-// Loads of the next block's keys are issued when this block's are used up, likewise the values, and page numbers one
-// block further ahead: nothing passes through LDS before the end.
+// Loads of the next block's keys are issued when this block's are used up, likewise the values: nothing passes through LDS
+// before the end.  The reference of the exponentials moves only when a row's maximum has grown by more than 2^8.
 template <int D, int NT>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(256, NT == 1 ? 3 : 2)
 attend_few(const AttnArgs a) {
     constexpr int kC = D / 4, kV = D / 16, kU = D / 32;      // channels of a key lane, of a value lane, products per tile
     constexpr int kRow = D + 4;                             // floats of a row in LDS (spread over the banks)
@@ -108,6 +108,57 @@ attend_few(const AttnArgs a) {
     const int rows = s.n * a.group;
     if (rows == 0 || rows > a.few_rows || part >= live_parts(s, a.few_len)) return;
     const int t_begin = (s.t_lo & ~63) + part * a.few_len, t_end = min(s.t_hi, t_begin + a.few_len);
+
+    const int32_t* table = a.page_table + (size_t)b * a.table_width;
+    const int page_mask = (1 << a.page_shift) - 1;
+    const int last_page = max(0, (s.len - 1) >> a.page_shift);      // entries behind it are not read
+    // lane i holds the page of tokens t_begin + 16 i .. + 15 (a part is at most 1024 long): page numbers are not loaded in
+    // the loop, where waiting for them would wait for the codes requested before them
+    const int pages = t_begin < t_end ? table[min((t_begin + 16 * lane) >> a.page_shift, last_page)] : 0;
+    auto entry = [&](int t) { return __shfl(pages, (t - t_begin) >> 4); };
+
+    u32x4 kw[2][kC / 16];
+    uint32_t ks;
+    uint32_t vw[8][kV / 4];
+    u32x2 vs;
+    bool v_ok = false;
+    auto load_k = [&](int t) {
+        t += 2 * n;
+        int page = entry(t);
+        page = (uint32_t)page < (uint32_t)a.num_pages ? page : 0;
+        const int off = t & page_mask;
+        const int64_t ph = (int64_t)page * a.kv_heads + h;
+        const uint8_t* p = a.k_codes + ((ph << a.page_shift) + off) * D + g * kC;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int c = 0; c < kC / 16; ++c) kw[i][c] = *reinterpret_cast<const u32x4*>(p + i * D + c * 16);
+        ks = *reinterpret_cast<const uint16_t*>(a.k_scales + ((ph * (D / 32) + g * kC / 32) << a.page_shift) + off);
+    };
+    auto load_v = [&](int t) {
+        t += 8 * g;
+        int page = entry(t);
+        v_ok = (uint32_t)page < (uint32_t)a.num_pages;
+        page = v_ok ? page : 0;
+        const int off = t & page_mask;
+        const int64_t ph = (int64_t)page * a.kv_heads + h;
+        const uint8_t* p = a.v_codes + ((ph << a.page_shift) + off) * D + n * kV;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (kV == 8) {
+                const u32x2 w = *reinterpret_cast<const u32x2*>(p + i * D);
+                vw[i][0] = w[0], vw[i][kV / 4 - 1] = w[1];
+            } else {
+                vw[i][0] = *reinterpret_cast<const uint32_t*>(p + i * D);
+            }
+        }
+        vs = *reinterpret_cast<const u32x2*>(a.v_scales + ((ph * (D / 32) + n * kV / 32) << a.page_shift) + off);
+    };
+    int t = t_begin + wave * 32;
+    if (t < t_end) {
+        load_k(t);
+        load_v(t);
+    }
 
     bf16x8 qf[NT][kU];
     int row_lo[NT], row_hi[NT];                             // tokens [lo, hi) are visible to this lane's row
@@ -126,46 +177,6 @@ attend_few(const AttnArgs a) {
     const int all_hi = a.causal ? min(s.len, s.first_pos + 1) : s.len;
     const int all_lo = a.window ? max(0, s.first_pos + s.n - a.window) : 0;
 
-    const int32_t* table = a.page_table + (size_t)b * a.table_width;
-    const int page_mask = (1 << a.page_shift) - 1;
-    const int last_page = max(0, (s.len - 1) >> a.page_shift);      // entries behind it are not read
-    auto entry = [&](int t) { return table[min(t >> a.page_shift, last_page)]; };
-    const int k_group = 16 * (n >> 2), v_group = 16 * g;    // offset of the lane's 16 tokens in a block
-
-    u32x4 kw[4][kC / 16];
-    uint32_t ks;
-    uint32_t vw[16][kV / 4];
-    u32x4 vs;
-    bool v_ok = false;
-    auto load_k = [&](int t, int page) {
-        page = (uint32_t)page < (uint32_t)a.num_pages ? page : 0;
-        const int off = (t + 4 * n) & page_mask;
-        const int64_t ph = (int64_t)page * a.kv_heads + h;
-        const uint8_t* p = a.k_codes + ((ph << a.page_shift) + off) * D + g * kC;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int c = 0; c < kC / 16; ++c) kw[i][c] = *reinterpret_cast<const u32x4*>(p + i * D + c * 16);
-        ks = *reinterpret_cast<const uint32_t*>(a.k_scales + ((ph * (D / 32) + g * kC / 32) << a.page_shift) + off);
-    };
-    auto load_v = [&](int t, int page) {
-        v_ok = (uint32_t)page < (uint32_t)a.num_pages;
-        page = v_ok ? page : 0;
-        const int off = (t + v_group) & page_mask;
-        const int64_t ph = (int64_t)page * a.kv_heads + h;
-        const uint8_t* p = a.v_codes + ((ph << a.page_shift) + off) * D + n * kV;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            if constexpr (kV == 8) {
-                const u32x2 w = *reinterpret_cast<const u32x2*>(p + i * D);
-                vw[i][0] = w[0], vw[i][kV / 4 - 1] = w[1];
-            } else {
-                vw[i][0] = *reinterpret_cast<const uint32_t*>(p + i * D);
-            }
-        }
-        vs = *reinterpret_cast<const u32x4*>(a.v_scales + ((ph * (D / 32) + n * kV / 32) << a.page_shift) + off);
-    };
-
     float m[NT], l[NT];
     f32x4 o[NT][kV];
 #pragma unroll
@@ -174,19 +185,11 @@ attend_few(const AttnArgs a) {
 #pragma unroll
         for (int j = 0; j < kV; ++j) o[x][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    int t = t_begin + wave * 64;
-    int kp = 0, vp = 0;
-    if (t < t_end) {
-        const int k0 = entry(t + k_group), v0 = entry(t + v_group);
-        kp = entry(t + 256 + k_group), vp = entry(t + 256 + v_group);
-        load_k(t, k0);
-        load_v(t, v0);
-    }
-    for (; t < t_end; t += 256) {
-        const bool more = t + 256 < t_end;
-        f32x4 sc[NT][4];
+    for (; t < t_end; t += 128) {
+        const bool more = t + 128 < t_end;
+        f32x4 sc[NT][2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 2; ++i) {
             const float kscale = scale_byte(ks, i);
             bf16x8 kf[kU];
 #pragma unroll
@@ -201,23 +204,23 @@ attend_few(const AttnArgs a) {
                 for (int u = 0; u < kU; ++u) sc[x][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[u], qf[x][u], sc[x][i], 0, 0, 0);
             }
         }
-        if (more) load_k(t + 256, kp);
-        const bool whole = t >= all_lo && t + 64 <= all_hi && __ballot(!v_ok) == 0;
+        if (more) load_k(t + 128);
+        const bool whole = t >= all_lo && t + 32 <= all_hi && __ballot(!v_ok) == 0;
         if (!whole) {
             // masked places may hold anything (unwritten codes, pages that are gone): their scores are replaced, their
             // values and scales become zeros and ones, so that a weight of zero stays a product of zero
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int tok = t + v_group + 4 * r + i;
+                    const int tok = t + 8 * g + 2 * r + i;
 #pragma unroll
                     for (int x = 0; x < NT; ++x)
                         if (!(v_ok && tok >= row_lo[x] && tok < row_hi[x])) sc[x][i][r] = -INFINITY;
                 }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int tok = t + v_group + i;
+            for (int i = 0; i < 8; ++i) {
+                const int tok = t + 8 * g + i;
                 if (!(v_ok && tok >= s.t_lo && tok < s.len)) {
 #pragma unroll
                     for (int c = 0; c < kV / 4; ++c) vw[i][c] = 0u;
@@ -225,64 +228,57 @@ attend_few(const AttnArgs a) {
                 }
             }
         }
-        bf16x8 ph[NT][2], pl[NT][2];                        // the weights as two bf16 terms
+        bf16x8 ph[NT], pl[NT];                              // the weights as two bf16 terms
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
             float mx = sc[x][0][0];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) mx = __builtin_fmaxf(mx, sc[x][i][r]);
             mx = __builtin_fmaxf(mx, shuffle_xor(mx, 16));
-            mx = __builtin_fmaxf(mx, shuffle_xor(mx, 32));
-            const float m2 = __builtin_fmaxf(m[x], mx * a.scale);
-            const float ref = m2 == -INFINITY ? 0.0f : m2;
-            if (__ballot(m2 > m[x])) {
-                const float f = exp2_(m[x] - ref);
+            mx = __builtin_fmaxf(mx, shuffle_xor(mx, 32)) * a.scale;
+            if (__ballot(mx > m[x] + 8.0f)) {
+                const float m2 = __builtin_fmaxf(m[x], mx);
+                const float f = m2 == -INFINITY ? 0.0f : exp2_(m[x] - m2);
                 l[x] *= f;
 #pragma unroll
                 for (int j = 0; j < kV; ++j) o[x][j] *= f;
+                m[x] = m2;
             }
-            m[x] = m2;
+            const float ref = m[x] == -INFINITY ? 0.0f : m[x];
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float p = exp2_(__builtin_fmaf(sc[x][e & 3][2 * u + (e >> 2)], a.scale, -ref));
-                    l[x] += p;
-                    ph[x][u][e] = (__bf16)p;
-                    pl[x][u][e] = (__bf16)(p - (float)ph[x][u][e]);
-                }
+            for (int e = 0; e < 8; ++e) {
+                const float p = exp2_(__builtin_fmaf(sc[x][e & 1][e >> 1], a.scale, -ref));
+                l[x] += p;
+                ph[x][e] = (__bf16)p;
+                pl[x][e] = (__bf16)(p - (float)ph[x][e]);
+            }
         }
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int c = 0; c < kV / 4; ++c) {                  // four channels of eight tokens
+            uint32_t f[4][4];                               // [channel][token pair]
 #pragma unroll
-            for (int c = 0; c < kV / 4; ++c) {              // four channels of eight tokens
-                uint32_t f[4][4];                           // [channel][token pair]
+            for (int e = 0; e < 4; ++e) {
+                const int i0 = 2 * e, i1 = i0 + 1;
+                const float s0 = scale_byte(vs[i0 / 4], i0 & 3), s1 = scale_byte(vs[i1 / 4], i1 & 3);
+                const uint32_t a0 = cvt_lo(vw[i0][c], s0), b0 = cvt_lo(vw[i1][c], s1);
+                const uint32_t a1 = cvt_hi(vw[i0][c], s0), b1 = cvt_hi(vw[i1][c], s1);
+                f[0][e] = low_halves(a0, b0), f[1][e] = high_halves(a0, b0);
+                f[2][e] = low_halves(a1, b1), f[3][e] = high_halves(a1, b1);
+            }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i0 = 8 * u + 2 * e, i1 = i0 + 1;
-                    const float s0 = scale_byte(vs[i0 / 4], i0 & 3), s1 = scale_byte(vs[i1 / 4], i1 & 3);
-                    const uint32_t a0 = cvt_lo(vw[i0][c], s0), b0 = cvt_lo(vw[i1][c], s1);
-                    const uint32_t a1 = cvt_hi(vw[i0][c], s0), b1 = cvt_hi(vw[i1][c], s1);
-                    f[0][e] = low_halves(a0, b0), f[1][e] = high_halves(a0, b0);
-                    f[2][e] = low_halves(a1, b1), f[3][e] = high_halves(a1, b1);
-                }
+            for (int j = 0; j < 4; ++j) {
+                const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{f[j][0], f[j][1], f[j][2], f[j][3]});
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{f[j][0], f[j][1], f[j][2], f[j][3]});
-#pragma unroll
-                    for (int x = 0; x < NT; ++x) {
-                        f32x4& acc = o[x][4 * c + j];
-                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl[x][u], acc, 0, 0, 0);
-                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph[x][u], acc, 0, 0, 0);
-                    }
+                for (int x = 0; x < NT; ++x) {
+                    f32x4& acc = o[x][4 * c + j];
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl[x], acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph[x], acc, 0, 0, 0);
                 }
             }
-        if (more) {
-            load_v(t + 256, vp);
-            if (t + 512 < t_end) kp = entry(t + 512 + k_group), vp = entry(t + 512 + v_group);
         }
+        if (more) load_v(t + 128);
     }
 
     // join the waves: element r of tile j is channel (4g + r) D/16 + j of row n
@@ -335,38 +331,49 @@ attend_few(const AttnArgs a) {
     }
 }
 
-// Joins the parts of a row, in part order, by one wave; `at` is the row's first part.
-template <int D>
+// Joins the parts of a row: W waves take the parts in turn, eight in flight each, and are added in wave order; `at` is the
+// row's first part.  Every wave of the workgroup takes part.
+template <int D, int W>
 __device__ __forceinline__ void join_row(const AttnArgs& a, const float* part_o, const float* part_ml, size_t at, int parts,
                                          size_t row, int head) {
-    const int lane = threadIdx.x & 63;
+    __shared__ float s_v[W][D], s_sum[W];
+    const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     float top = -INFINITY;
     for (int p = lane; p < parts; p += 64) top = __builtin_fmaxf(top, part_ml[2 * (at + p)]);
 #pragma unroll
     for (int d = 32; d; d >>= 1) top = __builtin_fmaxf(top, shuffle_xor(top, d));
     const float ref = top == -INFINITY ? 0.0f : top;
     float sum = 0.0f, v[D / 64] = {};
-    for (int p0 = 0; p0 < parts; p0 += 64) {
-        const int p = p0 + lane;
-        const float f = p < parts ? exp2_(part_ml[2 * (at + p)] - ref) : 0.0f;
-        sum += p < parts ? f * part_ml[2 * (at + p) + 1] : 0.0f;
-        const int count = min(64, parts - p0);
-        for (int j0 = 0; j0 < count; j0 += 8) {             // eight loads in flight; past the end: the last part, weight 0
-            float x[8][D / 64];
+    for (int p0 = wave; p0 < parts; p0 += 8 * W) {          // parts p0, p0 + W, .. p0 + 7 W; past the end: the last one, weight 0
+        float x[8][D / 64], m[8], l[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < 8; ++j) {
+            const size_t p = at + min(p0 + W * j, parts - 1);
+            m[j] = part_ml[2 * p], l[j] = part_ml[2 * p + 1];
 #pragma unroll
-                for (int c = 0; c < D / 64; ++c) x[j][c] = part_o[(at + p0 + min(j0 + j, count - 1)) * D + lane * (D / 64) + c];
+            for (int c = 0; c < D / 64; ++c) x[j][c] = part_o[p * D + lane * (D / 64) + c];
+        }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float fj = j0 + j < count ? __shfl(f, j0 + j) : 0.0f;
+        for (int j = 0; j < 8; ++j) {
+            const float f = p0 + W * j < parts ? exp2_(m[j] - ref) : 0.0f;
+            sum = __builtin_fmaf(f, l[j], sum);
 #pragma unroll
-                for (int c = 0; c < D / 64; ++c) v[c] = __builtin_fmaf(fj, x[j][c], v[c]);
-            }
+            for (int c = 0; c < D / 64; ++c) v[c] = __builtin_fmaf(f, x[j][c], v[c]);
         }
     }
+    if constexpr (W > 1) {
 #pragma unroll
-    for (int d = 32; d; d >>= 1) sum += shuffle_xor(sum, d);
+        for (int c = 0; c < D / 64; ++c) s_v[wave][lane * (D / 64) + c] = v[c];
+        if (lane == 0) s_sum[wave] = sum;
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int w = 1; w < W; ++w) {
+            sum += s_sum[w];
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) v[c] += s_v[w][lane * (D / 64) + c];
+        }
+    }
     const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
     __bf16* o = reinterpret_cast<__bf16*>(a.out + row * a.ldo + (size_t)head * D + lane * (D / 64));
 #pragma unroll
@@ -374,20 +381,18 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const float* part_o,
     if (a.lse && lane == 0) a.lse[row * a.q_heads + head] = sum > 0.0f ? (top + __log2f(sum)) * 0.69314718055994531f : -INFINITY;
 }
 
-// One wave per row of a (sequence, key head) of few rows.
+// One workgroup per row of a (sequence, key head) of few rows.
 template <int D>
 __global__ void __launch_bounds__(256)
 join_few(const AttnArgs a) {
-    const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t bh = unit / a.part_rows;
+    const unsigned unit = blockIdx.x, bh = unit / (unsigned)a.part_rows;
     const int r = (int)(unit - bh * a.part_rows), h = (int)(bh % a.kv_heads), b = (int)(bh / a.kv_heads);
-    if (b >= a.batch) return;
     const Seq s = sequence(a, b);
     const int rows = s.n * a.group;
     if (r >= rows || rows > a.few_rows) return;
     const int parts = live_parts(s, a.few_len);
     if (parts == 1) return;
-    join_row<D>(a, a.part_o, a.part_ml, (size_t)unit * a.max_parts, parts, (size_t)s.begin + r / a.group, h * a.group + r % a.group);
+    join_row<D, 4>(a, a.part_o, a.part_ml, (size_t)unit * a.max_parts, parts, (size_t)s.begin + r / a.group, h * a.group + r % a.group);
 }
 
 // Many query rows to a key head (prompts, chunks of prompts): bound by the matrix pipe, the exponentials and LDS reads.
@@ -673,14 +678,12 @@ attend_many(const AttnArgs a) {
     }
 }
 
-// One wave per (row of q, query head) of sequences with many rows.
+// One wave per (row of q, query head) of sequences with many rows: there are many of them, of few parts.
 template <int D>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(64)
 join_many(const AttnArgs a) {
     const int lane = threadIdx.x & 63;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row = (int)(unit / a.q_heads), head = (int)(unit % a.q_heads);
-    if (row >= a.total_q) return;
+    const int row = blockIdx.x / a.q_heads, head = blockIdx.x % a.q_heads;
     int b = -1;                                             // the row's sequence: lanes look at 64 of them at a time
     for (int b0 = 0; b0 < a.batch && b < 0; b0 += 64) {
         bool mine = false;
@@ -698,7 +701,7 @@ join_many(const AttnArgs a) {
     const TokenRange t = tile_tokens(a, s, (i * a.group + head % a.group) / kManyRows);
     const int parts = range_parts(t, a.many_len);
     if (parts == 1) return;
-    join_row<D>(a, a.many_o, a.many_ml, ((size_t)row * a.q_heads + head) * a.many_parts, parts, (size_t)row, head);
+    join_row<D, 1>(a, a.many_o, a.many_ml, ((size_t)row * a.q_heads + head) * a.many_parts, parts, (size_t)row, head);
 }
 
 }  // namespace
@@ -763,11 +766,11 @@ hipError_t launch_attention(const AttnArgs& a, const Plan& p, int dev, hipStream
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     if (p.max_parts > 1) {
-        join_few<D><<<((unsigned)a.batch * a.kv_heads * p.part_rows + 3) / 4, 256, 0, stream>>>(a);
+        join_few<D><<<(unsigned)a.batch * a.kv_heads * p.part_rows, 256, 0, stream>>>(a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     if (p.many_parts > 1) {
-        join_many<D><<<((unsigned)a.total_q * a.q_heads + 3) / 4, 256, 0, stream>>>(a);
+        join_many<D><<<(unsigned)a.total_q * a.q_heads, 64, 0, stream>>>(a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     return hipSuccess;
