@@ -409,7 +409,7 @@ constexpr int kManyRows = 256;
 
 template <int D>
 __device__ __forceinline__ int k_place(int row, int chunk) { return D == 128 ? chunk ^ (row & 15) : chunk ^ ((row >> 1) & 7); }
-__device__ __forceinline__ int v_place(int row, int chunk) { return chunk ^ (((row >> 1) ^ (row >> 4)) & 7); }
+__device__ __forceinline__ int v_place(int row, int chunk) { return chunk ^ (((row >> 1) ^ (row >> 4 & 1)) & 7); }
 
 template <int D>
 constexpr int many_lds() { return 4 * 64 * D * 2 + 2 * 16; }   // two buffers of keys and values, which 16-token groups exist
@@ -461,6 +461,8 @@ __device__ __forceinline__ void find_tile(const AttnArgs& a, int x, int* b, int*
     }
 }
 
+constexpr int kDeep = 6;                                    // operands that are read ahead of their product
+
 template <int D>
 __global__ void __launch_bounds__(512, 2)
 attend_many(const AttnArgs a) {
@@ -475,6 +477,7 @@ attend_many(const AttnArgs a) {
     const int part = xp % a.many_parts;
     int b, tile;
     find_tile(a, xp / a.many_parts, &b, &tile);
+    b = __builtin_amdgcn_readfirstlane(b), tile = __builtin_amdgcn_readfirstlane(tile);
     if (b < 0) return;
     const Seq s = sequence(a, b);
     const int rows = s.n * a.group, row0 = tile * kManyRows;
@@ -504,53 +507,62 @@ attend_many(const AttnArgs a) {
     const int some_hi = !wave_live ? 0 : a.causal ? min(s.len, wp1 + 1) : s.len, some_lo = a.window ? max(0, wp0 - a.window + 1) : 0;
     const int all_hi = a.causal ? min(s.len, wp0 + 1) : s.len, all_lo = a.window ? max(0, wp1 - a.window + 1) : 0;
 
-    // staging: a thread converts 16 channels of a key and a 4 x 4 tile of values (D = 64: one or the other)
+    // staging: a thread has a piece of 16 channels of a key and a 4 x 4 piece of values (D = 64: one or the other).  A wave's 8
+    // (16) tokens lie in one page: pages and addresses are scalars, what a lane adds to them stays the same
     const int32_t* table = a.page_table + (size_t)b * a.table_width;
     const int page_mask = (1 << a.page_shift) - 1, last_page = max(0, (s.len - 1) >> a.page_shift);
-    constexpr int kKc = D / 16;                             // 16-channel chunks of a key
-    const int id = D == 128 ? tid : tid & 255;
-    const bool do_k = D == 128 || tid < 256, do_v = D == 128 || tid >= 256;
-    const int k_tok = id / kKc, k_c = id % kKc;
-    const int v_quad = id / (D / 4), v_c = id % (D / 4);    // tokens 4 v_quad .. + 3, channels 4 v_c .. + 3
-    auto entry = [&](int t) { return table[min(t >> a.page_shift, last_page)]; };
+    const bool do_k = D == 128 || wave < 4, do_v = D == 128 || wave >= 4;
+    constexpr int kKc = D / 16, kVc = D / 4;                // pieces of a key, of four values' tokens
+    const int tok0 = D == 128 ? wave * 8 : (wave & 3) * 16; // the wave's first token of the tile
+    const int k_tok = lane / kKc, k_c = lane % kKc;         // from there: this lane's key, its 16 channels
+    const int v_tok = lane / kVc * 4, v_c = lane % kVc;     // tokens v_tok .. + 3, channels 4 v_c .. + 3
+    const uint32_t k_lane = lane * 16, ks_lane = ((uint32_t)(k_c / 2) << a.page_shift) + k_tok;
+    const uint32_t v_lane = v_tok * D + v_c * 4, vs_lane = ((uint32_t)(v_c / 8) << a.page_shift) + v_tok;
+    auto entry = [&](int t) {                               // page of the wave's tokens of the tile that starts with t
+        return __builtin_amdgcn_readfirstlane(table[min((t + tok0) >> a.page_shift, last_page)]);
+    };
     u32x4 kw = {};
     uint32_t kscale = 0, vw[4] = {}, vscale = 0;
-    bool k_ok = false, v_ok = false;
-    auto request = [&](int t, int kp, int vp) {
+    bool there = false;
+    auto request = [&](int t, int page) {
+        there = (uint32_t)page < (uint32_t)a.num_pages;
+        const int64_t ph = (int64_t)(there ? page : 0) * a.kv_heads + h;
+        const int off = (t + tok0) & page_mask;
+        const int64_t codes = ((ph << a.page_shift) + off) * D, scales = ((ph * (D / 32)) << a.page_shift) + off;
         if (do_k) {
-            k_ok = (uint32_t)kp < (uint32_t)a.num_pages;
-            const int64_t ph = (int64_t)(k_ok ? kp : 0) * a.kv_heads + h;
-            const int off = (t + k_tok) & page_mask;
-            kw = *reinterpret_cast<const u32x4*>(a.k_codes + ((ph << a.page_shift) + off) * D + k_c * 16);
-            kscale = a.k_scales[((ph * (D / 32) + k_c / 2) << a.page_shift) + off];
+            kw = *reinterpret_cast<const u32x4*>(a.k_codes + codes + k_lane);
+            kscale = a.k_scales[scales + ks_lane];
         }
         if (do_v) {
-            v_ok = (uint32_t)vp < (uint32_t)a.num_pages;
-            const int64_t ph = (int64_t)(v_ok ? vp : 0) * a.kv_heads + h;
-            const int off = (t + 4 * v_quad) & page_mask;
-            const uint8_t* p = a.v_codes + ((ph << a.page_shift) + off) * D + v_c * 4;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) vw[e] = *reinterpret_cast<const uint32_t*>(p + e * D);
-            vscale = *reinterpret_cast<const uint32_t*>(a.v_scales + ((ph * (D / 32) + v_c / 8) << a.page_shift) + off);
+            for (int e = 0; e < 4; ++e) vw[e] = *reinterpret_cast<const uint32_t*>(a.v_codes + codes + v_lane + e * D);
+            vscale = *reinterpret_cast<const uint32_t*>(a.v_scales + scales + vs_lane);
         }
     };
+    uint32_t k_to[2], v_to[4];                              // where the piece goes in a buffer
+#pragma unroll
+    for (int e = 0; e < 2; ++e) k_to[e] = (tok0 + k_tok) * (D * 2) + k_place<D>(tok0 + k_tok, 2 * k_c + e) * 16;
+    {
+        const int quad = (tok0 + v_tok) / 4, chunk = 2 * (quad >> 2) + (quad & 1), half = (quad >> 1) & 1;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v_to[c] = (4 * v_c + c) * 128 + v_place(4 * v_c + c, chunk) * 16 + half * 8;
+    }
     auto stage = [&](int t, int buf) {                      // the requested tile (first token t) into LDS
         if (do_k) {
             const float sc = scale_operand(kscale);
-            uint8_t* row_k = s_k + buf * kHalf + k_tok * (D * 2);
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                *reinterpret_cast<u32x4*>(row_k + k_place<D>(k_tok, 2 * k_c + e) * 16) =
+                *reinterpret_cast<u32x4*>(s_k + buf * kHalf + k_to[e]) =
                     u32x4{cvt_lo(kw[2 * e], sc), cvt_hi(kw[2 * e], sc), cvt_lo(kw[2 * e + 1], sc), cvt_hi(kw[2 * e + 1], sc)};
-            if (k_c == 0 && (k_tok & 15) == 0) s_ok[buf * 4 + k_tok / 16] = k_ok;
+            if (k_c == 0 && ((tok0 + k_tok) & 15) == 0) s_ok[buf * 4 + (tok0 + k_tok) / 16] = there;
         }
         if (do_v) {
             // places that nobody sees may hold anything: a weight of zero must stay a product of zero
-            if (!v_ok || t < range.lo || t + 64 > s.len) {
+            if (!there || t < range.lo || t + 64 > s.len) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int tok = t + 4 * v_quad + e;
-                    if (!(v_ok && tok >= range.lo && tok < s.len)) {
+                    const int tok = t + tok0 + v_tok + e;
+                    if (!(there && tok >= range.lo && tok < s.len)) {
                         vw[e] = 0u;
                         vscale = (vscale & ~(0xFFu << (8 * e))) | (127u << (8 * e));
                     }
@@ -562,13 +574,11 @@ attend_many(const AttnArgs a) {
                 const float sc = scale_byte(vscale, e);
                 lo[e] = cvt_lo(vw[e], sc), hi[e] = cvt_hi(vw[e], sc);
             }
-            const int chunk = 2 * (v_quad >> 2) + (v_quad & 1), half = (v_quad >> 1) & 1;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const uint32_t* w = c < 2 ? lo : hi;
-                const u32x2 q = c & 1 ? u32x2{high_halves(w[0], w[1]), high_halves(w[2], w[3])} : u32x2{low_halves(w[0], w[1]), low_halves(w[2], w[3])};
-                const int ch = 4 * v_c + c;
-                *reinterpret_cast<u32x2*>(s_v + buf * kHalf + ch * 128 + v_place(ch, chunk) * 16 + half * 8) = q;
+                *reinterpret_cast<u32x2*>(s_v + buf * kHalf + v_to[c]) =
+                    c & 1 ? u32x2{high_halves(w[0], w[1]), high_halves(w[2], w[3])} : u32x2{low_halves(w[0], w[1]), low_halves(w[2], w[3])};
             }
         }
     };
@@ -578,10 +588,10 @@ attend_many(const AttnArgs a) {
 #pragma unroll
     for (int c = 0; c < kCb; ++c) o[c] = v16f{};
 
-    int kp = 0, vp = 0;
+    int page = 0;                                           // of the tile after the one that is requested next
     if (t_begin < t_end) {
-        request(t_begin, entry(t_begin + k_tok), entry(t_begin + 4 * v_quad));
-        kp = entry(t_begin + 64 + k_tok), vp = entry(t_begin + 64 + 4 * v_quad);
+        request(t_begin, entry(t_begin));
+        page = entry(t_begin + 64);
         stage(t_begin, 0);
     }
     __syncthreads();
@@ -589,30 +599,42 @@ attend_many(const AttnArgs a) {
     for (int t = t_begin; t < t_end; t += 64, buf ^= 1) {
         const bool more = t + 64 < t_end;
         if (more) {
-            request(t + 64, kp, vp);
-            kp = entry(t + 128 + k_tok), vp = entry(t + 128 + 4 * v_quad);
+            request(t + 64, page);
+            page = entry(t + 128);
         }
         if (t < some_hi && t + 64 > some_lo) {              // wave-uniform
-            v16f sc[2];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                sc[x] = v16f{};
-                const uint8_t* row_k = s_k + buf * kHalf + (32 * x + n) * (D * 2);
-#pragma unroll
-                for (int u = 0; u < kU; ++u) {
-                    const bf16x8 kf = *reinterpret_cast<const bf16x8*>(row_k + k_place<D>(32 * x + n, 2 * u + hh) * 16);
-                    sc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[u], sc[x], 0, 0, 0);
-                }
-            }
+            // chunk 2 j + h of a lane's row is at (the row's address with chunk h) ^ 32 j; opaque, or every address of a tile
+            // would be kept in a register of its own
+            uint32_t at_v = (uint32_t)(n * 128 + v_place(n, hh) * 16), at_k = (uint32_t)(n * (D * 2) + k_place<D>(n, hh) * 16);
+            asm volatile("" : "+v"(at_v), "+v"(at_k));
             const uint32_t ok = *reinterpret_cast<const uint32_t*>(s_ok + buf * 4);
+            // operand i of the keys: tile half i % 2, step i / 2; of the values: channel block i % kCb, step i / kCb (neighbouring
+            // products go to different sums).  They are read kDeep products ahead, the first values before the softmax
+            auto read_k = [&](int i) { return *reinterpret_cast<const bf16x8*>(s_k + buf * kHalf + (at_k ^ (uint32_t)(i / 2 * 32)) + i % 2 * 32 * (D * 2)); };
+            auto read_v = [&](int i) { return *reinterpret_cast<const bf16x8*>(s_v + buf * kHalf + (at_v ^ (uint32_t)(i / kCb * 32)) + i % kCb * 32 * 128); };
+            v16f sc[2];
+            bf16x8 ring[kDeep];
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) ring[i] = read_k(i);
+#pragma unroll
+            for (int i = 0; i < 2 * kU; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                sc[i % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[i % kDeep], qf[i / 2], i < 2 ? v16f{} : sc[i % 2], 0, 0, 0);
+                if (i + kDeep < 2 * kU) ring[i % kDeep] = read_k(i + kDeep);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < kDeep; ++i) ring[i] = read_v(i);
             if (t < all_lo || t + 64 > all_hi || ok != 0x01010101u) {
+                // (in integer arithmetic: conditions would take two scalar registers for each element)
+                const int first = row_lo - t - 4 * hh, last = row_hi - 1 - t - 4 * hh;
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const int at = 32 * x + 8 * (e >> 2) + 4 * hh + (e & 3), tok = t + at;
-                        const bool there = (ok >> (8 * (2 * x + (e >> 3)))) & 1u;
-                        if (!(there && tok >= row_lo && tok < row_hi)) sc[x][e] = -INFINITY;
+                        const int at = 32 * x + 8 * (e >> 2) + (e & 3);
+                        const int hide = ((at - first) | (last - at) | ((int)((ok >> (8 * (2 * x + (e >> 3)))) & 1u) - 1)) >> 31;
+                        sc[x][e] = __uint_as_float((__float_as_uint(sc[x][e]) & ~(uint32_t)hide) | (0xFF800000u & (uint32_t)hide));
                     }
             }
             float mx = sc[0][0];
@@ -620,8 +642,8 @@ attend_many(const AttnArgs a) {
             for (int x = 0; x < 2; ++x)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) mx = __builtin_fmaxf(mx, sc[x][e]);
-            mx = __builtin_fmaxf(mx, shuffle_xor(mx, 32)) * a.scale;
-            if (__ballot(mx > m + 8.0f)) {
+            if (__ballot(mx * a.scale > m + 8.0f)) {        // (the two halves of a row are compared only then)
+                mx = __builtin_fmaxf(mx, shuffle_xor(mx, 32)) * a.scale;
                 const float m2 = __builtin_fmaxf(m, mx);
                 const float f = m2 == -INFINITY ? 0.0f : exp2_(m - m2);
                 l *= f;
@@ -640,14 +662,12 @@ attend_many(const AttnArgs a) {
                     pf[2 * x + (e >> 3)][e & 7] = (__bf16)p;
                 }
 #pragma unroll
-            for (int c = 0; c < kCb; ++c) {
-                const uint8_t* row_v = s_v + buf * kHalf + (32 * c + n) * 128;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const bf16x8 vf = *reinterpret_cast<const bf16x8*>(row_v + v_place(32 * c + n, 2 * j + hh) * 16);
-                    o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[j], o[c], 0, 0, 0);
-                }
+            for (int i = 0; i < 4 * kCb; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                o[i % kCb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[i % kDeep], pf[i / kCb], o[i % kCb], 0, 0, 0);
+                if (i + kDeep < 4 * kCb) ring[i % kDeep] = read_v(i + kDeep);
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
         if (more) stage(t + 64, buf ^ 1);
         __syncthreads();
@@ -714,35 +734,39 @@ struct Plan {
     bool few, many;                                         // which kernels run
 };
 
-// Part length of attend_few: enough workgroups for two to a compute unit (four where a sequence is long), at least 256
-// tokens (a block for each wave) and at most 1024, so that the longest of ragged sequences does not outlast the others.
-// attend_many cuts the tokens only where its row tiles are fewer than the compute units.
-Plan plan(int group, int kv_heads, int batch, int total_q, int max_q, int max_kv, int compute_units) {
+// Part length of attend_few: enough workgroups for four to a compute unit where there are tokens for it, at least 256
+// tokens (two blocks for each wave) and at most 1024, so that the longest of ragged sequences does not outlast the others
+// (64 sequences of up to 8192 tokens: parts of 512 and 1024 tokens 35 us, of 256 45 us; 4 of up to 131072: 74 us, 80 us).
+// attend_many cuts the tokens only where its row tiles are fewer than the compute units, into as many parts as make about
+// one workgroup to each.  A window bounds the tokens that matter: of a sequence of few rows, of a tile of many.
+Plan plan(int group, int kv_heads, int batch, int total_q, int max_q, int max_kv, int window, int compute_units) {
     Plan p = {};
     const int64_t rows = (int64_t)max_q * group;
     p.many = rows > 32;
     p.few = !p.many || batch > 1;
     p.few_rows = !p.few ? 0 : p.many ? 16 : rows > 16 ? 32 : 16;
     p.part_rows = (int)(rows < p.few_rows ? rows : p.few_rows);
-    const int64_t tokens = (int64_t)batch * kv_heads * max_kv;
-    int64_t len = (tokens / (4 * compute_units) + 255) & ~int64_t(255);
-    if (len < 256) len = 256;
-    if (len > 1024) len = 1024;
-    p.few_len = (int)len;
-    p.max_parts = p.few ? (int)((max_kv + 63 + len - 1) / len) : 1;
-    if (p.max_parts < 1) p.max_parts = 1;
+    auto span = [&](int queries) { return window > 0 && window < max_kv - queries ? window + queries : max_kv; };
+    p.max_parts = 1, p.few_len = 256;
+    if (p.few) {
+        const int64_t tokens = span(p.few_rows);
+        int64_t len = (batch * kv_heads * tokens / (4 * compute_units) + 255) & ~int64_t(255);
+        if (len < 256) len = 256;
+        if (len > 1024) len = 1024;
+        p.few_len = (int)len;
+        p.max_parts = (int)((tokens + 63 + len - 1) / len);
+        if (p.max_parts < 1) p.max_parts = 1;
+    }
     p.many_parts = 1, p.many_len = 1 << 30;
     if (p.many) {
         p.many_tiles = (int)((int64_t)total_q * group / kManyRows + batch);
         const int64_t groups = (int64_t)((int64_t)total_q * group / kManyRows + 1) * kv_heads;
-        if (groups < compute_units) {
-            int64_t n = 2 * compute_units / groups;
-            const int64_t most = (max_kv + 511) / 512;      // at least 512 tokens to a part
-            if (n > most) n = most;
-            if (n > 1) {
-                p.many_len = (int)(((max_kv + n - 1) / n + 63) & ~int64_t(63));
-                p.many_parts = (max_kv + 63 + p.many_len - 1) / p.many_len;
-            }
+        const int64_t tokens = span(kManyRows / group + 1);
+        int64_t n = compute_units / groups;
+        if (n > (tokens + 511) / 512) n = (tokens + 511) / 512;     // at least 512 tokens to a part
+        if (n > 1) {
+            p.many_len = (int)(((tokens + n - 1) / n + 63) & ~int64_t(63));
+            p.many_parts = (int)((tokens + 63 + p.many_len - 1) / p.many_len);
         }
     }
     return p;
@@ -778,10 +802,17 @@ hipError_t launch_attention(const AttnArgs& a, const Plan& p, int dev, hipStream
 
 }  // namespace
 
+namespace {
+
+size_t part_bytes(const Plan& p, const batq_paged_cache& c, int q_heads, int batch, int total_q) {
+    return (size_t)(few_units(p, batch, c.kv_heads) + many_units(p, total_q, q_heads)) * (c.head_dim + 2) * 4;
+}
+
+}  // namespace
+
 size_t paged_attention_workspace_bytes(const batq_paged_cache& c, int q_heads, int batch, int total_q, int max_q, int max_kv,
                                        int compute_units) {
-    const Plan p = plan(q_heads / c.kv_heads, c.kv_heads, batch, total_q, max_q, max_kv, compute_units);
-    return (size_t)(few_units(p, batch, c.kv_heads) + many_units(p, total_q, q_heads)) * (c.head_dim + 2) * 4;
+    return part_bytes(plan(q_heads / c.kv_heads, c.kv_heads, batch, total_q, max_q, max_kv, 0, compute_units), c, q_heads, batch, total_q);
 }
 
 hipError_t launch_paged_attention(const batq_paged_cache& c, const batq_paged_batch& b, const void* q, int64_t ldq,
@@ -791,7 +822,10 @@ hipError_t launch_paged_attention(const batq_paged_cache& c, const batq_paged_ba
     hipError_t e = hipGetDevice(&dev);
     const int cus = e == hipSuccess ? device_compute_units(dev, &e) : 0;
     if (e != hipSuccess) return e;
-    const Plan p = plan(q_heads / c.kv_heads, c.kv_heads, b.batch, b.total_q, b.max_q, b.max_kv, cus);
+    // a window's plan where it needs no more room than the plan without one, which is what the workspace is sized for
+    const Plan full = plan(q_heads / c.kv_heads, c.kv_heads, b.batch, b.total_q, b.max_q, b.max_kv, 0, cus);
+    Plan p = plan(q_heads / c.kv_heads, c.kv_heads, b.batch, b.total_q, b.max_q, b.max_kv, window, cus);
+    if (part_bytes(p, c, q_heads, b.batch, b.total_q) > part_bytes(full, c, q_heads, b.batch, b.total_q)) p = full;
     AttnArgs a = {};
     a.q = static_cast<const uint16_t*>(q), a.ldq = ldq, a.ldo = ldo, a.out = static_cast<uint16_t*>(out), a.lse = lse;
     a.k_codes = c.k_codes, a.k_scales = c.k_scales, a.v_codes = c.v_codes, a.v_scales = c.v_scales;
