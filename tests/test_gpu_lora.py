@@ -146,3 +146,61 @@ def test_lora_beside_the_projection_on_streams_and_in_graphs(B):
             g.replay()
         torch.cuda.synchronize()
         assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[2]), rep
+
+
+def test_sizes_at_the_edges(B):
+    """Widths of one column, ranks at the ends, rows of every tile remainder, many rows with many adapters mixed."""
+    import torch
+    for M, K, N, r, n, pattern in ((1, 32, 1, 128, 1, "one"), (15, 64, 63, 8, 15, "each"), (16, 64, 65, 56, 2, "mixed"), (512, 96, 40, 104, 9, "mixed"),
+                                   (600, 160, 130, 8, 40, "mixed"), (1025, 32, 257, 48, 3, "runs"), (2000, 512, 64, 16, 2, "none")):
+        rng = np.random.default_rng(M * 7 + N)
+        X, Xv, A, Av, Bm, Bv, base, basev, scales, index = problem(rng, M, K, N, r, n, "bf16", "f32", pattern)
+        out = B.batq_lora_add(X, A, Bm, dev(index), base, scales=dev(scales))
+        torch.cuda.synchronize()
+        check(out.cpu().numpy().astype(np.float64), Xv, Av, Bv, basev, scales, index, "f32")
+
+
+def test_garbage_in_the_workspace_and_beside_the_rows_does_not_show(B):
+    """NaN in the workspace, in rows of X behind M and in padding columns."""
+    import torch
+    rng = np.random.default_rng(8)
+    for M, pattern in ((20, "mixed"), (700, "mixed")):
+        X, Xv, A, Av, Bm, Bv, base, basev, scales, index = problem(rng, M, 96, 70, 24, 3, "bf16", "bf16", pattern)
+        wide = torch.full((M + 40, 96 + 32), float("nan"), dtype=torch.bfloat16, device="cuda")
+        wide[:M, :96] = X
+        ws = torch.full((B.batq_lora_workspace(M, 96, 70, 24, 3),), 0xFF, dtype=torch.uint8, device="cuda")
+        out = B.batq_lora_add(wide[:M, :96], A, Bm, dev(index), base, scales=dev(scales), workspace=ws)
+        torch.cuda.synchronize()
+        check(out.float().cpu().numpy().astype(np.float64), Xv, Av, Bv, basev, scales, index, "bf16")
+
+
+def test_two_calls_at_once(B):
+    import torch
+    rng = np.random.default_rng(9)
+    probs = [problem(rng, M, 512, 300, 16, 4, "bf16", "f32", "mixed") for M in (30, 700)]
+    want, ws, streams = [], [], [torch.cuda.Stream() for _ in probs]
+    for X, _, A, _, Bm, _, base, _, scales, index in probs:
+        want.append(B.batq_lora_add(X, A, Bm, dev(index), base, scales=dev(scales)))
+        ws.append(torch.empty(B.batq_lora_workspace(X.shape[0], 512, 300, 16, 4), dtype=torch.uint8, device="cuda"))
+    devs = [(dev(p[9]), dev(p[8])) for p in probs]
+    outs = [torch.zeros_like(w) for w in want]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (X, _, A, _, Bm, _, base, _, _, _), (index, scales), w, out, s in zip(probs, devs, ws, outs, streams):
+            with torch.cuda.stream(s):
+                B.batq_lora_add(X, A, Bm, index, base, scales=scales, out=out, workspace=w)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(outs, want))
+
+
+def test_binding_refuses_what_does_not_fit(B):
+    import torch
+    X, A, Bm = torch.zeros((2, 64), device="cuda"), torch.zeros((1, 8, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((1, 40, 8), dtype=torch.bfloat16, device="cuda")
+    index, base = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros((2, 40), device="cuda")
+    B.batq_lora_add(X, A, Bm, index, base)
+    for bad in (dict(X=X.cpu()), dict(X=X[:, ::2]), dict(A=A.float()), dict(B=Bm[:, :, :4]), dict(index=index.long()), dict(base=base[:1]),
+                dict(base=base.t()), dict(out=base.bfloat16()), dict(scales=torch.zeros(2, device="cuda"))):
+        with pytest.raises(ValueError):
+            B.batq_lora_add(**{**dict(X=X, A=A, B=Bm, index=index, base=base), **bad})
+    with pytest.raises(B.BatqError):
+        B.batq_lora_add(X, A, Bm, index, base, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))

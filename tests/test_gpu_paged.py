@@ -464,6 +464,96 @@ def test_attention_is_repeatable_and_runs_on_a_side_stream_and_in_graphs(B):
         assert bool(torch.isfinite(junk).all())
 
 
+def test_attention_of_a_large_ragged_batch(B):
+    """More sequences than a wave has lanes: chunks and single tokens in any order, empty ones among them."""
+    rng = np.random.default_rng(14)
+    hq, hkv, D, page = 6, 2, 64, 16
+    n = 150
+    lens = rng.integers(0, 90, n)
+    qs = np.where(rng.random(n) < 0.2, rng.integers(0, 60, n), 1)
+    qs[[0, 70, 149]] = 0, 120, 95
+    lens[[70, 149]] = 300, 95
+    cache, (kv, vv), qd, q, cu, lens, table, T = attend_case(rng, B, lens, qs, hq, hkv, D, page, spare=1)
+    for window in (0, 40):
+        got, lse = run_attention(B, cache, qd, cu, lens, table, T, hq, window=window)
+        ref.assert_attention(got, lse, ref.attention(kv, vv, q, cu, lens, table, page, D ** -0.5, True, window, T))
+
+
+def test_attention_cut_into_parts_with_a_window(B):
+    """Windows that start and end inside parts, for single tokens and for chunks of long sequences."""
+    rng = np.random.default_rng(15)
+    for hq, hkv, D, page, lens, qs in ((4, 1, 128, 16, [5000, 900], [1, 2]), (2, 1, 64, 64, [4000], [200])):
+        cache, (kv, vv), qd, q, cu, lens, table, T = attend_case(rng, B, lens, qs, hq, hkv, D, page)
+        for window in (1, 255, 1000, 3777):
+            got, lse = run_attention(B, cache, qd, cu, lens, table, T, hq, window=window)
+            ref.assert_attention(got, lse, ref.attention(kv, vv, q, cu, lens, table, page, D ** -0.5, True, window, T))
+
+
+def test_pages_behind_a_window_may_be_gone(B):
+    """A server frees pages that no query sees any more: their table entries may be anything, and reused pages may hold
+    another sequence's tokens or none."""
+    rng = np.random.default_rng(16)
+    hq, hkv, D, page, window = 4, 2, 128, 16, 50
+    for qn in (1, 3, 70):
+        L = 500
+        cache, (kv, vv), qd, q, cu, lens, table, T = attend_case(rng, B, [L, 33], [qn, 1], hq, hkv, D, page)
+        first = max(0, L - qn - window + 1) // page          # pages before this one are seen by nobody
+        want = ref.attention(kv, vv, q, cu, lens, table, page, D ** -0.5, True, window, T)
+        for filler in (-1, 2 ** 30, int(table[1, 2])):       # gone, nonsense, a page with unwritten places
+            broken = table.copy()
+            broken[0, :first] = filler
+            got, lse = run_attention(B, cache, qd, cu, lens, broken, T, hq, window=window)
+            ref.assert_attention(got, lse, want)
+
+
+def test_two_attentions_at_once(B):
+    """Calls on two streams with a workspace each do not meet."""
+    import torch
+    rng = np.random.default_rng(17)
+    hq, hkv, D, page = 8, 2, 128, 16
+    cases = [attend_case(rng, B, lens, qs, hq, hkv, D, page) for lens, qs in (([3000, 10], [1, 1]), ([2500], [60]), ([64] * 20, [1] * 20))]
+    args = [(c[0], c[2], dev(c[4]), dev(c[5]), dev(c[6]), int(np.diff(c[4]).max()), int(c[5].max())) for c in cases]
+    want = [B.batq_paged_attention(*a) for a in args]
+    ws = [torch.empty(max(16, B.batq_paged_attention_workspace(a[0], hq, a[3].shape[0], a[1].shape[0], a[5], a[6])), dtype=torch.uint8, device="cuda") for a in args]
+    streams = [torch.cuda.Stream() for _ in args]
+    torch.cuda.synchronize()
+    for rep in range(3):
+        outs = [torch.zeros_like(w) for w in want]
+        torch.cuda.synchronize()
+        for _ in range(4):
+            for a, w, o_, s in zip(args, ws, outs, streams):
+                with torch.cuda.stream(s):
+                    B.batq_paged_attention(*a, out=o_, workspace=w)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(outs, want)), rep
+
+
+def test_binding_refuses_what_does_not_fit(B):
+    import torch
+    cache = B.PagedCache(4, 16, 2, 64)
+    q = torch.zeros((3, 256), dtype=torch.bfloat16, device="cuda")
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    good = (cache, q, i32(0, 3), i32(5), i32(0, 1).view(1, 2), 3, 5)
+    B.batq_paged_attention(*good)
+    for k, bad in ((1, q.float()), (1, q[:, ::2]), (2, i32(0, 3).long()), (2, i32(0, 2, 3)), (3, i32(5).cpu()), (4, i32(0, 1)), (1, q.cpu())):
+        with pytest.raises(ValueError):
+            B.batq_paged_attention(*good[:k], bad, *good[k + 1:])
+    with pytest.raises(B.BatqError):
+        B.batq_paged_attention(*good, workspace=torch.empty(100, dtype=torch.uint8, device="cuda")[1:])   # alignment
+    long = (cache, q, i32(0, 3), i32(5), i32(0, 1).view(1, 2), 3, 100000)
+    with pytest.raises(B.BatqError):
+        B.batq_paged_attention(*long, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    k = torch.zeros((2, 128), dtype=torch.bfloat16, device="cuda")
+    slots = torch.zeros(2, dtype=torch.int64, device="cuda")
+    B.batq_kv_paged_append(cache, k, k, slots)
+    for bad in (dict(k=k.cpu()), dict(v=k[:1]), dict(slots=slots.int()), dict(rope=torch.zeros((4, 64), device="cuda")),
+                dict(q=k[:1]), dict(v=k.float())):
+        with pytest.raises(ValueError):
+            B.batq_kv_paged_append(**{**dict(cache=cache, k=k, v=k, slots=slots), **bad})
+    with pytest.raises(B.BatqError):
+        B.batq_kv_paged_append(cache, k, k, slots, tk=B.Transform(64, None, None, None))
+
+
 # ---------------------------------------------------------------------------------------- together
 @pytest.mark.parametrize("transforms", [False, True])
 def test_a_serving_step_end_to_end(B, transforms):
