@@ -426,7 +426,8 @@ typedef struct {
  *           The slots of a call must differ: what one holds that two tokens were written to is unspecified.
  * q, k, v share xdtype (bf16 or fp32) and may be column ranges of one tensor; all pointers and row pitches are 16-byte
  * aligned (slots 8-byte, positions 4-byte).  q_out must not overlap q.  The products of the transform are carried to
- * fp32 accuracy: rotated values are not rounded to 16 bits.  M == 0 is a no-op.
+ * fp32 accuracy: rotated values are not rounded to 16 bits.  M == 0 is a no-op.  M rounded up to 32, times all heads
+ * (queries, keys, values), times head_dim, is less than 2^36.
  * BATQ_ERR_MISMATCH: tk or tv has another width. */
 batq_status batq_kv_paged_append(const batq_paged_cache* cache, const batq_transform* tk, const batq_transform* tv,
                                  const batq_rope* rope, const void* q, int64_t ldq, int q_heads, void* q_out,
@@ -446,13 +447,16 @@ batq_status batq_kv_paged_append(const batq_paged_cache* cache, const batq_trans
  *   max_q, max_kv  bounds of the query and token counts that the call is planned for: of a sequence with more, the
  *               first max_q queries are served, and it counts as max_kv tokens long
  * The lists are read on the device and nothing in them is trusted: rows outside total_q, tokens behind table_width
- * pages and pages outside [0, num_pages) take no part.
- *   q, out      bf16, total_q x q_heads * head_dim, 16-byte aligned rows; q_heads a multiple of kv_heads, at most
- *               128 query heads to a key head.  Scores, softmax and sums are fp32; the probabilities are multiplied with
+ * pages and pages outside [0, num_pages) take no part.  Places that a query does not see may hold anything, NaN codes
+ * too; a query that sees a NaN key gets NaN, and of a value that is not finite in bf16 the channels that hold it.
+ *   q, out      bf16, total_q x q_heads * head_dim, 16-byte aligned rows, not overlapping; q_heads a multiple of
+ *               kv_heads, at most 128 query heads to a key head.  Scores, softmax and sums are fp32; the probabilities are multiplied with
  *               the values as bf16 (sequences of few queries: as two bf16 terms).
  *   lse         DEVICE fp32 [total_q][q_heads] or NULL
  *   workspace   DEVICE, 256-byte aligned, batq_paged_attention_workspace() bytes: partial results of long
- *               sequences that are cut into parts.  Its contents need not be cleared.
+ *               sequences that are cut into parts.  Its contents need not be cleared.  Calls that may run at the same
+ *               time (two streams, two captured graphs) need one each.
+ * BATQ_ERR_SHAPE: also for batch * kv_heads from 2^19 on, or from 2^24 / (max_kv / 1024 + 2).
  * For queries and keys through batq_kv_paged_append with tk, out is in the basis of tv: batq_transform_apply with
  * BATQ_APPLY_INVERSE takes it back, or T_v^-1 is folded into the output projection offline. */
 typedef struct {
@@ -479,7 +483,9 @@ batq_status batq_paged_attention(const batq_paged_cache* cache, const batq_paged
  *            overlap it otherwise, nor X.  One rounding to the output type.
  * X, A, B 16-byte aligned, row pitch of X a multiple of 16 bytes; base and out aligned to their elements.  The products
  * are carried to fp32 accuracy (the intermediate X A^T is not rounded to 16 bits).
- *   workspace  DEVICE, 256-byte aligned, batq_lora_workspace() bytes; its contents need not be cleared. */
+ * M, K and N are at most 2^26.  Outputs that depend on an infinite or NaN input or weight are infinite or NaN.
+ *   workspace  DEVICE, 256-byte aligned, batq_lora_workspace() bytes; its contents need not be cleared.  Calls that may
+ *              run at the same time need one each. */
 size_t batq_lora_workspace(int M, int K, int N, int rank, int adapters);
 batq_status batq_lora_add(const void* X, batq_dtype xdtype, int M, int K, int64_t ldx, const void* A, const void* B,
                           int N, int rank, int adapters, const float* scales, const int32_t* index, const void* base,

@@ -892,6 +892,8 @@ batq_status batq_kv_paged_append(const batq_paged_cache* cache, const batq_trans
     if (M < 0 || M > (1 << 30) || ldk < width || ldv < width || q_heads < 0 || q_heads > (1 << 19) || q_heads % cache->kv_heads != 0)
         return BATQ_ERR_SHAPE;
     if (q_heads > 0 && (ldq < (int64_t)q_heads * D || ldq_out < (int64_t)q_heads * D)) return BATQ_ERR_SHAPE;
+    // a launch has fewer than 2^32 threads, a wave for 32 tokens of 32 channels
+    if (((int64_t)M + 31) / 32 * (q_heads + 2 * cache->kv_heads) * (D / 32) >= 1 << 26) return BATQ_ERR_SHAPE;
     if ((tk && tk->K != width) || (tv && tv->K != width)) return BATQ_ERR_MISMATCH;
     if (rope) {
         if (!rope->table) return BATQ_ERR_NULL;
@@ -921,8 +923,10 @@ static batq_status check_attention_dims(const batq_paged_cache* c, int q_heads, 
     if (batch < 0 || batch > (1 << 20) || total_q < 0 || max_q < 0 || max_kv < 0 || max_kv > (1 << 30) ||
         (int64_t)total_q * q_heads > INT32_MAX || (int64_t)max_q * q_heads > INT32_MAX)
         return BATQ_ERR_SHAPE;
-    // workgroups are numbered with 32 bits: the shortest parts are 256 tokens
-    if ((int64_t)batch * c->kv_heads * (max_kv / 256 + 2) > INT32_MAX) return BATQ_ERR_SHAPE;
+    // a launch has fewer than 2^32 threads: workgroups of 256 for the parts of (sequence, key head) pairs (1024 tokens long
+    // where there are many) and for up to 32 rows each, of 512 for tiles of 256 rows
+    const int64_t pairs = (int64_t)batch * c->kv_heads;
+    if (pairs * (max_kv / 1024 + 2) >= 1 << 24 || pairs * 32 >= 1 << 24 || (int64_t)total_q * q_heads / 256 + pairs >= 1 << 23) return BATQ_ERR_SHAPE;
     return BATQ_OK;
 }
 
@@ -970,6 +974,7 @@ batq_status batq_paged_attention(const batq_paged_cache* cache, const batq_paged
 // ---- low-rank adapters
 static batq_status check_lora_dims(int M, int K, int N, int rank, int adapters) {
     if (M < 0 || K <= 0 || K % 32 != 0 || N <= 0 || rank < 8 || rank > 128 || rank % 8 != 0 || adapters < 1) return BATQ_ERR_SHAPE;
+    if (M > 1 << 26 || K > 1 << 26 || N > 1 << 26) return BATQ_ERR_SHAPE;      // (a launch has fewer than 2^32 threads)
     return BATQ_OK;
 }
 

@@ -322,7 +322,7 @@ Plan plan(int M, int K, int adapters) {
     p.tiles = (int)(((int64_t)M + 15) / 16);
     p.slots = p.few ? 64 / p.tiles : 1;
     if (p.slots > 16) p.slots = 16;
-    if (p.slots > adapters + 1) p.slots = adapters + 1;     // (rows without an adapter count as one)
+    if (p.slots - 1 > adapters) p.slots = adapters + 1;     // (rows without an adapter count as one)
     if (p.slots < 1) p.slots = 1;
     int n = p.few ? 256 / p.tiles : 1;
     if (n > (K + 255) / 256) n = (K + 255) / 256;
@@ -351,12 +351,12 @@ hipError_t shrink(const LoraArgs& a, bool few, unsigned grid, int dev, hipStream
 
 template <typename YT, int G>
 hipError_t launch_expand(LoraArgs& a, const Plan& p, hipStream_t stream) {
-    // tiles of a workgroup: as many as leave eight workgroups to a compute unit; workgroups are numbered with 32 bits
+    // tiles of a workgroup: as many as leave eight workgroups to a compute unit, within 2^23 workgroups
     a.groups_n = (int)(((int64_t)a.N + 255) / 256);
     const int64_t units = (int64_t)p.tiles * p.slots * a.groups_n;
     int64_t t = p.few ? 1 : (int64_t)p.tiles * a.groups_n / 2048;
     if (t > 32) t = 32;
-    if (t < units / (1 << 30) + 1) t = units / (1 << 30) + 1;
+    if (t < units / (1 << 22) + 1) t = units / (1 << 22) + 1;
     a.tile_rows = (int)t;
     const unsigned grid = (unsigned)((p.tiles + t - 1) / t * p.slots * a.groups_n);
     if (p.parts > 1) expand_kernel<YT, G, kMaxParts><<<grid, 256, 0, stream>>>(a);

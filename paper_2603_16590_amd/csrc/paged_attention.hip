@@ -38,6 +38,10 @@ struct AttnArgs {
     float *many_o, *many_ml;                                // likewise [row of q][query head][part]
 };
 
+// First token that the window leaves to a query at `pos`, which may be far below zero (more queries than tokens) beside a
+// window of any size.
+__device__ __forceinline__ int first_seen(const AttnArgs& a, int pos) { return a.window && pos >= a.window ? pos - a.window + 1 : 0; }
+
 // Sequence b as the kernels take it: nothing in the lists is trusted.
 struct Seq {
     int begin, n, len;                                      // first row, queries served, tokens
@@ -54,7 +58,7 @@ __device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
     s.len = (int)min((int64_t)max(0, min(a.kv_len[b], a.max_kv)), (int64_t)a.table_width << a.page_shift);
     s.first_pos = s.len - n;
     s.t_hi = a.causal ? max(0, min(s.len, s.first_pos + s.n)) : s.len;
-    s.t_lo = a.window ? min(s.t_hi, max(0, s.first_pos - a.window + 1)) : 0;
+    s.t_lo = min(s.t_hi, first_seen(a, s.first_pos));
     return s;
 }
 
@@ -80,6 +84,18 @@ __device__ __forceinline__ uint32_t cvt_hi(uint32_t w, float sc) {
 __device__ __forceinline__ uint32_t low_halves(uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x05040100u); }
 __device__ __forceinline__ uint32_t high_halves(uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x07060302u); }
 __device__ __forceinline__ float scale_byte(uint32_t w, int i) { return scale_operand((w >> (8 * i)) & 0xFFu); }
+
+// A weight of zero times a value that is not finite is not zero, and a matrix product has no mask: where a block's tokens are
+// seen by some rows only and such a value may be among them, it is taken as zero, and the sums of the rows that do see it
+// become NaN by themselves.
+// Whether four codes with their scale may give one: NaN codes; scales from 2^120 on (448 x 2^120 is past bf16).
+__device__ __forceinline__ uint32_t odd_codes(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ uint32_t odd_scales(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x09090909u) & w & 0x80808080u; }
+// All bits of the bf16 halves that are not finite.
+__device__ __forceinline__ uint32_t odd_halves(uint32_t w) {
+    return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+}
+
 __device__ __forceinline__ float shuffle_xor(float x, int d) { return __shfl_xor(x, d); }
 
 // Few query rows to a key head (decoding, short drafts): bound by the stream of codes.  A workgroup takes one part of one
@@ -171,11 +187,11 @@ attend_few(const AttnArgs a) {
         for (int u = 0; u < kU; ++u) qf[x][u] = *reinterpret_cast<const bf16x8*>(p + 8 * u);
         const int pos = s.first_pos + i;
         row_hi[x] = !live ? 0 : a.causal ? min(s.len, pos + 1) : s.len;
-        row_lo[x] = a.window ? max(0, pos - a.window + 1) : 0;
+        row_lo[x] = first_seen(a, pos);
     }
     // blocks in [all_lo, all_hi) are seen whole by every row
     const int all_hi = a.causal ? min(s.len, s.first_pos + 1) : s.len;
-    const int all_lo = a.window ? max(0, s.first_pos + s.n - a.window) : 0;
+    const int all_lo = first_seen(a, s.first_pos + s.n - 1);
 
     float m[NT], l[NT];
     f32x4 o[NT][kV];
@@ -206,6 +222,7 @@ attend_few(const AttnArgs a) {
         }
         if (more) load_k(t + 128);
         const bool whole = t >= all_lo && t + 32 <= all_hi && __ballot(!v_ok) == 0;
+        bool odd = false;                                   // wave-uniform
         if (!whole) {
             // masked places may hold anything (unwritten codes, pages that are gone): their scores are replaced, their
             // values and scales become zeros and ones, so that a weight of zero stays a product of zero
@@ -221,11 +238,19 @@ attend_few(const AttnArgs a) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int tok = t + 8 * g + i;
-                if (!(v_ok && tok >= s.t_lo && tok < s.len)) {
+                if (!(v_ok && tok >= s.t_lo && tok < s.t_hi)) {
 #pragma unroll
                     for (int c = 0; c < kV / 4; ++c) vw[i][c] = 0u;
                     vs[i / 4] = (vs[i / 4] & ~(0xFFu << (8 * (i & 3)))) | (127u << (8 * (i & 3)));
                 }
+            }
+            if (s.n > 1) {                                  // (one query: the tokens left are seen by all rows)
+                uint32_t any = odd_scales(vs[0]) | odd_scales(vs[1]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int c = 0; c < kV / 4; ++c) any |= odd_codes(vw[i][c]);
+                odd = __ballot(any != 0) != 0;
             }
         }
         bf16x8 ph[NT], pl[NT];                              // the weights as two bf16 terms
@@ -273,8 +298,25 @@ attend_few(const AttnArgs a) {
 #pragma unroll
                 for (int x = 0; x < NT; ++x) {
                     f32x4& acc = o[x][4 * c + j];
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl[x], acc, 0, 0, 0);
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, ph[x], acc, 0, 0, 0);
+                    bf16x8 vx = vf;
+                    if (odd) {
+                        // a product of ones in their places with ones in the places that a row sees counts what each sum meets
+                        u32x4 w = __builtin_bit_cast(u32x4, vf), ones;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) ones[e] = odd_halves(w[e]) & 0x3F803F80u, w[e] &= ~odd_halves(w[e]);
+                        vx = __builtin_bit_cast(bf16x8, w);
+                        bf16x8 sees;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const int tok = t + 8 * g + e;
+                            sees[e] = (__bf16)(v_ok && tok >= row_lo[x] && tok < row_hi[x] ? 1.0f : 0.0f);
+                        }
+                        const f32x4 z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ones), sees, f32x4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[r] += z[r] > 0.0f ? __builtin_nanf("") : 0.0f;
+                    }
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vx, pl[x], acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vx, ph[x], acc, 0, 0, 0);
                 }
             }
         }
@@ -314,14 +356,14 @@ attend_few(const AttnArgs a) {
         const int i = r / a.group, head = h * a.group + r - i * a.group;
         const size_t row = (size_t)(s.begin + i);
         if (only) {
-            const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+            const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
             uint16_t* p = a.out + row * a.ldo + (size_t)head * D + c0;
 #pragma unroll
             for (int j = 0; j < kV; j += 4) {
                 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
                 *reinterpret_cast<bf16x4*>(p + j) = bf16x4{(__bf16)(v[j] * inv), (__bf16)(v[j + 1] * inv), (__bf16)(v[j + 2] * inv), (__bf16)(v[j + 3] * inv)};
             }
-            if (a.lse && c0 == 0) a.lse[row * a.q_heads + head] = sum > 0.0f ? (top + __log2f(sum)) * 0.69314718055994531f : -INFINITY;
+            if (a.lse && c0 == 0) a.lse[row * a.q_heads + head] = sum != 0.0f ? (top + __log2f(sum)) * 0.69314718055994531f : -INFINITY;
         } else {
             const size_t at = ((size_t)bh * a.part_rows + r) * a.max_parts + part;
 #pragma unroll
@@ -374,11 +416,11 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const float* part_o,
             for (int c = 0; c < D / 64; ++c) v[c] += s_v[w][lane * (D / 64) + c];
         }
     }
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
     __bf16* o = reinterpret_cast<__bf16*>(a.out + row * a.ldo + (size_t)head * D + lane * (D / 64));
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) o[c] = (__bf16)(v[c] * inv);
-    if (a.lse && lane == 0) a.lse[row * a.q_heads + head] = sum > 0.0f ? (top + __log2f(sum)) * 0.69314718055994531f : -INFINITY;
+    if (a.lse && lane == 0) a.lse[row * a.q_heads + head] = sum != 0.0f ? (top + __log2f(sum)) * 0.69314718055994531f : -INFINITY;
 }
 
 // One workgroup per row of a (sequence, key head) of few rows.
@@ -412,14 +454,14 @@ __device__ __forceinline__ int k_place(int row, int chunk) { return D == 128 ? c
 __device__ __forceinline__ int v_place(int row, int chunk) { return chunk ^ (((row >> 1) ^ (row >> 4 & 1)) & 7); }
 
 template <int D>
-constexpr int many_lds() { return 4 * 64 * D * 2 + 2 * 16; }   // two buffers of keys and values, which 16-token groups exist
+constexpr int many_lds() { return 4 * 64 * D * 2 + 2 * 16; }   // two buffers of keys and values, marks
 
 // Tokens that some row of a sequence's 256-row tile sees.
 __device__ __forceinline__ TokenRange tile_tokens(const AttnArgs& a, const Seq& s, int tile) {
     const int i0 = tile * kManyRows / a.group, i1 = (min(s.n * a.group, (tile + 1) * kManyRows) - 1) / a.group;
     TokenRange t;
     t.hi = a.causal ? max(0, min(s.len, s.first_pos + i1 + 1)) : s.len;
-    t.lo = a.window ? min(t.hi, max(0, s.first_pos + i0 - a.window + 1)) : 0;
+    t.lo = min(t.hi, first_seen(a, s.first_pos + i0));
     return t;
 }
 
@@ -471,6 +513,7 @@ attend_many(const AttnArgs a) {
     uint8_t* const s_k = lds;                               // [2][64][D] bf16
     uint8_t* const s_v = lds + 2 * kHalf;                   // [2][D][64] bf16
     uint8_t* const s_ok = lds + 4 * kHalf;                  // [2][4]: whether the page of 16 tokens exists
+    uint8_t* const s_odd = s_ok + 16;                       // [8]: whether a wave took values as zero
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, hh = lane >> 5;
     const int h = blockIdx.x % a.kv_heads, xp = blockIdx.x / a.kv_heads;
@@ -499,13 +542,16 @@ attend_many(const AttnArgs a) {
     }
     const int pos = s.first_pos + i;
     const int row_hi = !live ? 0 : a.causal ? min(s.len, pos + 1) : s.len;
-    const int row_lo = a.window ? max(0, pos - a.window + 1) : 0;
+    const int row_lo = first_seen(a, pos);
     // the wave's rows: [some_lo, some_hi) is seen by some, [all_lo, all_hi) by all of them
     const int wr0 = row0 + wave * 32, wr1 = min(rows, wr0 + 32) - 1;
     const bool wave_live = wr0 < rows;
     const int wp0 = s.first_pos + wr0 / a.group, wp1 = s.first_pos + wr1 / a.group;
-    const int some_hi = !wave_live ? 0 : a.causal ? min(s.len, wp1 + 1) : s.len, some_lo = a.window ? max(0, wp0 - a.window + 1) : 0;
-    const int all_hi = a.causal ? min(s.len, wp0 + 1) : s.len, all_lo = a.window ? max(0, wp1 - a.window + 1) : 0;
+    const int some_hi = !wave_live ? 0 : a.causal ? min(s.len, wp1 + 1) : s.len, some_lo = first_seen(a, wp0);
+    const int all_hi = a.causal ? min(s.len, wp0 + 1) : s.len, all_lo = first_seen(a, wp1);
+    // likewise of the workgroup's rows
+    const int last_pos = s.first_pos + (min(rows, row0 + kManyRows) - 1) / a.group;
+    const int tile_all_hi = a.causal ? min(s.len, s.first_pos + row0 / a.group + 1) : s.len, tile_all_lo = first_seen(a, last_pos);
 
     // staging: a thread has a piece of 16 channels of a key and a 4 x 4 piece of values (D = 64: one or the other).  A wave's 8
     // (16) tokens lie in one page: pages and addresses are scalars, what a lane adds to them stays the same
@@ -547,6 +593,8 @@ attend_many(const AttnArgs a) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) v_to[c] = (4 * v_c + c) * 128 + v_place(4 * v_c + c, chunk) * 16 + half * 8;
     }
+    auto partly_seen = [&](int t) { return t < tile_all_lo || t + 64 > tile_all_hi; };
+    bool odd = false;                                       // wave-uniform
     auto stage = [&](int t, int buf) {                      // the requested tile (first token t) into LDS
         if (do_k) {
             const float sc = scale_operand(kscale);
@@ -558,11 +606,11 @@ attend_many(const AttnArgs a) {
         }
         if (do_v) {
             // places that nobody sees may hold anything: a weight of zero must stay a product of zero
-            if (!there || t < range.lo || t + 64 > s.len) {
+            if (!there || t < range.lo || t + 64 > range.hi) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int tok = t + tok0 + v_tok + e;
-                    if (!(there && tok >= range.lo && tok < s.len)) {
+                    if (!(there && tok >= range.lo && tok < range.hi)) {
                         vw[e] = 0u;
                         vscale = (vscale & ~(0xFFu << (8 * e))) | (127u << (8 * e));
                     }
@@ -573,6 +621,11 @@ attend_many(const AttnArgs a) {
             for (int e = 0; e < 4; ++e) {
                 const float sc = scale_byte(vscale, e);
                 lo[e] = cvt_lo(vw[e], sc), hi[e] = cvt_hi(vw[e], sc);
+            }
+            if (partly_seen(t) && __ballot((odd_scales(vscale) | odd_codes(vw[0]) | odd_codes(vw[1]) | odd_codes(vw[2]) | odd_codes(vw[3])) != 0)) {
+                odd = true;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) lo[e] &= ~odd_halves(lo[e]), hi[e] &= ~odd_halves(hi[e]);
             }
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
@@ -672,11 +725,35 @@ attend_many(const AttnArgs a) {
         if (more) stage(t + 64, buf ^ 1);
         __syncthreads();
     }
+    if (lane == 0) s_odd[wave] = odd;
+    __syncthreads();
+    const u32x2 odds = *reinterpret_cast<const u32x2*>(s_odd);
+    if (odds[0] | odds[1]) {                                // (rare: as slow as it likes)
+        for (int tok = t_begin; tok < t_end; ++tok) {
+            const int pg = table[min(tok >> a.page_shift, last_page)];
+            if (!partly_seen(tok & ~63) || tok < range.lo || (uint32_t)pg >= (uint32_t)a.num_pages) continue;
+            const bool sees = tok >= row_lo && tok < row_hi;
+            const int64_t ph = (int64_t)pg * a.kv_heads + h;
+            const uint8_t* p = a.v_codes + ((ph << a.page_shift) + (tok & page_mask)) * D + 4 * hh;
+#pragma unroll
+            for (int c = 0; c < kCb; ++c) {
+                const float sc = scale_operand(a.v_scales[((ph * (D / 32) + c) << a.page_shift) + (tok & page_mask)]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t w = *reinterpret_cast<const uint32_t*>(p + 32 * c + 8 * e);
+                    const uint32_t x = odd_halves(cvt_lo(w, sc)), y = odd_halves(cvt_hi(w, sc));
+                    const uint32_t hit[4] = {x & 0xFFFFu, x >> 16, y & 0xFFFFu, y >> 16};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) o[c][4 * e + k] += sees && hit[k] ? __builtin_nanf("") : 0.0f;
+                }
+            }
+        }
+    }
     if (!live || i >= s.n) return;
     l += shuffle_xor(l, 32);
     // element e of o[c] is channel 32c + 8 (e / 4) + 4h + e % 4
     if (parts == 1) {
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        const float inv = l != 0.0f ? 1.0f / l : 0.0f;
         uint16_t* p = a.out + row * a.ldo + (size_t)head * D + 4 * hh;
 #pragma unroll
         for (int c = 0; c < kCb; ++c)
@@ -686,7 +763,7 @@ attend_many(const AttnArgs a) {
                 *reinterpret_cast<bf16x4*>(p + 32 * c + 8 * e) =
                     bf16x4{(__bf16)(o[c][4 * e] * inv), (__bf16)(o[c][4 * e + 1] * inv), (__bf16)(o[c][4 * e + 2] * inv), (__bf16)(o[c][4 * e + 3] * inv)};
             }
-        if (a.lse && hh == 0) a.lse[row * a.q_heads + head] = l > 0.0f ? (m + __log2f(l)) * 0.69314718055994531f : -INFINITY;
+        if (a.lse && hh == 0) a.lse[row * a.q_heads + head] = l != 0.0f ? (m + __log2f(l)) * 0.69314718055994531f : -INFINITY;
     } else {
         const size_t at = (row * a.q_heads + head) * a.many_parts + part;
         float* p = a.many_o + at * D + 4 * hh;
@@ -759,7 +836,9 @@ Plan plan(int group, int kv_heads, int batch, int total_q, int max_q, int max_kv
     }
     p.many_parts = 1, p.many_len = 1 << 30;
     if (p.many) {
-        p.many_tiles = (int)((int64_t)total_q * group / kManyRows + batch);
+        // sum of ceil(rows / 256) over sequences of more than few_rows rows, rows / (few_rows + 1) of them at most
+        const int64_t all = (int64_t)total_q * group, longer = all / (p.few_rows + 1);
+        p.many_tiles = (int)(all / kManyRows + (longer < batch ? longer : batch));
         const int64_t groups = (int64_t)((int64_t)total_q * group / kManyRows + 1) * kv_heads;
         const int64_t tokens = span(kManyRows / group + 1);
         int64_t n = compute_units / groups;
@@ -824,7 +903,8 @@ hipError_t launch_paged_attention(const batq_paged_cache& c, const batq_paged_ba
     if (e != hipSuccess) return e;
     // a window's plan where it needs no more room than the plan without one, which is what the workspace is sized for
     const Plan full = plan(q_heads / c.kv_heads, c.kv_heads, b.batch, b.total_q, b.max_q, b.max_kv, 0, cus);
-    Plan p = plan(q_heads / c.kv_heads, c.kv_heads, b.batch, b.total_q, b.max_q, b.max_kv, window, cus);
+    // (without causal a window has no upper end)
+    Plan p = plan(q_heads / c.kv_heads, c.kv_heads, b.batch, b.total_q, b.max_q, b.max_kv, causal ? window : 0, cus);
     if (part_bytes(p, c, q_heads, b.batch, b.total_q) > part_bytes(full, c, q_heads, b.batch, b.total_q)) p = full;
     AttnArgs a = {};
     a.q = static_cast<const uint16_t*>(q), a.ldq = ldq, a.ldo = ldo, a.out = static_cast<uint16_t*>(out), a.lse = lse;

@@ -506,6 +506,53 @@ def test_pages_behind_a_window_may_be_gone(B):
             ref.assert_attention(got, lse, want)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_values_that_are_not_finite(B, D):
+    """NaN codes where some rows look and others do not: in a causal prompt, short drafts and windows; a key of NaN makes the
+    rows that see it NaN, a value its channel of them, nothing else changes."""
+    rng = np.random.default_rng(18 + D)
+    page = 16
+    for hq, hkv, lens, qs, window, causal in ((2, 1, [200, 90], [200, 3], 0, True), (4, 4, [333], [333], 40, True), (12, 2, [150, 700], [2, 5], 0, True),
+                                              (8, 2, [300], [4], 6, True), (4, 1, [64, 1000], [1, 120], 100, True), (3, 1, [129], [100], 60, False),
+                                              (6, 2, [77, 500], [1, 2], 0, False)):
+        cache, _, qd, q, cu, lens, table, T = attend_case(rng, B, lens, qs, hq, hkv, D, page)
+        arrays = host(cache)
+        for what, count in ((2, 5), (2, 1), (0, 1)):        # values, one value, one key
+            a = [x.copy() for x in arrays]
+            for _ in range(count):
+                b = int(rng.integers(len(lens)))
+                tok = int(lens[b]) - 1 - int(rng.integers(0, min(int(lens[b]), qs[b] + 4)))
+                a[what][table[b, tok // page], rng.integers(hkv), tok % page, rng.integers(D)] = rng.choice([0x7F, 0xFF])
+            broken = B.PagedCache(cache.num_pages, page, hkv, D, tensors=[dev(x) for x in a])
+            with np.errstate(invalid="ignore"):
+                kv, vv = ref.cache_values(a[0], a[1]), ref.cache_values(a[2], a[3])
+                want = ref.attention(kv, vv, q, cu, lens, table, page, D ** -0.5, causal, window, T)
+            got, lse = run_attention(B, broken, qd, cu, lens, table, T, hq, window=window, causal=causal)
+            assert np.array_equal(np.isnan(got), np.isnan(want[0]))
+            assert np.array_equal(np.isnan(lse), np.isnan(want[1]))
+            clean = [np.where(np.isnan(want[0]), 0.0, x) for x in (want[0], want[2])]
+            smax, seen = np.where(np.isnan(want[3]), 0.0, want[3]), np.where(np.isnan(want[1]), 0.0, want[1])
+            ref.assert_attention(np.where(np.isnan(got), 0.0, got), np.where(np.isnan(lse), 0.0, lse), (clean[0], seen, clean[1], smax))
+
+
+def test_windows_without_causal_and_of_any_size(B):
+    """A window without causal ends nowhere above: rows of long sequences see more than a window; windows up to the largest
+    number beside sequences with more queries than tokens; fewer queries served than there are."""
+    rng = np.random.default_rng(19)
+    hq, hkv, D, page = 4, 2, 64, 16
+    cases = (([3000], [2500], 20, False, None), ([2100, 900], [1, 2], 7, False, None), ([40, 9], [60, 12], 2 ** 31 - 1, True, None),
+             ([2600], [2600], 30, False, 5), ([2600, 30], [1300, 1], 30, False, 3), ([2600, 30], [1300, 1], 30, True, 1), ([1500], [1400], 2 ** 31 - 1, False, 300))
+    for lens, qs, window, causal, max_q in cases:
+        cache, (kv, vv), qd, q, cu, lens, table, T = attend_case(rng, B, lens, qs, hq, hkv, D, page)
+        got, lse = run_attention(B, cache, qd, cu, lens, table, T, hq, window=window, causal=causal, max_q=max_q)
+        want = ref.attention(kv, vv, q, cu, lens, table, page, D ** -0.5, causal, window, T)
+        if max_q:
+            rest = np.concatenate([np.arange(cu[b] + min(max_q, cu[b + 1] - cu[b]), cu[b + 1]) for b in range(len(lens))])
+            assert np.all(got[rest] == 7.0) and np.all(lse[rest] == 7.0)
+            want[1][rest] = np.nan
+        ref.assert_attention(got, lse, want)
+
+
 def test_two_attentions_at_once(B):
     """Calls on two streams with a workspace each do not meet."""
     import torch

@@ -115,3 +115,15 @@ def test_binding_refusals(B):
         B.batq_lora_add(torch.zeros(2, 64), torch.zeros(1, 8, 32).bfloat16(), torch.zeros(1, 4, 8).bfloat16(), torch.zeros(2, dtype=torch.int32))
     with pytest.raises(ValueError):
         B.batq_lora_add(torch.zeros(2, 32), torch.zeros(1, 8, 32), torch.zeros(1, 4, 8).bfloat16(), torch.zeros(2, dtype=torch.int32))
+
+
+def test_sizes_past_a_launch_are_refused(B):
+    big = cache(kv_heads=4096)
+    for kw in (dict(batch=128, q_heads=4096, ldq=1 << 18, ldo=1 << 18), dict(batch=100, q_heads=4096, ldq=1 << 18, ldo=1 << 18, max_kv=1 << 20),
+               dict(batch=1, q_heads=4096, ldq=1 << 18, ldo=1 << 18, max_kv=1 << 30)):
+        assert attend(B, big, **kw) == 2, kw
+        assert B.lib.batq_paged_attention_workspace(C.byref(big), 4096, kw["batch"], 5, 4, kw.get("max_kv", 48)) == 0
+    assert append(B, big, M=1 << 22, ldk=1 << 18, ldv=1 << 18) == 2
+    for kw in (dict(M=(1 << 26) + 1), dict(K=(1 << 26) + 32, ldx=(1 << 26) + 32), dict(N=(1 << 26) + 1, ldb=(1 << 26) + 1, ldo=(1 << 26) + 1)):
+        assert lora(B, **kw) == 2, kw
+        assert B.lib.batq_lora_workspace(*[{**dict(M=4, K=64, N=40, rank=8, n=2), **kw}[k] for k in ("M", "K", "N", "rank", "n")]) == 0
