@@ -423,20 +423,6 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const float* part_o,
     if (a.lse && lane == 0) a.lse[row * a.q_heads + head] = sum != 0.0f ? (top + __log2f(sum)) * 0.69314718055994531f : -INFINITY;
 }
 
-// One workgroup per row of a (sequence, key head) of few rows.
-template <int D>
-__global__ void __launch_bounds__(256)
-join_few(const AttnArgs a) {
-    const unsigned unit = blockIdx.x, bh = unit / (unsigned)a.part_rows;
-    const int r = (int)(unit - bh * a.part_rows), h = (int)(bh % a.kv_heads), b = (int)(bh / a.kv_heads);
-    const Seq s = sequence(a, b);
-    const int rows = s.n * a.group;
-    if (r >= rows || rows > a.few_rows) return;
-    const int parts = live_parts(s, a.few_len);
-    if (parts == 1) return;
-    join_row<D, 4>(a, a.part_o, a.part_ml, (size_t)unit * a.max_parts, parts, (size_t)s.begin + r / a.group, h * a.group + r % a.group);
-}
-
 // Many query rows to a key head (prompts, chunks of prompts): bound by the matrix pipe, the exponentials and LDS reads.
 // A workgroup of eight waves takes 256 rows (row = query token * group + head of the group) of one (sequence, key head), 32
 // to a wave, and walks the visible tokens in tiles of 64.  The codes of the next tile are requested while this one is
@@ -775,12 +761,25 @@ attend_many(const AttnArgs a) {
     }
 }
 
-// One wave per (row of q, query head) of sequences with many rows: there are many of them, of few parts.
+// A row of a (sequence, key head) of few rows: by a workgroup.
 template <int D>
-__global__ void __launch_bounds__(64)
-join_many(const AttnArgs a) {
+__device__ __forceinline__ void join_few(const AttnArgs& a, unsigned unit) {
+    const unsigned bh = unit / (unsigned)a.part_rows;
+    const int r = (int)(unit - bh * a.part_rows), h = (int)(bh % a.kv_heads), b = (int)(bh / a.kv_heads);
+    const Seq s = sequence(a, b);
+    const int rows = s.n * a.group;
+    if (r >= rows || rows > a.few_rows) return;
+    const int parts = live_parts(s, a.few_len);
+    if (parts == 1) return;
+    join_row<D, 4>(a, a.part_o, a.part_ml, (size_t)unit * a.max_parts, parts, (size_t)s.begin + r / a.group, h * a.group + r % a.group);
+}
+
+// A (row of q, query head) of a sequence with many rows: by a wave, there are many of them, of few parts.
+template <int D>
+__device__ __forceinline__ void join_many(const AttnArgs& a, int unit) {
     const int lane = threadIdx.x & 63;
-    const int row = blockIdx.x / a.q_heads, head = blockIdx.x % a.q_heads;
+    const int row = unit / a.q_heads, head = unit - row * a.q_heads;
+    if (row >= a.total_q) return;
     int b = -1;                                             // the row's sequence: lanes look at 64 of them at a time
     for (int b0 = 0; b0 < a.batch && b < 0; b0 += 64) {
         bool mine = false;
@@ -799,6 +798,14 @@ join_many(const AttnArgs a) {
     const int parts = range_parts(t, a.many_len);
     if (parts == 1) return;
     join_row<D, 1>(a, a.many_o, a.many_ml, ((size_t)row * a.q_heads + head) * a.many_parts, parts, (size_t)row, head);
+}
+
+// Joins what both kernels have cut: the first `few` workgroups take a row each, the others four.
+template <int D>
+__global__ void __launch_bounds__(256)
+join_parts(const AttnArgs a, unsigned few) {
+    if (blockIdx.x < few) join_few<D>(a, blockIdx.x);
+    else join_many<D>(a, (int)((blockIdx.x - few) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)));
 }
 
 }  // namespace
@@ -868,15 +875,11 @@ hipError_t launch_attention(const AttnArgs& a, const Plan& p, int dev, hipStream
         else attend_few<D, 2><<<units, 256, 0, stream>>>(a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    if (p.max_parts > 1) {
-        join_few<D><<<(unsigned)a.batch * a.kv_heads * p.part_rows, 256, 0, stream>>>(a);
-        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    }
-    if (p.many_parts > 1) {
-        join_many<D><<<(unsigned)a.total_q * a.q_heads, 64, 0, stream>>>(a);
-        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    }
-    return hipSuccess;
+    const unsigned few = p.max_parts > 1 ? (unsigned)a.batch * a.kv_heads * p.part_rows : 0;
+    const unsigned many = p.many_parts > 1 ? ((unsigned)a.total_q * a.q_heads + 3) / 4 : 0;
+    if (few + many == 0) return hipSuccess;
+    join_parts<D><<<few + many, 256, 0, stream>>>(a, few);
+    return hipGetLastError();
 }
 
 }  // namespace
