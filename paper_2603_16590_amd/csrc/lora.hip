@@ -30,6 +30,7 @@ struct LoraArgs {
     int parts, part_k;                                      // parts of K and their length (a multiple of 256)
     int tile_rows, groups_n;                                // row tiles of a workgroup of expand_kernel, workgroups beside each other
     int vec;                                                // base and out rows allow 16-byte accesses
+    int past_cache;                                         // base and out together do not stay in the memory-side cache
 };
 
 // The adapter that row m uses, -1 for none.
@@ -184,6 +185,11 @@ struct Cols {
         if constexpr (sizeof(T) == 4) return __uint_as_float(w[c]);
         else return __uint_as_float(c & 1 ? w[c / 2] & 0xFFFF0000u : w[c / 2] << 16);
     }
+    // (in assembly: the compiler would make one plain store of this and of the other branch's)
+    __device__ __forceinline__ void store_nt(void* p) const {
+        if constexpr (sizeof(words) == 16) asm volatile("global_store_dwordx4 %0, %1, off nt\n\ts_nop 1" :: "v"(p), "v"(w) : "memory");
+        else asm volatile("global_store_dwordx2 %0, %1, off nt\n\ts_nop 1" :: "v"(p), "v"(w) : "memory");
+    }
     __device__ __forceinline__ void set(const float (&v)[C]) {
         if constexpr (sizeof(T) == 4) {
 #pragma unroll
@@ -298,7 +304,8 @@ expand_kernel(const LoraArgs a) {
                 if (whole) {
                     V w;
                     w.set(v);
-                    *reinterpret_cast<V*>(o) = w;
+                    if (a.past_cache) w.store_nt(o);
+                    else *reinterpret_cast<V*>(o) = w;
                 } else {
 #pragma unroll
                     for (int t = 0; t < C; ++t)
@@ -388,6 +395,10 @@ hipError_t launch_lora_add(const void* X, batq_dtype xdtype, int M, int K, int64
     a.M = M, a.K = K, a.N = N, a.rank = rank, a.adapters = adapters, a.slots = p.slots, a.parts = p.parts, a.part_k = p.part_k;
     const int64_t size = ydtype == BATQ_BF16 ? 2 : 4;
     a.vec = ((uintptr_t)out | (uintptr_t)base | (uintptr_t)(ldo * size) | (uintptr_t)(base ? ldb * size : 0)) % 16 == 0;
+    // Non-temporal stores from 192 MiB of base and out on (three quarters of the memory-side cache): 4096 x 14336 in bf16
+    // 69 -> 57 us and together with a reader of out right behind it 98 -> 97; at 8192 x 4096 (128 MiB) the reader pays for
+    // them, 72 -> 79 together, and in place (112 MiB for 4096 x 14336) they change nothing.
+    a.past_cache = (size_t)M * N * size * (base && base != out ? 2 : 1) > (size_t)192 << 20;
     const unsigned grid = (unsigned)p.tiles * p.slots * p.parts;
     if (hipError_t e = xdtype == BATQ_BF16 ? shrink<uint16_t>(a, p.few, grid, dev, stream) : shrink<float>(a, p.few, grid, dev, stream); e != hipSuccess)
         return e;
