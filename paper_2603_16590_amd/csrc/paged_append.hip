@@ -128,14 +128,15 @@ __device__ __forceinline__ void transform16(float (&y)[16], const bf16x8 (&t)[6]
     for (int r = 0; r < 16; ++r) y[r] = acc[r];
 }
 
-// Clips and quantises the lane's half of block blk; returns the codes, and the scale byte in *scale.
-__device__ __forceinline__ uint4 quantise16(float (&y)[16], const float* clip, const float* clip_max, int blk, uint32_t* scale) {
+// Clips and quantises the lane's half of a block; returns the codes, and the scale byte in *scale.  `clip` is 1 for no clipping,
+// or with `minmax` the ratio of the block's minimum beside clip_max of its maximum.
+__device__ __forceinline__ uint4 quantise16(float (&y)[16], bool minmax, float clip, float clip_max, uint32_t* scale) {
     const int lane = threadIdx.x & 63;
     auto other_half = [&](float x) -> float {
         return __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute((lane ^ 32) << 2, __builtin_bit_cast(int, x)));
     };
     float bound;
-    if (clip_max) {
+    if (minmax) {
         float mn = y[0], mx = y[0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) {
@@ -144,7 +145,7 @@ __device__ __forceinline__ uint4 quantise16(float (&y)[16], const float* clip, c
         }
         mn = __builtin_fminf(mn, other_half(mn));
         mx = __builtin_fmaxf(mx, other_half(mx));
-        const float lo = clip[blk] * mn, hi = clip_max[blk] * mx;
+        const float lo = clip * mn, hi = clip_max * mx;
 #pragma unroll
         for (int r = 0; r < 16; ++r) y[r] = clamp_lo_hi(y[r], lo, hi);
         bound = __builtin_fmaxf(__builtin_fabsf(clamp_lo_hi(mn, lo, hi)), __builtin_fabsf(clamp_lo_hi(mx, lo, hi)));
@@ -152,8 +153,7 @@ __device__ __forceinline__ uint4 quantise16(float (&y)[16], const float* clip, c
         float x = __builtin_fabsf(y[0]);
 #pragma unroll
         for (int r = 1; r < 16; ++r) x = __builtin_fmaxf(x, __builtin_fabsf(y[r]));
-        bound = __builtin_fmaxf(x, other_half(x));
-        if (clip) bound *= clip[blk];
+        bound = __builtin_fmaxf(x, other_half(x)) * clip;
     }
     const uint32_t sb = e8m0_of_bound_fp8(bound);
     const float sc = scale_operand(sb);
@@ -201,6 +201,11 @@ append_few(const AppendArgs a) {
                                    : static_cast<const XT*>(a.v) + (size_t)mm * a.ldv;
     const int blk = (kind == kQuery ? head / a.group : head) * kBlocks + b;     // block of the transform
     const uint4* op = kind == kQuery ? a.tq : kind == kKey ? a.tk : a.tv;
+    const float* clips = kind == kKey ? a.clip_k : a.clip_v;
+    const float* clips_max = kind == kKey ? a.clip_k_max : a.clip_v_max;
+    float clip = 1.0f, clip_max = 1.0f;
+    if (kind != kQuery && clips) clip = clips[blk];
+    if (kind != kQuery && clips_max) clip_max = clips_max[blk];
     bf16x8 t[6];
     if (op)
 #pragma unroll
@@ -218,7 +223,7 @@ append_few(const AppendArgs a) {
         return;
     }
     uint32_t sb;
-    const uint4 codes = kind == kKey ? quantise16(y, a.clip_k, a.clip_k_max, blk, &sb) : quantise16(y, a.clip_v, a.clip_v_max, blk, &sb);
+    const uint4 codes = quantise16(y, clips_max, clip, clip_max, &sb);
     if (!live || slot < 0 || slot >= a.num_slots) return;
     const int64_t off = slot & ((1 << a.page_shift) - 1), ph = (slot >> a.page_shift) * a.kv_heads + head;
     *reinterpret_cast<uint4*>((kind == kKey ? a.k_codes : a.v_codes) + (((ph << a.page_shift) + off) * D + b * 32 + 16 * kg)) = codes;
@@ -261,8 +266,14 @@ append_many(const AppendArgs a) {
     const int tiles = (a.M + 31) >> 5, tile0 = (int)(blockIdx.x / head_groups) * a.tiles_wg, tile1 = min(tiles, tile0 + a.tiles_wg);
     const uint4* op = kind == kQuery ? a.tq : kind == kKey ? a.tk : a.tv;
     const int blk0 = (kind == kQuery ? head / a.group : head) * kBlocks;
-    const float* clip = kind == kKey ? a.clip_k : a.clip_v;
-    const float* clip_max = kind == kKey ? a.clip_k_max : a.clip_v_max;
+    const float* clips = kind == kKey ? a.clip_k : a.clip_v;
+    const float* clips_max = kind == kKey ? a.clip_k_max : a.clip_v_max;
+    float clip[kBlocks], clip_max[kBlocks];                 // scalars
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+        auto scalar = [&](const float* p) { return p && kind != kQuery ? __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(p[blk0 + b]))) : 1.0f; };
+        clip[b] = scalar(clips), clip_max[b] = scalar(clips_max);
+    }
     const XT* src = (kind == kQuery ? static_cast<const XT*>(a.q) : kind == kKey ? static_cast<const XT*>(a.k) : static_cast<const XT*>(a.v)) + (size_t)head * D;
     const int64_t ld = kind == kQuery ? a.ldq : kind == kKey ? a.ldk : a.ldv;
     const bool rotated = a.table && kind != kValue;
@@ -287,27 +298,26 @@ append_many(const AppendArgs a) {
                          :: "v"(voff), "s"(from), "s"(x_lds + (uint32_t)(buf * kTile + i * 1024)) : "memory");
         }
     };
-    // the tile's rows of the table: thread i moves chunks i, i + 256, ... of rotary_dim / 4 a row
-    const int t_chunks = a.table ? a.rotary_dim / 4 : 1;
+    // the tile's rows of the table: thread i moves chunks i % 8, i % 8 + 8, ... of row i / 8
+    const int t_chunks = a.table ? a.rotary_dim / 4 : 0, t_row = threadIdx.x >> 3, t_c = threadIdx.x & 7;
     u32x4 tw[4] = {};
-    int pos[4] = {};
-    auto positions = [&](int tile) {
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const int r = (x * 256 + (int)threadIdx.x) / t_chunks;
-            pos[x] = r < 32 ? a.positions[min(tile * 32 + r, a.M - 1)] : 0;
-        }
-    };
+    int pos = 0;
+    auto positions = [&](int tile) { pos = a.positions[min(tile * 32 + t_row, a.M - 1)]; };
     auto request_table = [&]() {
+        const u32x4* p = reinterpret_cast<const u32x4*>(a.table + (size_t)(pos >= 0 && pos < a.table_rows ? pos : 0) * a.rotary_dim) + t_c;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const int i = x * 256 + (int)threadIdx.x;
-            if (i < 32 * t_chunks)
-                tw[x] = *(reinterpret_cast<const u32x4*>(a.table + (size_t)(pos[x] >= 0 && pos[x] < a.table_rows ? pos[x] : 0) * a.rotary_dim) + i % t_chunks);
-        }
+        for (int x = 0; x < 4; ++x)
+            if (t_c + 8 * x < t_chunks) tw[x] = p[8 * x];
     };
-    // a tile's slots and positions are asked for a tile ahead (the table's positions two): in the loop nothing is waited
-    // for but the one wait at its top
+    // (not __syncthreads, which would also wait for the loads and stores on their way)
+    auto barrier = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    // a tile's slots and positions are asked for a tile ahead (the table's positions two).  Loads and stores are counted
+    // together, in order: the loop waits once, when a tile's results are ready and before they are stored, so that the next
+    // tile's loads have had the arithmetic of this one to arrive and the stores have that of the next one to leave
+    auto landed = [&]() {
+        __builtin_amdgcn_s_waitcnt(0x0F70);                 // vmcnt(0)
+        asm volatile("" ::: "memory");
+    };
     auto slot_of = [&](int tile) { return kind == kQuery ? (int64_t)0 : a.slots[min(tile * 32 + (lane & 31), a.M - 1)]; };
     auto position_of = [&](int tile) { return a.table ? a.positions[min(tile * 32 + (lane & 31), a.M - 1)] : 0; };
     if (a.table) {
@@ -318,27 +328,25 @@ append_many(const AppendArgs a) {
     int64_t next_slot = slot_of(tile0);                     // (every workgroup has a tile)
     int next_pos = position_of(tile0);
     if (busy) request(tile0, 0);
+    landed();
     for (int tile = tile0, buf = 0; tile < tile1; ++tile, buf ^= 1) {
         // opaque here: otherwise every LDS address of a tile is kept in a register of its own across the tiles
         asm volatile("" : "+v"(lane));
+        lane &= 63;                                         // (its range is not known behind that)
         const int l32 = lane & 31, kg = lane >> 5, m = tile * 32 + l32;
-        __builtin_amdgcn_s_waitcnt(0x0F70);                 // vmcnt(0): the tile has landed
-        asm volatile("" ::: "memory");
         const int64_t slot = next_slot;
         const bool there = m < a.M && (!a.table || (next_pos >= 0 && next_pos < a.table_rows));
         const bool live = there && slot >= 0 && slot < a.num_slots;
         if (a.table) {
-            __syncthreads();                                // the last tile's angles have been used
+            barrier();                                      // the last tile's angles have been used
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const int i = x * 256 + (int)threadIdx.x, r = i / t_chunks;
-                if (i < 32 * t_chunks) *reinterpret_cast<u32x4*>(s_t + (at(r, 32) ^ ((i - r * t_chunks) * 16))) = tw[x];
-            }
+            for (int x = 0; x < 4; ++x)
+                if (t_c + 8 * x < t_chunks) *reinterpret_cast<u32x4*>(s_t + (at(t_row, 32) ^ ((t_c + 8 * x) * 16))) = tw[x];
             if (tile + 1 < tile1) {
                 request_table();
                 positions(min(tile + 2, tiles - 1));
             }
-            __syncthreads();
+            barrier();
         }
         if (tile + 1 < tile1) {
             next_slot = slot_of(tile + 1), next_pos = position_of(tile + 1);
@@ -380,6 +388,7 @@ append_many(const AppendArgs a) {
                 }
             }
         };
+        uint32_t scale_bytes = 0;
         auto finish = [&](float (&y)[16], const bf16x8 (&tb)[6], int b) {
             if (op) transform16(y, tb, kSize == 2 && !rotated);
             if (kind == kQuery) {
@@ -387,9 +396,9 @@ append_many(const AppendArgs a) {
                 for (int h = 0; h < 2; ++h) *reinterpret_cast<bf16x8*>(x_at + (own ^ (32 * kSize * b + 16 * h))) = to_bf16(y + 8 * h);
             } else {
                 uint32_t sb;
-                const uint4 codes = quantise16(y, clip, clip_max, blk0 + b, &sb);
+                const uint4 codes = quantise16(y, clips_max, clip[b], clip_max[b], &sb);
+                scale_bytes |= sb << (8 * b);
                 *reinterpret_cast<uint4*>(x_at + (own ^ (32 * kSize * b))) = codes;
-                if (live && kg == 0) (kind == kKey ? a.k_scales : a.v_scales)[((ph * kBlocks + b) << a.page_shift) + off] = (uint8_t)sb;
             }
             __builtin_amdgcn_sched_barrier(0);              // block by block: interleaved, they would not fit the registers
         };
@@ -431,6 +440,9 @@ append_many(const AppendArgs a) {
             pair(t[2], t[3], 2, 3);
         }
         wave_lds_order();
+        landed();
+        // (used here, or the compiler would wait for them behind the stores)
+        asm volatile("" : "+v"(next_slot), "+v"(next_pos), "+v"(tw[0]), "+v"(tw[1]), "+v"(tw[2]), "+v"(tw[3]), "+v"(pos));
         // rows out: lane l moves chunk l % kQCh (kCCh) of row l / kQCh, from where its lane put it; what the row's own lane
         // knows about it is shuffled over
         if (kind == kQuery) {
@@ -441,6 +453,9 @@ append_many(const AppendArgs a) {
                 if (__shfl((int)there, r)) store16_through(a.q_out + (size_t)(tile * 32 + r) * a.ldq_out + (size_t)head * D + c * 8, v);
             }
         } else {
+            if (live && kg == 0)
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) (kind == kKey ? a.k_scales : a.v_scales)[((ph * kBlocks + b) << a.page_shift) + off] = (uint8_t)(scale_bytes >> (8 * b));
             const int64_t to = live ? ((ph << a.page_shift) + off) * D : -1;
 #pragma unroll
             for (int i = 0; i < kCCh / 2; ++i) {
