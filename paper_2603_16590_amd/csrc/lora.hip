@@ -110,7 +110,8 @@ constexpr int shrink_lds() { return W * (Piece<XT, 16>::kBytes + Piece<uint16_t,
 // h[m][j] = sum over a part of K of X[m][k] A_a[j][k].  A workgroup takes (16 rows, adapters of a slot, part of K); its W
 // waves split the part into W ranges and are added through LDS in wave order.  A wave works on 64 k at a time, out of
 // its own pieces of LDS, while the next 64 are on their way to registers.  Bound: the stream of X (many rows), the latency
-// of index, loads and sums in a row (few).
+// of index, loads and sums in a row (few).  Measured: 4096 rows of K 4096 in bf16, rank 32: 12 us (2.8 TB/s); 32 rows with 16
+// adapters of rank 16: 4.5 us.
 template <typename XT, int JT, int W>
 __global__ void __launch_bounds__(64 * W)
 shrink_kernel(const LoraArgs a) {
@@ -206,7 +207,9 @@ struct Cols {
 // adapter's B for its columns in registers (G groups of 32 rank indexes) until a row wants another adapter.  Column t of the C
 // instructions of a tile is column C i + t in lane (i, g) = (l % 16, l / 16): a lane ends with C neighbouring columns of
 // rows 4g .. 4g + 3, 16 lanes with a contiguous piece of a row.  h is taken as three bf16 terms (24 bits).  The sums start
-// from base, which is requested a tile ahead.  Bound: base in, out out.
+// from base, which is requested a tile ahead.  Bound: base in, out out.  Measured: 4096 x 14336 in bf16, rank 32: 62.6 us
+// (3.8 TB/s in and out; with 8 columns to a lane the same in half the waves, 16 registers spilled and 78 us in three quarters);
+// 32 x 4096 with 16 adapters: 7.6 us.
 template <typename YT, int G, int P>
 __global__ void __launch_bounds__(256, P > 1 ? (G == 4 ? 1 : 2) : G == 1 ? 4 : 2)
 expand_kernel(const LoraArgs a) {
@@ -230,8 +233,14 @@ expand_kernel(const LoraArgs a) {
     float s = 0.0f;
     int loaded = -1;
     V next[4];
-    if (tile0 < tile1) request(tile0, next);
-    int mine_next = tile0 < tile1 ? adapters(tile0) : -2;
+    if (slot == 0) request(tile0, next);
+    int mine_next = adapters(tile0);
+    if (slot > 0) {                                         // (one tile, which may have fewer adapters than there are slots)
+        bool any = false;
+        for_adapters(a, mine_next, slot, [&](int) { any = true; });
+        if (!any) return;
+        request(tile0, next);
+    }
     for (int tile = tile0; tile < tile1; ++tile) {
         const int row0 = tile * 16, mine = mine_next;
         V now[4];
@@ -316,26 +325,31 @@ expand_kernel(const LoraArgs a) {
     }
 }
 
-// How a call is cut.  Few rows (decoding): a tile's adapters are spread over workgroups, and K is cut into parts so that
-// there are about two workgroups to a compute unit if the rows of a tile share one or two adapters, at least 256 to a part.
-// Many rows: whole rows of X to a workgroup, so that h is written and read once.
+// How a call is cut.  Up to 512 rows a tile's adapters are spread over workgroups, 64 / tiles at most.  Up to 64 rows, K is cut
+// into parts so that there are about two workgroups of four waves to a compute unit if the rows of a tile share one or two
+// adapters, at least 256 to a part.  More rows: workgroups of eight waves, and parts only as long as there is a compute unit
+// for each, of 2048, or of 4096 where N is wide (each part of h is read again for every 256 columns): K 14336 with 16 x 4096
+// at 256 rows 14.6 us in one part, 9.3 in four, 12.2 in eight of the small kind; K 4096 with 32 x 14336 at 256 rows
+// 14.1 in one part, 15.9 in two, 26 in eight; at 64 rows the small kind 15.5 (K 14336, rank 64) beside 24.9.
 struct Plan {
     int tiles, slots, parts, part_k;
     bool few;
 };
-Plan plan(int M, int K, int adapters) {
+Plan plan(int M, int K, int N, int adapters) {
     Plan p;
-    p.few = M <= 512;
+    p.few = M <= 64;
     p.tiles = (int)(((int64_t)M + 15) / 16);
-    p.slots = p.few ? 64 / p.tiles : 1;
+    p.slots = M <= 512 ? 64 / p.tiles : 1;
     if (p.slots > 16) p.slots = 16;
     if (p.slots - 1 > adapters) p.slots = adapters + 1;     // (rows without an adapter count as one)
-    if (p.slots < 1) p.slots = 1;
-    int n = p.few ? 256 / p.tiles : 1;
-    if (n > (K + 255) / 256) n = (K + 255) / 256;
-    if (n > kMaxParts) n = kMaxParts;
-    p.part_k = (int)((((int64_t)K + n - 1) / n + 511) & ~int64_t(511));     // whole steps of 64 for each of 8 waves
-    if (n > 1) p.part_k = ((K + n - 1) / n + 255) & ~255;
+    const int least = p.few ? 256 : N / 2 > K ? 4096 : 2048, most = p.few ? kMaxParts : 4;
+    int n = 256 / p.tiles;
+    if (n > (K + least - 1) / least) n = (K + least - 1) / least;
+    if (n > most) n = most;
+    if (n < 1) n = 1;
+    // whole steps of 64 for each of a workgroup's waves
+    const int step = p.few && n > 1 ? 256 : 512;
+    p.part_k = ((K + n - 1) / n + step - 1) / step * step;
     p.parts = (K + p.part_k - 1) / p.part_k;
     return p;
 }
@@ -358,15 +372,20 @@ hipError_t shrink(const LoraArgs& a, bool few, unsigned grid, int dev, hipStream
 
 template <typename YT, int G>
 hipError_t launch_expand(LoraArgs& a, const Plan& p, hipStream_t stream) {
-    // tiles of a workgroup: as many as leave eight workgroups to a compute unit, within 2^23 workgroups
     a.groups_n = (int)(((int64_t)a.N + 255) / 256);
-    const int64_t units = (int64_t)p.tiles * p.slots * a.groups_n;
-    int64_t t = p.few ? 1 : (int64_t)p.tiles * a.groups_n / 2048;
+    // a tile's adapters: spread over workgroups while there are fewer than four to a compute unit (333 rows in runs of 20
+    // beside 3616 x 5000: 14.4 us with two to a tile, 16.9 with one; those that find no adapter are not free: 128 rows with
+    // one adapter to a tile beside 4096 x 4096, this kernel 7.5 us with eight to a tile, 4.8 with one)
+    const int64_t wide = (int64_t)p.tiles * a.groups_n;
+    a.slots = wide >= 1024 ? 1 : (int)(1024 / wide < p.slots ? 1024 / wide : p.slots);
+    // tiles of a workgroup: as many as leave eight workgroups to a compute unit, within 2^23 workgroups
+    int64_t t = a.slots > 1 ? 1 : wide / 2048;
     if (t > 32) t = 32;
-    if (t < units / (1 << 22) + 1) t = units / (1 << 22) + 1;
+    if (t < wide / (1 << 22) + 1) t = wide / (1 << 22) + 1;
     a.tile_rows = (int)t;
-    const unsigned grid = (unsigned)((p.tiles + t - 1) / t * p.slots * a.groups_n);
-    if (p.parts > 1) expand_kernel<YT, G, kMaxParts><<<grid, 256, 0, stream>>>(a);
+    const unsigned grid = (unsigned)((p.tiles + t - 1) / t * a.slots * a.groups_n);
+    if (p.parts > 4) expand_kernel<YT, G, kMaxParts><<<grid, 256, 0, stream>>>(a);
+    else if (p.parts > 1) expand_kernel<YT, G, 4><<<grid, 256, 0, stream>>>(a);
     else expand_kernel<YT, G, 1><<<grid, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
@@ -379,8 +398,8 @@ hipError_t expand(LoraArgs& a, const Plan& p, hipStream_t stream) {
 
 }  // namespace
 
-size_t lora_workspace_bytes(int M, int K, int, int rank, int adapters) {
-    return M > 0 ? (size_t)plan(M, K, adapters).parts * M * rank * 4 : 0;
+size_t lora_workspace_bytes(int M, int K, int N, int rank, int adapters) {
+    return M > 0 ? (size_t)plan(M, K, N, adapters).parts * M * rank * 4 : 0;
 }
 
 hipError_t launch_lora_add(const void* X, batq_dtype xdtype, int M, int K, int64_t ldx, const void* A, const void* B,
@@ -388,7 +407,7 @@ hipError_t launch_lora_add(const void* X, batq_dtype xdtype, int M, int K, int64
                            int64_t ldb, void* out, int64_t ldo, batq_dtype ydtype, void* workspace, hipStream_t stream) {
     int dev = 0;
     if (hipError_t e = hipGetDevice(&dev); e != hipSuccess) return e;
-    const Plan p = plan(M, K, adapters);
+    const Plan p = plan(M, K, N, adapters);
     LoraArgs a = {};
     a.X = X, a.A = static_cast<const uint16_t*>(A), a.B = static_cast<const uint16_t*>(B), a.scales = scales, a.index = index;
     a.base = base, a.out = out, a.h = static_cast<float*>(workspace), a.ldx = ldx, a.ldb = ldb, a.ldo = ldo;
