@@ -830,9 +830,16 @@ struct Plan {
 // Part length of attend_few: enough workgroups for four to a compute unit where there are tokens for it, at least 256
 // tokens (two blocks for each wave) and at most 1024, so that the longest of ragged sequences does not outlast the others
 // (64 sequences of up to 8192 tokens: parts of 512 and 1024 tokens 35 us, of 256 45 us; 4 of up to 131072: 74 us, 80 us).
-// attend_many cuts the tokens only where its row tiles are fewer than the compute units, into as many parts as make about
-// one workgroup to each.  A window bounds the tokens that matter: of a sequence of few rows, of a tile of many.
-Plan plan(int group, int kv_heads, int batch, int total_q, int max_q, int max_kv, int window, int compute_units) {
+// A window bounds the tokens that matter: of a sequence of few rows, of a tile of many.
+// attend_many cuts the tokens only where its row tiles are fewer than the compute units (one workgroup to each at a time), into the
+// number of parts with the least estimated time, in units of a block of 64 tokens (about 2 us): whole rounds over the card
+// where the tiles are alike (1.1: a round of exactly all compute units has come out as two), half of that and a part at the
+// end where they are not (lengths, the triangle of a prompt); 4 blocks for what a part begins and ends with, 4 for the
+// join, 10 MB of partial results written and read to a block.  Beside parts that make one workgroup, or two, to a compute
+// unit: 4 sequences of 256 queries and 8192 tokens, 32 and 8 heads of 128 channels 216 us (273, 216); 8 of 128 and 2048 79
+// (80, 89); 2 of 512 and 4096, 8 heads and 1, 44 (43, 60); 9 ragged sequences of up to 500 queries and 10000 tokens with a
+// window of 4096, 16 heads and 2 of 64, 37 (45, 37).
+Plan plan(int head_dim, int group, int kv_heads, int batch, int total_q, int max_q, int max_kv, int window, int compute_units) {
     Plan p = {};
     const int64_t rows = (int64_t)max_q * group;
     p.many = rows > 32;
@@ -855,13 +862,20 @@ Plan plan(int group, int kv_heads, int batch, int total_q, int max_q, int max_kv
         // sum of ceil(rows / 256) over sequences of more than few_rows rows, rows / (few_rows + 1) of them at most
         const int64_t all = (int64_t)total_q * group, longer = all / (p.few_rows + 1);
         p.many_tiles = (int)(all / kManyRows + (longer < batch ? longer : batch));
-        const int64_t groups = (int64_t)((int64_t)total_q * group / kManyRows + 1) * kv_heads;
-        const int64_t tokens = span(kManyRows / group + 1);
-        int64_t n = compute_units / groups;
-        if (n > (tokens + 511) / 512) n = (tokens + 511) / 512;     // at least 512 tokens to a part
-        if (n > 1) {
-            p.many_len = (int)(((tokens + n - 1) / n + 63) & ~int64_t(63));
-            p.many_parts = (int)((tokens + 63 + p.many_len - 1) / p.many_len);
+        const bool same = (int64_t)batch * max_q == total_q;   // every sequence has max_q queries
+        const int64_t tiles = same ? batch * ((rows + kManyRows - 1) / kManyRows) : all / kManyRows + (longer < batch ? longer : batch) / 2;
+        const int64_t units = (tiles < 1 ? 1 : tiles) * kv_heads, tokens = span(kManyRows / group + 1);
+        const bool even = same && max_q <= max_kv / 4;
+        double best = 0;
+        for (int n = 1; n == 1 || (units < compute_units && n <= 64 && n * 256 <= tokens); ++n) {
+            const int64_t len = ((tokens + n - 1) / n + 63) & ~int64_t(63);
+            const double load = (double)units * n / compute_units;
+            double cost = (even ? ceil(1.1 * load) : 0.5 * load + 1.0) * (double)(len / 64 + 4);
+            if (n > 1) cost += 4.0 + (double)total_q * group * kv_heads * n * head_dim * 8e-7;
+            if (n > 1 && cost >= best) continue;
+            best = cost;
+            p.many_len = n > 1 ? (int)len : 1 << 30;
+            p.many_parts = n > 1 ? (int)((tokens + 63 + len - 1) / len) : 1;
         }
     }
     return p;
@@ -903,7 +917,7 @@ size_t part_bytes(const Plan& p, const batq_paged_cache& c, int q_heads, int bat
 
 size_t paged_attention_workspace_bytes(const batq_paged_cache& c, int q_heads, int batch, int total_q, int max_q, int max_kv,
                                        int compute_units) {
-    return part_bytes(plan(q_heads / c.kv_heads, c.kv_heads, batch, total_q, max_q, max_kv, 0, compute_units), c, q_heads, batch, total_q);
+    return part_bytes(plan(c.head_dim, q_heads / c.kv_heads, c.kv_heads, batch, total_q, max_q, max_kv, 0, compute_units), c, q_heads, batch, total_q);
 }
 
 hipError_t launch_paged_attention(const batq_paged_cache& c, const batq_paged_batch& b, const void* q, int64_t ldq,
@@ -914,9 +928,9 @@ hipError_t launch_paged_attention(const batq_paged_cache& c, const batq_paged_ba
     const int cus = e == hipSuccess ? device_compute_units(dev, &e) : 0;
     if (e != hipSuccess) return e;
     // a window's plan where it needs no more room than the plan without one, which is what the workspace is sized for
-    const Plan full = plan(q_heads / c.kv_heads, c.kv_heads, b.batch, b.total_q, b.max_q, b.max_kv, 0, cus);
+    const Plan full = plan(c.head_dim, q_heads / c.kv_heads, c.kv_heads, b.batch, b.total_q, b.max_q, b.max_kv, 0, cus);
     // (without causal a window has no upper end)
-    Plan p = plan(q_heads / c.kv_heads, c.kv_heads, b.batch, b.total_q, b.max_q, b.max_kv, causal ? window : 0, cus);
+    Plan p = plan(c.head_dim, q_heads / c.kv_heads, c.kv_heads, b.batch, b.total_q, b.max_q, b.max_kv, causal ? window : 0, cus);
     if (part_bytes(p, c, q_heads, b.batch, b.total_q) > part_bytes(full, c, q_heads, b.batch, b.total_q)) p = full;
     AttnArgs a = {};
     a.q = static_cast<const uint16_t*>(q), a.ldq = ldq, a.ldo = ldo, a.out = static_cast<uint16_t*>(out), a.lse = lse;
