@@ -51,8 +51,8 @@
  *     valid until the stream has passed the call.  The caller owns every tensor it
  *     passes; the library owns only what is inside its handles.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).
- *     Online calls (batq_quantize_act*, batq_gemm_*, batq_linear*, the cache calls) only
- *     enqueue kernels: no host synchronisation, no allocation, no state kept between
+ *     Online calls (batq_quantize_act*, batq_gemm_*, batq_linear*, the cache calls,
+ *     batq_paged_attention, batq_lora_add) only enqueue kernels: no host synchronisation, no allocation, no state kept between
  *     calls.  Which kernels run is a function of the call's arguments and the device
  *     alone, so a call gives the same bits on any stream, eagerly or while the stream
  *     is captured into a graph.  Scratch memory comes from the caller (`workspace`).
@@ -76,7 +76,8 @@ typedef enum {
     BATQ_ERR_NULL = 1,        /* a required pointer is NULL                                  */
     BATQ_ERR_SHAPE = 2,       /* K % 32 != 0, a size <= 0, or a leading dimension too small  */
     BATQ_ERR_DTYPE = 3,       /* unknown batq_dtype                                          */
-    BATQ_ERR_UNSUPPORTED = 4, /* (g_outer, g_inner) not one of (4,8), (8,4), or unknown form    */
+    BATQ_ERR_UNSUPPORTED = 4, /* (g_outer, g_inner) not one of (4,8), (8,4), or unknown form;
+                                 a paged cache's head_dim not 64 or 128                      */
     BATQ_ERR_SINGULAR = 5,    /* G or some P_k is not invertible                             */
     BATQ_ERR_CLIP_RANGE = 6,  /* a clip ratio is not in (0, 1]                               */
     BATQ_ERR_WORKSPACE = 7,   /* workspace smaller than batq_linear_workspace()              */
