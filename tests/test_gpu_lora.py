@@ -204,3 +204,15 @@ def test_binding_refuses_what_does_not_fit(B):
             B.batq_lora_add(**{**dict(X=X, A=A, B=Bm, index=index, base=base), **bad})
     with pytest.raises(B.BatqError):
         B.batq_lora_add(X, A, Bm, index, base, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("M,K,N,r,n,pattern,xdt", [(100, 4128, 72, 24, 3, "mixed", "bf16"), (70, 8992, 50, 8, 70, "each", "f32"), (513, 4096, 65, 40, 5, "mixed", "bf16"),
+                                                   (65, 2080, 300, 128, 4, "runs", "bf16"), (64, 2080, 300, 72, 4, "mixed", "f32"), (200, 16384, 33, 16, 2, "mixed", "bf16")])
+def test_long_contractions(B, M, K, N, r, n, pattern, xdt):
+    """K in two to eight parts, on both sides of 64 and of 512 rows."""
+    import torch
+    rng = np.random.default_rng(M + K)
+    X, Xv, A, Av, Bm, Bv, base, basev, scales, index = problem(rng, M, K, N, r, n, xdt, "f32", pattern)
+    out = B.batq_lora_add(X, A, Bm, dev(index), base, scales=dev(scales))
+    torch.cuda.synchronize()
+    check(out.cpu().numpy().astype(np.float64), Xv, Av, Bv, basev, scales, index, "f32")
