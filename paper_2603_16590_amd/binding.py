@@ -683,25 +683,34 @@ def _scratch(t, dev: int) -> int:
 class PagedCache:
     """The arrays of a paged MXFP8 key/value cache (batq_paged_cache): ``k_codes`` and ``v_codes``
     [pages, kv_heads, page_size, head_dim], ``k_scales`` and ``v_scales`` [pages, kv_heads, head_dim / 32, page_size],
-    uint8.  Allocated on the current device, or ``tensors`` in that order: codes, scales of the keys, of the values."""
+    uint8.  Allocated on the current device, or ``tensors`` in that order: codes, scales of the keys, of the values.
+    What it holds is fixed when it is made (calls pass the arrays' addresses): attributes cannot be assigned, and a call on a
+    cache whose arrays' memory has been moved or freed since is refused.  Other arrays: another PagedCache."""
 
     def __init__(self, num_pages: int, page_size: int, kv_heads: int, head_dim: int, tensors=None):
         import torch
-        self.num_pages, self.page_size, self.kv_heads, self.head_dim = num_pages, page_size, kv_heads, head_dim
         if not lib.batq_kv_paged_code_bytes(num_pages, page_size, kv_heads, head_dim):
             raise ValueError(f"a paged cache of {num_pages} pages of {page_size} tokens, {kv_heads} heads of {head_dim} channels is not supported")
         codes, scales = (num_pages, kv_heads, page_size, head_dim), (num_pages, kv_heads, head_dim // 32, page_size)
         if tensors is None:
             tensors = [torch.zeros(s, dtype=torch.uint8, device="cuda") for s in (codes, scales, codes, scales)]
-        self.device = _device()
+        device = _device()
         for t, shape in zip(tensors, (codes, scales, codes, scales)):
-            _list(t, torch.uint8, shape, self.device, "cache")
-        self.k_codes, self.k_scales, self.v_codes, self.v_scales = tensors
-        self._d = _CacheDesc(num_pages, page_size, kv_heads, head_dim, *(t.data_ptr() for t in tensors))
+            _list(t, torch.uint8, shape, device, "cache")
+        k_codes, k_scales, v_codes, v_scales = tensors
+        at = [t.data_ptr() for t in tensors]
+        self.__dict__.update(num_pages=num_pages, page_size=page_size, kv_heads=kv_heads, head_dim=head_dim, device=device,
+                             k_codes=k_codes, k_scales=k_scales, v_codes=v_codes, v_scales=v_scales,
+                             _at=at, _d=_CacheDesc(num_pages, page_size, kv_heads, head_dim, *at))
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{name}: a paged cache holds the arrays and sizes that it was made with")
 
     def desc(self, dev: int):
         if dev != self.device:
             raise _elsewhere(self.k_codes, dev, "cache")
+        if self._at != [self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(), self.v_scales.data_ptr()]:
+            raise ValueError("cache: the memory of its arrays has been moved or freed since it was made")
         return C.byref(self._d)
 
 

@@ -127,3 +127,30 @@ def test_sizes_past_a_launch_are_refused(B):
     for kw in (dict(M=(1 << 26) + 1), dict(K=(1 << 26) + 32, ldx=(1 << 26) + 32), dict(N=(1 << 26) + 1, ldb=(1 << 26) + 1, ldo=(1 << 26) + 1)):
         assert lora(B, **kw) == 2, kw
         assert B.lib.batq_lora_workspace(*[{**dict(M=4, K=64, N=40, rank=8, n=2), **kw}[k] for k in ("M", "K", "N", "rank", "n")]) == 0
+
+
+def test_a_cache_does_not_keep_addresses_that_are_gone(B, monkeypatch):
+    """Calls pass the addresses of a cache's arrays: it cannot be given others, and arrays whose memory has been moved or freed are refused."""
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(B.binding, "_device", lambda: -1)   # (the arrays are host memory here, which is device -1 to torch)
+    shapes = ((4, 2, 16, 64), (4, 2, 2, 16)) * 2
+    arrays = [torch.zeros(s, dtype=torch.uint8) for s in shapes]
+    c = B.PagedCache(4, 16, 2, 64, tensors=arrays)
+    assert c.k_codes is arrays[0] and c.v_scales is arrays[3] and (c.num_pages, c.page_size, c.kv_heads, c.head_dim) == (4, 16, 2, 64)
+    d = c.desc(-1)._obj
+    assert [d.k_codes, d.k_scales, d.v_codes, d.v_scales] == [t.data_ptr() for t in arrays]
+    for name, value in (("k_codes", arrays[2]), ("k_scales", arrays[3]), ("v_codes", arrays[0]), ("v_scales", arrays[1]), ("num_pages", 8),
+                        ("page_size", 32), ("kv_heads", 1), ("head_dim", 128), ("device", 0)):
+        with pytest.raises(AttributeError):
+            setattr(c, name, value)
+    assert c.desc(-1)._obj.k_codes == arrays[0].data_ptr()
+    for i in range(4):
+        fresh = [torch.zeros(s, dtype=torch.uint8) for s in shapes]
+        c = B.PagedCache(4, 16, 2, 64, tensors=fresh)
+        c.desc(-1)
+        if i % 2:
+            fresh[i].untyped_storage().resize_(0)           # freed
+        else:
+            fresh[i].data = torch.zeros(shapes[i], dtype=torch.uint8)       # moved
+        with pytest.raises(ValueError):
+            c.desc(-1)
