@@ -441,6 +441,7 @@ batq_status batq_kv_paged_append(const batq_paged_cache* cache, const batq_trans
  *   o_i = sum_t p_t v_t,  p = softmax over the visible t of scale * (q_i . k_t),  lse_i = log sum_t exp(scale * (q_i . k_t))
  * with keys and values as the cache holds them.  A query at position i of its sequence sees t <= i if causal != 0 (else
  * every t < kv_len) and, with window > 0, only t > i - window.  A query that sees nothing gets zeros and lse -infinity.
+ *   scale       positive, below 2e38
  *   cu_q        DEVICE int32 [batch + 1], not decreasing, from 0 to at most total_q (rows of q, out and lse); rows of no
  *               sequence are left as they are
  *   kv_len      DEVICE int32 [batch]

@@ -953,7 +953,8 @@ batq_status batq_paged_attention(const batq_paged_cache* cache, const batq_paged
     if (batq_status st = check_attention_dims(cache, q_heads, b->batch, b->total_q, b->max_q, b->max_kv); st != BATQ_OK) return st;
     if (batq_status st = check_paged_cache(cache); st != BATQ_OK) return st;
     const int64_t width = (int64_t)q_heads * cache->head_dim;
-    if (ldq < width || ldo < width || b->table_width < 0 || window < 0 || !(scale > 0.0f) || !(scale < 3.0e38f)) return BATQ_ERR_SHAPE;
+    if (ldq < width || ldo < width || b->table_width < 0 || window < 0) return BATQ_ERR_SHAPE;
+    if (!(scale > 0.0f) || !(scale < 2.0e38f)) return BATQ_ERR_SHAPE;          // (times log2 e it is finite)
     if (b->batch == 0 || b->total_q == 0 || b->max_q == 0) return BATQ_OK;
     if (!q || !out || !b->cu_q || !b->kv_len || (!b->page_table && b->table_width > 0)) return BATQ_ERR_NULL;
     if (!aligned16(q) || !aligned16(out) || (ldq * 2) % 16 != 0 || (ldo * 2) % 16 != 0 || q == out ||

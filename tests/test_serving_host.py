@@ -154,3 +154,10 @@ def test_a_cache_does_not_keep_addresses_that_are_gone(B, monkeypatch):
             fresh[i].data = torch.zeros(shapes[i], dtype=torch.uint8)       # moved
         with pytest.raises(ValueError):
             c.desc(-1)
+
+
+def test_scales_that_overflow_are_refused(B):
+    """The kernels keep scores in units of ln 2: a scale whose product with log2 e is infinite would make a score of zero NaN."""
+    for scale in (2.5e38, 2.9e38, 3.4e38):
+        assert attend(B, cache(), scale=scale) == 2
+    assert attend(B, cache(), scale=1.9e38, q=None) == 1    # (the next check)
