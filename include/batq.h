@@ -486,8 +486,9 @@ batq_status batq_paged_attention(const batq_paged_cache* cache, const batq_paged
  * X, A, B 16-byte aligned, row pitch of X a multiple of 16 bytes; base and out aligned to their elements.  The products
  * are carried to fp32 accuracy (the intermediate X A^T is not rounded to 16 bits).
  * M, K and N are at most 2^26.  Outputs that depend on an infinite or NaN input or weight are infinite or NaN.
- *   workspace  DEVICE, 256-byte aligned, batq_lora_workspace() bytes; its contents need not be cleared.  Calls that may
- *              run at the same time need one each. */
+ *   workspace  DEVICE, 256-byte aligned; its contents need not be cleared.  Calls that may run at the same time need one
+ *              each.  batq_lora_workspace() bytes are enough for every call of at most that M, K and rank, any N and adapters
+ *              (fewer rows alone can take more room than many: they are computed in more parts). */
 size_t batq_lora_workspace(int M, int K, int N, int rank, int adapters);
 batq_status batq_lora_add(const void* X, batq_dtype xdtype, int M, int K, int64_t ldx, const void* A, const void* B,
                           int N, int rank, int adapters, const float* scales, const int32_t* index, const void* base,

@@ -780,6 +780,7 @@ def batq_paged_attention(cache: PagedCache, q, cu_q, kv_len, page_table, max_q: 
 
 
 def batq_lora_workspace(M: int, K: int, N: int, rank: int, adapters: int) -> int:
+    """Bytes of scratch that every batq_lora_add call of at most this M, K and rank can run with."""
     return int(lib.batq_lora_workspace(M, K, N, rank, adapters))
 
 

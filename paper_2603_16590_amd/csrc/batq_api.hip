@@ -980,7 +980,7 @@ static batq_status check_lora_dims(int M, int K, int N, int rank, int adapters) 
 }
 
 size_t batq_lora_workspace(int M, int K, int N, int rank, int adapters) {
-    return check_lora_dims(M, K, N, rank, adapters) == BATQ_OK ? batq::lora_workspace_bytes(M, K, N, rank, adapters) : 0;
+    return check_lora_dims(M, K, N, rank, adapters) == BATQ_OK ? batq::lora_workspace_bytes(M, K, rank) : 0;
 }
 
 batq_status batq_lora_add(const void* X, batq_dtype xdtype, int M, int K, int64_t ldx, const void* A, const void* B,
@@ -999,7 +999,7 @@ batq_status batq_lora_add(const void* X, batq_dtype xdtype, int M, int K, int64_
         (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || X == out || (base == out && ldb != ldo))
         return BATQ_ERR_SHAPE;
     if (batq_status st = check_device(); st != BATQ_OK) return st;
-    const size_t need = batq::lora_workspace_bytes(M, K, N, rank, adapters);
+    const size_t need = batq::lora_parts_bytes(M, K, N, rank, adapters);
     if (need > workspace_bytes || (need > 0 && !workspace)) return BATQ_ERR_WORKSPACE;
     BATQ_HIP(batq::launch_lora_add(X, xdtype, M, K, ldx, A, B, N, rank, adapters, scales, index, base, ldb, out, ldo, ydtype,
                                    workspace, static_cast<hipStream_t>(stream)));

@@ -136,7 +136,8 @@ size_t paged_attention_workspace_bytes(const batq_paged_cache& c, int q_heads, i
 hipError_t launch_paged_attention(const batq_paged_cache& c, const batq_paged_batch& b, const void* q, int64_t ldq,
                                   int q_heads, float scale, bool causal, int window, void* out, int64_t ldo, float* lse,
                                   void* workspace, hipStream_t stream);
-size_t lora_workspace_bytes(int M, int K, int N, int rank, int adapters);
+size_t lora_parts_bytes(int M, int K, int N, int rank, int adapters);       // what a call takes of its workspace
+size_t lora_workspace_bytes(int M, int K, int rank);
 hipError_t launch_lora_add(const void* X, batq_dtype xdtype, int M, int K, int64_t ldx, const void* A, const void* B,
                            int N, int rank, int adapters, const float* scales, const int32_t* index, const void* base,
                            int64_t ldb, void* out, int64_t ldo, batq_dtype ydtype, void* workspace, hipStream_t stream);

@@ -398,8 +398,25 @@ hipError_t expand(LoraArgs& a, const Plan& p, hipStream_t stream) {
 
 }  // namespace
 
-size_t lora_workspace_bytes(int M, int K, int N, int rank, int adapters) {
+size_t lora_parts_bytes(int M, int K, int N, int rank, int adapters) {
     return M > 0 ? (size_t)plan(M, K, N, adapters).parts * M * rank * 4 : 0;
+}
+
+// Fewer rows can take more room, in more parts: the most that any call of at most M rows over at most K with at most `rank`
+// takes.  The number of parts (at most that of plan() in front of its rounding, with the shorter least length of wide and narrow
+// N) falls with the number of 16-row tiles only, so the most rows for each number are looked at.
+size_t lora_workspace_bytes(int M, int K, int rank) {
+    auto most = [&](int rows, int least, int parts) {
+        const int n = (int)(((int64_t)K + least - 1) / least);
+        return (size_t)(n < parts ? n : parts) * (rows < M ? rows : M);
+    };
+    size_t h = most(64, 256, kMaxParts);
+    if (M > 64)
+        for (int n = 4; n >= 1; --n) {
+            const size_t x = most(n == 1 ? M : 256 / n * 16, 2048, n);
+            if (x > h) h = x;
+        }
+    return M > 0 ? h * rank * 4 : 0;
 }
 
 hipError_t launch_lora_add(const void* X, batq_dtype xdtype, int M, int K, int64_t ldx, const void* A, const void* B,

@@ -216,3 +216,23 @@ def test_long_contractions(B, M, K, N, r, n, pattern, xdt):
     out = B.batq_lora_add(X, A, Bm, dev(index), base, scales=dev(scales))
     torch.cuda.synchronize()
     check(out.cpu().numpy().astype(np.float64), Xv, Av, Bv, basev, scales, index, "f32")
+
+
+def test_one_workspace_serves_every_smaller_call(B):
+    """A workspace sized for the largest call, full of NaN, with calls of fewer rows in more parts."""
+    import torch
+    K, N, r, n = 4096, 72, 16, 3
+    ws = torch.full((B.batq_lora_workspace(3000, K, N, r, n),), 0xFF, dtype=torch.uint8, device="cuda")
+    for M in (3000, 2048, 1024, 513, 65, 64, 17, 1):
+        rng = np.random.default_rng(M)
+        X, Xv, A, Av, Bm, Bv, base, basev, scales, index = problem(rng, M, K, N, r, n, "bf16", "f32", "mixed")
+        out = B.batq_lora_add(X, A, Bm, dev(index), base, scales=dev(scales), workspace=ws)
+        torch.cuda.synchronize()
+        check(out.cpu().numpy().astype(np.float64), Xv, Av, Bv, basev, scales, index, "f32")
+    small = torch.full((B.batq_lora_workspace(64, 8192, N, r, n),), 0xFF, dtype=torch.uint8, device="cuda")
+    for M, k in ((64, 8192), (64, 512), (9, 4096)):
+        rng = np.random.default_rng(M + k)
+        X, Xv, A, Av, Bm, Bv, base, basev, scales, index = problem(rng, M, k, N, r, n, "f32", "bf16", "mixed")
+        out = B.batq_lora_add(X, A, Bm, dev(index), base, scales=dev(scales), workspace=small)
+        torch.cuda.synchronize()
+        check(out.float().cpu().numpy().astype(np.float64), Xv, Av, Bv, basev, scales, index, "bf16")

@@ -161,3 +161,25 @@ def test_scales_that_overflow_are_refused(B):
     for scale in (2.5e38, 2.9e38, 3.4e38):
         assert attend(B, cache(), scale=scale) == 2
     assert attend(B, cache(), scale=1.9e38, q=None) == 1    # (the next check)
+
+
+def lora_parts(M, K, N):
+    """Parts of K that a call of the adapters computes (each takes M x rank floats of its workspace)."""
+    tiles, few = -(-M // 16), M <= 64
+    least, most = (256, 8) if few else (4096 if N // 2 > K else 2048, 4)
+    n = max(1, min(256 // tiles, -(-K // least), most))
+    step = 256 if few and n > 1 else 512
+    return -(-K // (-(-(-(-K // n)) // step) * step))
+
+
+@pytest.mark.parametrize("K", [32, 256, 288, 608, 2048, 2080, 4096, 4128, 8192, 14336, 16384, 1 << 20])
+def test_lora_workspace_of_the_largest_call_is_enough_for_smaller_ones(B, K):
+    """A server sizes its workspace once: fewer rows, a shorter K or a smaller rank never ask for more."""
+    w, before = B.lib.batq_lora_workspace, 0
+    for M in sorted({m + d for m in [1, 16, 32, 48, 64, 128, 512, 1024, 1360, 1376, 2048, 4096, 8192] for d in (-1, 0, 1) if m + d > 0}):
+        got = w(M, K, 64, 16, 2)
+        for N in (64, 1 << 24):
+            assert got == w(M, K, N, 16, 3) and got >= 4 * 16 * M * lora_parts(M, K, N)
+        assert got >= before and w(M, K, 64, 24, 2) >= got and w(M, K + 32, 64, 16, 2) >= got and w(M, K + 2048, 64, 16, 2) >= got
+        assert got <= 4 * 16 * max(M, min(M, 64) * 8, min(M, 1024) * 4, min(M, 1360) * 3, min(M, 2048) * 2)
+        before = got
