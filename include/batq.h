@@ -455,9 +455,10 @@ batq_status batq_kv_paged_append(const batq_paged_cache* cache, const batq_trans
  *               kv_heads, at most 128 query heads to a key head.  Scores, softmax and sums are fp32; the probabilities are multiplied with
  *               the values as bf16 (sequences of few queries: as two bf16 terms).
  *   lse         DEVICE fp32 [total_q][q_heads] or NULL
- *   workspace   DEVICE, 256-byte aligned, batq_paged_attention_workspace() bytes: partial results of long
- *               sequences that are cut into parts.  Its contents need not be cleared.  Calls that may run at the same
- *               time (two streams, two captured graphs) need one each.
+ *   workspace   DEVICE, 256-byte aligned: partial results of long sequences that are cut into parts.  Its contents need not
+ *               be cleared.  Calls that may run at the same time (two streams, two captured graphs) need one each.
+ *               batq_paged_attention_workspace() bytes are enough for every call of at most that batch, total_q, max_q and
+ *               max_kv, with any window (a few sequences are cut into more parts than many, short prompts into more than long)
  * BATQ_ERR_SHAPE: also for batch * kv_heads from 2^19 on, or from 2^24 / (max_kv / 1024 + 2).
  * For queries and keys through batq_kv_paged_append with tk, out is in the basis of tv: batq_transform_apply with
  * BATQ_APPLY_INVERSE takes it back, or T_v^-1 is folded into the output projection offline. */

@@ -746,7 +746,7 @@ def batq_kv_paged_append(cache: PagedCache, k, v, slots, positions=None, q=None,
 
 
 def batq_paged_attention_workspace(cache: PagedCache, q_heads: int, batch: int, total_q: int, max_q: int, max_kv: int) -> int:
-    """Bytes of scratch for batq_paged_attention calls within these bounds on the current device."""
+    """Bytes of scratch that every batq_paged_attention call within these bounds can run with on the current device."""
     return int(lib.batq_paged_attention_workspace(C.byref(cache._d), q_heads, batch, total_q, max_q, max_kv))
 
 

@@ -965,7 +965,7 @@ batq_status batq_paged_attention(const batq_paged_cache* cache, const batq_paged
     if (batq_status st = check_device(); st != BATQ_OK) return st;
     const int cus = current_compute_units();
     if (!cus) return BATQ_ERR_DEVICE;
-    const size_t need = batq::paged_attention_workspace_bytes(*cache, q_heads, b->batch, b->total_q, b->max_q, b->max_kv, cus);
+    const size_t need = batq::paged_attention_part_bytes(*cache, q_heads, b->batch, b->total_q, b->max_q, b->max_kv, cus);
     if (need > workspace_bytes || (need > 0 && !workspace)) return BATQ_ERR_WORKSPACE;
     BATQ_HIP(batq::launch_paged_attention(*cache, *b, q, ldq, q_heads, scale, causal != 0, window, out, ldo, lse, workspace,
                                           static_cast<hipStream_t>(stream)));

@@ -131,6 +131,8 @@ hipError_t launch_kv_paged_append(const batq_paged_cache& c, const batq_transfor
                                   int64_t ldq_out, const void* k, int64_t ldk, const void* v, int64_t ldv,
                                   batq_dtype xdtype, const int32_t* positions, const int64_t* slots, int M,
                                   hipStream_t stream);
+size_t paged_attention_part_bytes(const batq_paged_cache& c, int q_heads, int batch, int total_q, int max_q, int max_kv,
+                                  int compute_units);      // what a call takes of its workspace
 size_t paged_attention_workspace_bytes(const batq_paged_cache& c, int q_heads, int batch, int total_q, int max_q,
                                        int max_kv, int compute_units);
 hipError_t launch_paged_attention(const batq_paged_cache& c, const batq_paged_batch& b, const void* q, int64_t ldq,

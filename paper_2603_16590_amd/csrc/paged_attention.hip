@@ -827,6 +827,19 @@ struct Plan {
     bool few, many;                                         // which kernels run
 };
 
+// Rows x parts that attend_many may be cut into for calls of at most total_q queries and max_kv tokens: what the estimate below
+// asks for, give or take.  It weighs tokens / 64 n blocks of a part against writing n rows' results, which makes n fall
+// with the root of tokens / rows, and rows x parts grow with that of tokens x rows; rows are cut only while there are fewer
+// tiles of them than compute units.  Grows with both arguments, so that a workspace serves smaller calls.
+int64_t many_room(int head_dim, int q_heads, int kv_heads, int64_t total_q, int max_kv, int compute_units) {
+    if (max_kv < 512) return 0;
+    int64_t rows = (int64_t)kManyRows * (compute_units + kv_heads);
+    if (rows > total_q * q_heads) rows = total_q * q_heads;
+    const int64_t all = rows * ((max_kv < 64 * 256 ? max_kv / 256 : 64) + 1);
+    const int64_t most = (int64_t)(sqrt((double)rows * (max_kv + 1024.0)) * (head_dim == 64 ? 22.6 : 16.0));
+    return all < most ? all : most;
+}
+
 // Part length of attend_few: enough workgroups for four to a compute unit where there are tokens for it, at least 256
 // tokens (two blocks for each wave) and at most 1024, so that the longest of ragged sequences does not outlast the others
 // (64 sequences of up to 8192 tokens: parts of 512 and 1024 tokens 35 us, of 256 45 us; 4 of up to 131072: 74 us, 80 us).
@@ -866,16 +879,18 @@ Plan plan(int head_dim, int group, int kv_heads, int batch, int total_q, int max
         const int64_t tiles = same ? batch * ((rows + kManyRows - 1) / kManyRows) : all / kManyRows + (longer < batch ? longer : batch) / 2;
         const int64_t units = (tiles < 1 ? 1 : tiles) * kv_heads, tokens = span(kManyRows / group + 1);
         const bool even = same && max_q <= max_kv / 4;
+        const int64_t room = many_room(head_dim, group * kv_heads, kv_heads, total_q, max_kv, compute_units);
         double best = 0;
         for (int n = 1; n == 1 || (units < compute_units && n <= 64 && n * 256 <= tokens); ++n) {
-            const int64_t len = ((tokens + n - 1) / n + 63) & ~int64_t(63);
+            const int64_t len = ((tokens + n - 1) / n + 63) & ~int64_t(63), parts = n > 1 ? (tokens + 63 + len - 1) / len : 1;
+            if (n > 1 && all * kv_heads * parts > room) continue;
             const double load = (double)units * n / compute_units;
             double cost = (even ? ceil(1.1 * load) : 0.5 * load + 1.0) * (double)(len / 64 + 4);
             if (n > 1) cost += 4.0 + (double)total_q * group * kv_heads * n * head_dim * 8e-7;
             if (n > 1 && cost >= best) continue;
             best = cost;
             p.many_len = n > 1 ? (int)len : 1 << 30;
-            p.many_parts = n > 1 ? (int)((tokens + 63 + len - 1) / len) : 1;
+            p.many_parts = (int)parts;
         }
     }
     return p;
@@ -915,9 +930,27 @@ size_t part_bytes(const Plan& p, const batq_paged_cache& c, int q_heads, int bat
 
 }  // namespace
 
+size_t paged_attention_part_bytes(const batq_paged_cache& c, int q_heads, int batch, int total_q, int max_q, int max_kv,
+                                  int compute_units) {
+    return part_bytes(plan(c.head_dim, q_heads / c.kv_heads, c.kv_heads, batch, total_q, max_q, max_kv, 0, compute_units), c, q_heads, batch, total_q);
+}
+
+// At least the former for every batch, total_q, max_q and max_kv up to the given ones (a few sequences are cut into more parts
+// than many, few rows than a prompt).  attend_few: up to 32 rows of each pair of a sequence and a key head, one part to
+// 256 tokens but at most four to a compute unit (a 64th more: the rounding of their length), or to 1024 tokens; each pair's
+// last part and the one by which a range that starts inside a block can be longer, 1 + 62 / 256, on top.
 size_t paged_attention_workspace_bytes(const batq_paged_cache& c, int q_heads, int batch, int total_q, int max_q, int max_kv,
                                        int compute_units) {
-    return part_bytes(plan(c.head_dim, q_heads / c.kv_heads, c.kv_heads, batch, total_q, max_q, max_kv, 0, compute_units), c, q_heads, batch, total_q);
+    const int64_t rows = (int64_t)max_q * (q_heads / c.kv_heads), pairs = (int64_t)batch * c.kv_heads;
+    int64_t units = 0;
+    if (max_kv > 256 - 63) {
+        int64_t parts = (pairs * max_kv + 255) / 256;
+        if (parts > 4 * compute_units + compute_units / 16 + 1) parts = 4 * compute_units + compute_units / 16 + 1;
+        if (parts < (pairs * max_kv + 1023) / 1024) parts = (pairs * max_kv + 1023) / 1024;
+        units = (parts + pairs + (pairs + 3) / 4) * (rows < 32 ? rows : 32);
+    }
+    if (rows > 32) units += many_room(c.head_dim, q_heads, c.kv_heads, total_q, max_kv, compute_units);
+    return (size_t)units * (c.head_dim + 2) * 4;
 }
 
 hipError_t launch_paged_attention(const batq_paged_cache& c, const batq_paged_batch& b, const void* q, int64_t ldq,

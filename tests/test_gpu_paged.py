@@ -575,6 +575,35 @@ def test_two_attentions_at_once(B):
         assert all(torch.equal(x, y) for x, y in zip(outs, want)), rep
 
 
+def test_workspace_sizes_grow_with_every_bound(B):
+    """A server sizes its workspace once, for its largest batch: no smaller call may ask for more."""
+    rng = np.random.default_rng(20)
+    for D, hq, hkv in ((128, 32, 8), (128, 28, 4), (64, 16, 2), (64, 1, 1), (128, 128, 1), (64, 24, 24)):
+        cache = B.PagedCache(2, 16, hkv, D)
+        size = lambda *a: B.batq_paged_attention_workspace(cache, hq, *a)
+        assert size(1, 8192, 8192, 8192) >= size(1, 1, 1, 8192) and size(5, 5, 1, 8192) >= size(4, 4, 1, 8192)
+        for _ in range(400):
+            big = [int(np.exp(rng.uniform(0, np.log(n)))) for n in (200, 8192, 8192, 200000)]
+            small = [int(rng.integers(1, n + 1)) if rng.random() < 0.7 else n for n in big]
+            assert size(*small) <= size(*big), (small, big)
+
+
+def test_one_workspace_serves_every_smaller_attention(B):
+    """Calls of every kind (a prompt, chunks cut into parts, drafts, single tokens, windows) share the workspace of their bounds."""
+    import torch
+    rng = np.random.default_rng(21)
+    hq, hkv, D, page = 4, 2, 64, 16
+    lens, qs = [6000, 2500, 1700, 900, 300], [1, 40, 3, 9, 300]
+    cache, (kv, vv), qd, q, cu, lens, table, T = attend_case(rng, B, lens, qs, hq, hkv, D, page)
+    ws = torch.full((B.batq_paged_attention_workspace(cache, hq, 5, T, 2500, 8192),), 0xFF, dtype=torch.uint8, device="cuda")
+    for rows, window in (([0, 1, 2, 3, 4], 0), ([0], 0), ([1], 0), ([1], 700), ([2, 3], 0), ([0, 3], 100), ([4], 0), ([1, 4], 0)):
+        sel = np.concatenate([np.arange(cu[b], cu[b + 1]) for b in rows])
+        c = np.concatenate([[0], np.cumsum([cu[b + 1] - cu[b] for b in rows])]).astype(np.int32)
+        part = qd[torch.from_numpy(sel).cuda()].contiguous()
+        got, lse = run_attention(B, cache, part, c, lens[rows], table[rows], len(sel), hq, window=window, workspace=ws)
+        ref.assert_attention(got, lse, ref.attention(kv, vv, q[sel], c, lens[rows], table[rows], page, D ** -0.5, True, window, len(sel)))
+
+
 def test_binding_refuses_what_does_not_fit(B):
     import torch
     cache = B.PagedCache(4, 16, 2, 64)
