@@ -426,7 +426,7 @@ typedef struct {
  *           written).  A token whose position is outside the table is left out: neither cache nor q_out are written.
  *           The slots of a call must differ: what one holds that two tokens were written to is unspecified.
  * q, k, v share xdtype (bf16 or fp32) and may be column ranges of one tensor; all pointers and row pitches are 16-byte
- * aligned (slots 8-byte, positions 4-byte).  q_out must not overlap q.  The products of the transform are carried to
+ * aligned (slots 8-byte, positions 4-byte).  q_out must not overlap q, k or v.  The products of the transform are carried to
  * fp32 accuracy: rotated values are not rounded to 16 bits.  M == 0 is a no-op.  M rounded up to 32, times all heads
  * (queries, keys, values), times head_dim, is less than 2^36.
  * BATQ_ERR_MISMATCH: tk or tv has another width. */

@@ -907,7 +907,8 @@ batq_status batq_kv_paged_append(const batq_paged_cache* cache, const batq_trans
     if (!aligned16(k) || !aligned16(v) || (ldk * size) % 16 != 0 || (ldv * size) % 16 != 0 ||
         (reinterpret_cast<uintptr_t>(slots) & 7u) != 0 || (reinterpret_cast<uintptr_t>(positions) & 3u) != 0)
         return BATQ_ERR_SHAPE;
-    if (q_heads > 0 && (!aligned16(q) || !aligned16(q_out) || (ldq * size) % 16 != 0 || (ldq_out * 2) % 16 != 0 || q == q_out))
+    if (q_heads > 0 && (!aligned16(q) || !aligned16(q_out) || (ldq * size) % 16 != 0 || (ldq_out * 2) % 16 != 0 ||
+                        q_out == q || q_out == k || q_out == v))
         return BATQ_ERR_SHAPE;
     if (batq_status st = check_device(); st != BATQ_OK) return st;
     BATQ_HIP(batq::launch_kv_paged_append(*cache, tk, tv, rope, q, ldq, q_heads, q_out, ldq_out, k, ldk, v, ldv, xdtype,

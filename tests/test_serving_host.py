@@ -183,3 +183,9 @@ def test_lora_workspace_of_the_largest_call_is_enough_for_smaller_ones(B, K):
         assert got >= before and w(M, K, 64, 24, 2) >= got and w(M, K + 32, 64, 16, 2) >= got and w(M, K + 2048, 64, 16, 2) >= got
         assert got <= 4 * 16 * max(M, min(M, 64) * 8, min(M, 1024) * 4, min(M, 1360) * 3, min(M, 2048) * 2)
         before = got
+
+
+def test_queries_are_not_written_over_keys_or_values(B):
+    """Other workgroups may still read them."""
+    for kw in (dict(k=3 * P), dict(v=3 * P)):
+        assert append(B, cache(), q=2 * P, q_heads=2, ldq=128, ldqo=128, q_out=3 * P, **kw) == 2
