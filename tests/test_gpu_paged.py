@@ -575,6 +575,39 @@ def test_two_attentions_at_once(B):
         assert all(torch.equal(x, y) for x, y in zip(outs, want)), rep
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_scale_byte_255_is_nan(B, D):
+    """E8M0 255 is NaN whatever the block's codes are: a key makes the rows that see it NaN, a value its block of 32 channels;
+    where nobody looks it does nothing."""
+    rng = np.random.default_rng(22 + D)
+    page = 16
+    for hq, hkv, lens, qs, window in ((4, 2, [200, 90], [1, 1], 0), (4, 2, [200], [200], 50), (6, 2, [300, 70], [3, 2], 0), (2, 1, [1000], [130], 0)):
+        cache, _, qd, q, cu, lens, table, T = attend_case(rng, B, lens, qs, hq, hkv, D, page)
+        arrays = host(cache)
+        for what in (1, 3):
+            a = [x.copy() for x in arrays]
+            for tok in (int(lens[0]) - 1, int(lens[0]) - 1 - min(60, qs[0])):
+                a[what][table[0, tok // page], hkv - 1, D // 32 - 1, tok % page] = 255
+            broken = B.PagedCache(cache.num_pages, page, hkv, D, tensors=[dev(x) for x in a])
+            with np.errstate(invalid="ignore"):
+                kv, vv = (np.where(np.repeat(x[1].transpose(0, 1, 3, 2), 32, -1) == 255, np.nan, ref.cache_values(*x)) for x in (a[:2], a[2:]))
+                want = ref.attention(kv, vv, q, cu, lens, table, page, D ** -0.5, True, window, T)
+            got, lse = run_attention(B, broken, qd, cu, lens, table, T, hq, window=window)
+            assert np.isnan(want[0]).any() and not np.isnan(want[0]).all()
+            assert np.array_equal(np.isnan(got), np.isnan(want[0])) and np.array_equal(np.isnan(lse), np.isnan(want[1]))
+
+
+@pytest.mark.parametrize("hq,hkv,lens,qs,window", [(128, 1, [300, 40, 1], [1, 3, 1], 0), (100, 1, [200, 1030], [1, 9], 0), (128, 1, [700], [30], 64),
+                                                   (384, 3, [90, 33], [2, 1], 5), (33, 1, [2100], [1], 0)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_of_many_heads_to_a_key_head(B, hq, hkv, lens, qs, window, D):
+    """Groups of 33 to 128 query heads: one token alone is more rows than a tile of the few-row kernel."""
+    rng = np.random.default_rng(hq + sum(lens))
+    cache, (kv, vv), qd, q, cu, lens, table, T = attend_case(rng, B, lens, qs, hq, hkv, D, 32, spare=1)
+    got, lse = run_attention(B, cache, qd, cu, lens, table, T, hq, window=window)
+    ref.assert_attention(got, lse, ref.attention(kv, vv, q, cu, lens, table, 32, D ** -0.5, True, window, T))
+
+
 def test_workspace_sizes_grow_with_every_bound(B):
     """A server sizes its workspace once, for its largest batch: no smaller call may ask for more."""
     rng = np.random.default_rng(20)
