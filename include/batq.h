@@ -394,8 +394,9 @@ batq_status batq_kv_dequantize(const uint8_t* codes, const uint8_t* scales, int6
  * table lists them.  The arrays (DEVICE, caller-owned, 16-byte aligned) hold per page:
  *   codes   [kv_heads][page_size][head_dim] E4M3 bytes, batq_kv_paged_code_bytes() in all
  *   scales  [kv_heads][head_dim / 32][page_size] E8M0 bytes, batq_kv_paged_scale_bytes() in all
- * A block is one token's 32 channels, quantised exactly as batq_kv_append with act_bits 8 does, so a token's bytes do
- * not depend on the call or the order that brought it.  head_dim is 64 or 128, page_size 16, 32, 64, 128 or 256, and
+ * A block is one token's 32 channels, clipped and quantised as batq_kv_append with act_bits 8 does, and a token's bytes do
+ * not depend on the call or the order that brought it.  Without rotation they are batq_kv_append's, except of fp32 input
+ * behind a transform, whose sums are formed in another order there (both to fp32 accuracy).  head_dim is 64 or 128, page_size 16, 32, 64, 128 or 256, and
  * num_pages * page_size may pass 2^31.  The size functions return 0 for invalid arguments. */
 typedef struct {
     int num_pages, page_size, kv_heads, head_dim;

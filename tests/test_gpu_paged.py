@@ -232,6 +232,107 @@ def test_append_of_many_tokens_equals_pieces(B, dtype, D, rot, inter):
             assert np.array_equal(x, y)
 
 
+# Calls past 16 D units of 32 tokens x 32 channels, whose rotations the kernel for many tokens takes: every layout of it (head
+# width, element size), pair distance and direction; 15 heads leave a wave of the last workgroup without one, and 141 tiles of
+# 32 tokens are two for some workgroups, the last one ragged.
+MANY = [
+    # D, rot, interleaved, dtype
+    (64, 64, False, "bf16"), (64, 64, False, "f32"), (64, 32, True, "f32"), (64, 16, True, "bf16"), (64, 0, False, "bf16"), (64, 0, False, "f32"),
+    (128, 64, False, "bf16"), (128, 64, False, "f32"), (128, 128, False, "bf16"), (128, 128, False, "f32"), (128, 128, True, "bf16"),
+    (128, 48, True, "f32"), (128, 0, False, "bf16"), (128, 0, False, "f32"),
+]
+MANY_M, MANY_HQ, MANY_HKV = 4489, 9, 3
+
+
+def many_tokens(D, rot, inter):
+    """Whether the kernel for many tokens takes the call."""
+    return -(-MANY_M // 32) * (MANY_HQ + 2 * MANY_HKV) * (D // 32) > 16 * D and (rot % 64 == 0 or inter)
+
+
+@pytest.mark.parametrize("D,rot,inter,dtype", MANY)
+def test_append_of_many_tokens_is_bit_exact(B, D, rot, inter, dtype):
+    assert many_tokens(D, rot, inter)
+    test_append_without_transforms_is_bit_exact(B, MANY_M, MANY_HQ, MANY_HKV, D, 64, rot, inter, dtype)
+
+
+@pytest.mark.parametrize("D,rot,inter,dtype,form", [(64, 64, False, "bf16", "kron"), (64, 32, True, "f32", "dense"), (64, 0, False, "f32", "kron"), (64, 0, False, "bf16", "dense"),
+                                                    (128, 64, False, "bf16", "dense"), (128, 128, False, "f32", "kron"), (128, 128, True, "bf16", "kron"), (128, 0, False, "bf16", "kron")])
+def test_append_of_many_tokens_with_transforms(B, D, rot, inter, dtype, form):
+    assert many_tokens(D, rot, inter)
+    test_append_with_transforms(B, MANY_M, MANY_HQ, MANY_HKV, D, 32, rot, inter, dtype, form)
+
+
+def other_transforms(B, rng, width):
+    """Clipping alone, and the two-ratio form (minimum and maximum of a block) with dense blocks."""
+    lo, hi = (rng.uniform(0.7, 1.0, width // 32).astype(np.float32) for _ in range(2))
+    blocks = (np.eye(32) + 0.03 * rng.standard_normal((width // 32, 32, 32))).astype(np.float32)
+    return B.Transform(width, None, None, rng.uniform(0.7, 1.0, width // 32).astype(np.float32)), B.Transform.general(width, dense=blocks, clip_min=lo, clip_max=hi)
+
+
+@pytest.mark.parametrize("D,rot,inter,dtype", MANY)
+def test_append_of_many_tokens_equals_short_calls(B, D, rot, inter, dtype):
+    """Calls of 96 tokens go to the kernel for few: the same bytes and queries, with one clip ratio for the keys and two for the values,
+    and the other way round."""
+    import torch
+    assert many_tokens(D, rot, inter)
+    rng = np.random.default_rng(D + rot)
+    M, hq, hkv, page = MANY_M, MANY_HQ, MANY_HKV, 128
+    X = torch.randn((M, (hq + 2 * hkv) * D), device="cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    q, k, v = X.split((hq * D, hkv * D, hkv * D), 1)
+    clip, minmax = other_transforms(B, rng, hkv * D)
+    table = dev(ref.rope_table(4000, rot)) if rot else None
+    slots, pos = torch.randperm(40 * page, device="cuda")[:M], torch.randint(0, 4000, (M,), device="cuda", dtype=torch.int32)
+    slots[[9, M - 1]], slots[4000] = -1, 40 * page
+    if rot:
+        pos[33], pos[M - 2] = -5, 4000
+    for tk, tv in ((clip, minmax), (minmax, clip)):
+        a, b = B.PagedCache(40, page, hkv, D), B.PagedCache(40, page, hkv, D)
+        qa = torch.full((M, hq * D), 7.0, dtype=torch.bfloat16, device="cuda")
+        qb = qa.clone()
+        B.batq_kv_paged_append(a, k, v, slots, pos, q=q, q_out=qa, rope=table, interleaved=inter, tk=tk, tv=tv)
+        for lo in range(0, M, 96):
+            s = slice(lo, min(M, lo + 96))
+            B.batq_kv_paged_append(b, k[s], v[s], slots[s], pos[s], q=q[s], q_out=qb[s], rope=table, interleaved=inter, tk=tk, tv=tv)
+        torch.cuda.synchronize()
+        assert torch.equal(qa, qb)
+        for x, y in zip(host(a), host(b)):
+            assert np.array_equal(x, y)
+
+
+@pytest.mark.parametrize("D,dtype", [(64, "bf16"), (64, "f32"), (128, "bf16")])
+def test_append_of_many_tokens_writes_the_bytes_of_batq_kv_append(B, D, dtype):
+    """Without rotation, one sequence in page order: what the row-window cache holds, with each kind of clipping.  Transformed fp32
+    rows are summed in another order there: 32 products in fp32 are within 32 x 2^-24 of S = sum |x| |T|.  The columns of |T| and
+    |T^-1| add up to less than 3 here and clip ratios are at least 0.7, so S < 9 max |y| < 16 b for a block's bound b < 2^9 units
+    (2^scale): the two sums of an element are less than 2 x 2^-19 x 16 x 2^9 = 2^-5 units apart, and what they are rounded to a step more."""
+    import torch
+    rng = np.random.default_rng(23)
+    M, hkv, page = 10240 if D == 64 else 4700, 4, 16
+    width = hkv * D
+    assert -(-M // 32) * 2 * hkv * (D // 32) > 16 * D
+    X = torch.randn((M, width), device="cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+
+    def values(codes, scales):
+        return codes.view(torch.float8_e4m3fn).double().view(M, -1, 32) * torch.exp2(scales.double() - 127).unsqueeze(-1)
+
+    for n, t in enumerate(other_transforms(B, rng, width) + (_transforms(B, rng, hkv, D, "kron")[0],)):
+        cache = B.PagedCache(-(-M // page), page, hkv, D)
+        B.batq_kv_paged_append(cache, X, X, torch.arange(M, device="cuda"), tk=t, tv=t)
+        codes = torch.zeros(B.batq_code8_bytes(M, width), dtype=torch.uint8, device="cuda")
+        scales = torch.zeros(B.batq_scale_bytes(M, width), dtype=torch.uint8, device="cuda")
+        B.batq_kv_append(t, X, codes, scales, 0, M, bits=8)
+        rc, rs = B.batq_codes8_to_rowmajor(codes, M, width), B.batq_scales_to_rowmajor(scales, M, width)
+        torch.cuda.synchronize()
+        for c, s in ((cache.k_codes, cache.k_scales), (cache.v_codes, cache.v_scales)):
+            c, s = c.permute(0, 2, 1, 3).reshape(-1, width)[:M], s.permute(0, 3, 1, 2).reshape(-1, width // 32)[:M]
+            if dtype == "bf16" or n == 0:                   # (the first one has no blocks)
+                assert torch.equal(c, rc) and torch.equal(s, rs)
+                continue
+            a, b, unit = values(c, s), values(rc, rs), torch.exp2(torch.maximum(s, rs).double() - 127).unsqueeze(-1)
+            step = torch.clamp(torch.exp2(torch.floor(torch.log2(torch.maximum(a.abs(), b.abs()).clamp_min(1e-300))) - 3), min=unit * 2.0 ** -9)
+            assert bool(((a - b).abs() <= step + unit * 2.0 ** -5).all())
+
+
 # ---------------------------------------------------------------------------------------- attention
 def attend_case(rng, B, lens, qs, hq, hkv, D, page, spare=0):
     lens, qs = np.array(lens), np.array(qs)
