@@ -676,6 +676,53 @@ def test_two_attentions_at_once(B):
         assert all(torch.equal(x, y) for x, y in zip(outs, want)), rep
 
 
+def weights_rounded_once(kv, vv, q, cu, lens, table, page, scale, rows):
+    """What attention of these rows (b, i) would give if its weights lost their second bf16 term: [row, head, channel] in 64 bits."""
+    hkv, D = kv.shape[1], kv.shape[3]
+    hq, out = q.shape[1], []
+    for b, i in rows:
+        t = np.arange(lens[b] - (cu[b + 1] - cu[b]) + i + 1)
+        ids = table[b][t // page]
+        for h in range(hq):
+            s = kv[ids, h * hkv // hq, t % page] @ q[cu[b] + i, h] * scale
+            p = np.exp(s - s.max())
+            out.append(o.bf16_round(p.astype(np.float32)).astype(np.float64) @ vv[ids, h * hkv // hq, t % page] / p.sum())
+    return np.array(out).reshape(len(rows), hq, D)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("hq,hkv,lens,qs", [(8, 2, [64, 63, 40, 5], [1] * 4), (8, 2, [70, 64], [3, 4]), (8, 2, [50, 64], [8, 5]), (6, 2, [60, 33, 400], [1, 2, 60]),
+                                            (8, 1, [3000, 61], [1, 1]), (16, 1, [64, 900], [1, 40])])
+def test_weights_of_few_rows_have_two_terms(B, D, hq, hkv, lens, qs):
+    """Sequences of few rows multiply their weights as two bf16 terms.  The bound for that is only tight where the sum nearly cancels
+    (else the rounding of the output hides the second term) and scores are small, so the scale is; among the channels of contexts of
+    up to 70 tokens there are enough of those: the same sums with weights rounded once are outside it."""
+    rng = np.random.default_rng(24 + D + hq + sum(lens))
+    page, scale = 16, D ** -0.5 / 16
+    cache, (kv, vv), qd, q, cu, lens, table, T = attend_case(rng, B, lens, qs, hq, hkv, D, page)
+    got, lse = run_attention(B, cache, qd, cu, lens, table, T, hq, scale=scale)
+    want = ref.attention(kv, vv, q, cu, lens, table, page, scale, True, 0, T)
+    group = hq // hkv
+    most = 32 if max(qs) * group <= 32 else 16              # beside a sequence of more than 32 rows only those of up to 16
+    rows = [(b, i) for b in range(len(qs)) if qs[b] * group <= most for i in range(qs[b])]
+    assert rows
+    sel = np.array([cu[b] + i for b, i in rows])
+    picked = tuple(x[sel] for x in want)
+    ref.assert_attention(got[sel], lse[sel], picked, terms=2)
+    if max(lens[b] for b, _ in rows) <= 70:
+        with pytest.raises(AssertionError):
+            ref.assert_attention(weights_rounded_once(kv, vv, q, cu, lens, table, page, scale, rows), None, picked, terms=2)
+
+
+@pytest.mark.parametrize("lens,qs,hq,hkv,D,page,window", [c for c in ATTEND if max(c[1]) * (c[2] // c[3]) <= 32])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_of_few_rows_to_two_terms(B, lens, qs, hq, hkv, D, page, window, causal):
+    rng = np.random.default_rng(25 + sum(lens) + hq)
+    cache, (kv, vv), qd, q, cu, lens, table, T = attend_case(rng, B, lens, qs, hq, hkv, D, page)
+    got, lse = run_attention(B, cache, qd, cu, lens, table, T, hq, causal=causal, window=window)
+    ref.assert_attention(got, lse, ref.attention(kv, vv, q, cu, lens, table, page, D ** -0.5, causal, window, T), terms=2)
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_scale_byte_255_is_nan(B, D):
     """E8M0 255 is NaN whatever the block's codes are: a key makes the rows that see it NaN, a value its block of 32 channels;
