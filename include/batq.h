@@ -454,12 +454,16 @@ batq_status batq_kv_paged_append(const batq_paged_cache* cache, const batq_trans
  * too; a query that sees a NaN key gets NaN, and of a value that is not finite in bf16 the channels that hold it.
  *   q, out      bf16, total_q x q_heads * head_dim, 16-byte aligned rows, not overlapping; q_heads a multiple of
  *               kv_heads, at most 128 query heads to a key head.  Scores, softmax and sums are fp32; the probabilities are multiplied with
- *               the values as bf16 (sequences of few queries: as two bf16 terms).
+ *               the values as bf16, 2^-8 relative at most, or as two bf16 terms, 2^-16, for sequences of few rows (queries times
+ *               heads of a group): at most 32, or 16 in a call whose max_q allows more than 32
  *   lse         DEVICE fp32 [total_q][q_heads] or NULL
  *   workspace   DEVICE, 256-byte aligned: partial results of long sequences that are cut into parts.  Its contents need not
  *               be cleared.  Calls that may run at the same time (two streams, two captured graphs) need one each.
  *               batq_paged_attention_workspace() bytes are enough for every call of at most that batch, total_q, max_q and
  *               max_kv, with any window (a few sequences are cut into more parts than many, short prompts into more than long)
+ * Sequences of few rows are cut into parts for idle compute units, the others only as far as their rows do not fill the card: one
+ * with many rows (a draft under many query heads to a key head) over a context much longer than the others' is better
+ * served by a call of its own (16 queries over 131072 tokens beside a prompt of 8192: 3.8 ms together, 0.7 in two calls).
  * BATQ_ERR_SHAPE: also for batch * kv_heads from 2^19 on, or from 2^24 / (max_kv / 1024 + 2).
  * For queries and keys through batq_kv_paged_append with tk, out is in the basis of tv: batq_transform_apply with
  * BATQ_APPLY_INVERSE takes it back, or T_v^-1 is folded into the output projection offline. */
