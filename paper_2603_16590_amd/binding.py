@@ -684,7 +684,7 @@ class PagedCache:
     """The arrays of a paged MXFP8 key/value cache (batq_paged_cache): ``k_codes`` and ``v_codes``
     [pages, kv_heads, page_size, head_dim], ``k_scales`` and ``v_scales`` [pages, kv_heads, head_dim / 32, page_size],
     uint8.  Allocated on the current device, or ``tensors`` in that order: codes, scales of the keys, of the values.
-    What it holds is fixed when it is made (calls pass the arrays' addresses): attributes cannot be assigned, and a call on a
+    What it holds is fixed when it is made (calls pass the arrays' addresses): arrays and sizes cannot be assigned, and a call on a
     cache whose arrays' memory has been moved or freed since is refused.  Other arrays: another PagedCache."""
 
     def __init__(self, num_pages: int, page_size: int, kv_heads: int, head_dim: int, tensors=None):
@@ -703,8 +703,12 @@ class PagedCache:
                              k_codes=k_codes, k_scales=k_scales, v_codes=v_codes, v_scales=v_scales,
                              _at=at, _d=_CacheDesc(num_pages, page_size, kv_heads, head_dim, *at))
 
+    _HELD = frozenset(("num_pages", "page_size", "kv_heads", "head_dim", "device", "k_codes", "k_scales", "v_codes", "v_scales", "_at", "_d"))
+
     def __setattr__(self, name, value):
-        raise AttributeError(f"{name}: a paged cache holds the arrays and sizes that it was made with")
+        if name in self._HELD:
+            raise AttributeError(f"{name}: a paged cache holds the arrays and sizes that it was made with")
+        object.__setattr__(self, name, value)
 
     def desc(self, dev: int):
         if dev != self.device:

@@ -189,3 +189,15 @@ def test_queries_are_not_written_over_keys_or_values(B):
     """Other workgroups may still read them."""
     for kw in (dict(k=3 * P), dict(v=3 * P)):
         assert append(B, cache(), q=2 * P, q_heads=2, ldq=128, ldqo=128, q_out=3 * P, **kw) == 2
+
+
+def test_a_cache_can_carry_what_a_program_attaches(B, monkeypatch):
+    """Only the arrays and sizes are fixed."""
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(B.binding, "_device", lambda: -1)
+    c = B.PagedCache(4, 16, 2, 64, tensors=[torch.zeros(s, dtype=torch.uint8) for s in ((4, 2, 16, 64), (4, 2, 2, 16)) * 2])
+    c.layer = 3
+    c.layer += 1
+    assert c.layer == 4
+    with pytest.raises(AttributeError):
+        c._at = []
