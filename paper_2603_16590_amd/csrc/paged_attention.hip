@@ -833,14 +833,17 @@ struct Plan {
 // Rows x parts that attend_many may be cut into for calls of at most total_q queries and max_kv tokens: what the estimate below
 // asks for, give or take.  It weighs tokens / 64 n blocks of a part against writing n rows' results, which makes n fall
 // with the root of tokens / rows, and rows x parts grow with that of tokens x rows; rows are cut only while there are fewer
-// tiles of them than compute units.  Grows with both arguments, so that a workspace serves smaller calls.
+// tiles of them than compute units.  Never more than 2^20, sixteen tiles to a compute unit (thousands of rows over contexts from
+// 131072 tokens on would be cut further: to 0.94 of the estimated time at best up to 2^20 tokens).  Grows with both arguments, so
+// that a workspace serves smaller calls.
 int64_t many_room(int head_dim, int q_heads, int kv_heads, int64_t total_q, int max_kv, int compute_units) {
     if (max_kv < 512) return 0;
     int64_t rows = (int64_t)kManyRows * (compute_units + kv_heads);
     if (rows > total_q * q_heads) rows = total_q * q_heads;
     const int64_t all = rows * ((max_kv < 64 * 256 ? max_kv / 256 : 64) + 1);
     const int64_t most = (int64_t)(sqrt((double)rows * (max_kv + 1024.0)) * (head_dim == 64 ? 22.6 : 16.0));
-    return all < most ? all : most;
+    const int64_t least = all < most ? all : most;
+    return least < (1 << 20) ? least : 1 << 20;
 }
 
 // Part length of attend_few: enough workgroups for four to a compute unit where there are tokens for it, at least 256

@@ -723,6 +723,16 @@ def test_attention_of_few_rows_to_two_terms(B, lens, qs, hq, hkv, D, page, windo
     ref.assert_attention(got, lse, ref.attention(kv, vv, q, cu, lens, table, page, D ** -0.5, causal, window, T), terms=2)
 
 
+def test_workspace_of_long_contexts_stays_in_bounds(B):
+    """Partial results are a tradeoff of a few blocks of tokens against writing them: never more than 2^20 rows x parts of a call's
+    sequences of many rows, and 32 rows x a part for 1024 tokens (at least four to a compute unit) of those of few."""
+    for D, hq, hkv in ((128, 32, 8), (64, 16, 2), (128, 128, 1)):
+        cache = B.PagedCache(2, 16, hkv, D)
+        for max_kv in (8192, 131072, 1 << 20, 1 << 24):
+            few = 32 * (max(hkv * max_kv // 1024, 5 * 256) + 2 * hkv)
+            assert B.batq_paged_attention_workspace(cache, hq, 1, 8192, 8192, max_kv) <= ((1 << 20) + few) * (D + 2) * 4
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_scale_byte_255_is_nan(B, D):
     """E8M0 255 is NaN whatever the block's codes are: a key makes the rows that see it NaN, a value its block of 32 channels;
