@@ -396,8 +396,8 @@ batq_status batq_kv_dequantize(const uint8_t* codes, const uint8_t* scales, int6
  *   scales  [kv_heads][head_dim / 32][page_size] E8M0 bytes, batq_kv_paged_scale_bytes() in all
  * A block is one token's 32 channels, clipped and quantised as batq_kv_append with act_bits 8 does, and a token's bytes do
  * not depend on the call or the order that brought it.  Without rotation they are batq_kv_append's, except of fp32 input
- * behind a transform, whose sums are formed in another order there (both to fp32 accuracy).  head_dim is 64 or 128, page_size 16, 32, 64, 128 or 256, and
- * num_pages * page_size may pass 2^31.  The size functions return 0 for invalid arguments. */
+ * behind a transform, whose sums are formed in another order there (both to fp32 accuracy).  head_dim is 64 or 128,
+ * page_size 16, 32, 64, 128 or 256, and num_pages * page_size may pass 2^31.  The size functions return 0 for invalid arguments. */
 typedef struct {
     int num_pages, page_size, kv_heads, head_dim;
     uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
@@ -455,7 +455,7 @@ batq_status batq_kv_paged_append(const batq_paged_cache* cache, const batq_trans
  *   q, out      bf16, total_q x q_heads * head_dim, 16-byte aligned rows, not overlapping; q_heads a multiple of
  *               kv_heads, at most 128 query heads to a key head.  Scores, softmax and sums are fp32; the probabilities are multiplied with
  *               the values as bf16, 2^-8 relative at most, or as two bf16 terms, 2^-16, for sequences of few rows (queries times
- *               heads of a group): at most 32, or 16 in a call whose max_q allows more than 32
+ *               heads of a group): all up to 32 where max_q allows no more, else those of up to 16 in a call of several sequences
  *   lse         DEVICE fp32 [total_q][q_heads] or NULL
  *   workspace   DEVICE, 256-byte aligned: partial results of long sequences that are cut into parts.  Its contents need not
  *               be cleared.  Calls that may run at the same time (two streams, two captured graphs) need one each.
