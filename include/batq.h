@@ -52,7 +52,7 @@
  *     passes; the library owns only what is inside its handles.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).
  *     Online calls (batq_quantize_act*, batq_gemm_*, batq_linear*, the cache calls,
- *     batq_paged_attention, batq_lora_add) only enqueue kernels: no host synchronisation, no allocation, no state kept between
+ *     batq_paged_attention*, batq_kv_paged_*, batq_lora_add) only enqueue kernels: no host synchronisation, no allocation, no state kept between
  *     calls.  Which kernels run is a function of the call's arguments and the device
  *     alone, so a call gives the same bits on any stream, eagerly or while the stream
  *     is captured into a graph.  Scratch memory comes from the caller (`workspace`).
@@ -478,6 +478,61 @@ size_t batq_paged_attention_workspace(const batq_paged_cache* cache, int q_heads
 batq_status batq_paged_attention(const batq_paged_cache* cache, const batq_paged_batch* b, const void* q, int64_t ldq,
                                  int q_heads, float scale, int causal, int window, void* out, int64_t ldo, float* lse,
                                  void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------
+ * The cache in 4 bits, and kept to a budget.
+ * cache_bits is the width of a cache's codes: 8 as above, or 4 (else BATQ_ERR_UNSUPPORTED).  A cache of 4 bits holds MXFP4:
+ *   codes   [kv_heads][page_size][head_dim / 2] bytes a page, channel 2 j of a token in bits 3:0 of its byte j, channel 2 j + 1 in
+ *           bits 7:4; batq_kv_paged_code_bytes_ex() in all.  Scales as in a cache of 8 bits.
+ * A block is clipped and quantised as batq_kv_append with act_bits 4 does.  All that is said above of the append and of the attention
+ * holds for either width; the plain calls are these with cache_bits 8, and a workspace serves both.  No code of 4 bits is NaN: of
+ * a NaN block the scale byte is 255. */
+size_t batq_kv_paged_code_bytes_ex(int num_pages, int page_size, int kv_heads, int head_dim, int cache_bits);
+batq_status batq_kv_paged_append_ex(const batq_paged_cache* cache, int cache_bits, const batq_transform* tk,
+                                    const batq_transform* tv, const batq_rope* rope, const void* q, int64_t ldq, int q_heads,
+                                    void* q_out, int64_t ldq_out, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                    batq_dtype xdtype, const int32_t* positions, const int64_t* slots, int M, void* stream);
+batq_status batq_paged_attention_ex(const batq_paged_cache* cache, int cache_bits, const batq_paged_batch* b, const void* q,
+                                    int64_t ldq, int q_heads, float scale, int causal, int window, void* out, int64_t ldo,
+                                    float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* What each cached token has received of the attention.  For the batch, queries, scale, causal and window of an attention call
+ * and the lse that it returned, each key head h and token t of a sequence:
+ *   w[h][t] = sum of exp(scale * (q_i . k_t) - lse_i) over the queries i that see t and the query heads that read h
+ *   score   DEVICE fp32 [num_pages][kv_heads][page_size], laid out as the cache's pages: a token's place is set to w, or with
+ *           add != 0 to what it held plus w.  The queries' own tokens (the last cu_q[b + 1] - cu_q[b] of a sequence) are new: their
+ *           places are always set, so that pages need not be cleared.  Places that hold no token are left as they are.
+ *   lse     DEVICE fp32 [total_q][q_heads]; a row with -infinity (it saw nothing) adds nothing
+ * A batch whose queries are fewer than those of the attention (a prompt's last ones) has their rows alone in q and lse.  max_q and max_kv
+ * bound what is served as there; q is read alone.  Sums are fp32, in an order that depends on the arguments alone.  A NaN score comes from
+ * a NaN lse, or from a key that is NaN.  The tokens of a page that several sequences of a call share get the sum of one of them.
+ *   workspace   DEVICE, 256-byte aligned, its contents need not be cleared, one for calls that may run at the same time each;
+ *               batq_kv_paged_score_workspace() bytes are enough for every call of at most that batch, total_q, max_q and max_kv
+ * BATQ_ERR_SHAPE: also for batch * kv_heads * (max_kv / 256 + 1) from 2^24 on. */
+size_t batq_kv_paged_score_workspace(const batq_paged_cache* cache, int q_heads, int batch, int total_q, int max_q, int max_kv);
+batq_status batq_kv_paged_score(const batq_paged_cache* cache, int cache_bits, const batq_paged_batch* b, const void* q,
+                                int64_t ldq, int q_heads, float scale, int causal, int window, const float* lse, float* score,
+                                int add, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Eviction by score.  Of every sequence and key head n = min(kv_len[b], budget) tokens are kept: the first `first` and the last `last`
+ * of them all (first + last <= budget) and those with the largest scores between (of equal ones the earlier; NaN, and tokens of pages
+ * that do not exist, count as the smallest).  They move, in their order, to places 0 .. n - 1 of the pages out_table[b][0 ..]:
+ * keys, values, scales and scores, byte for byte.  Every sequence moves, the short ones whole; pages of page_table are only read, so
+ * they may be shared between sequences (a common prefix), and are the caller's to free afterwards.
+ *   out_table  DEVICE int32 [batch][out_width], out_width * page_size >= min(budget, max_kv, table_width * page_size); no page of it may be
+ *              listed twice or be among those of page_table (what such pages hold then is unspecified)
+ *   keep       DEVICE int32 [batch][kv_heads][budget], out: the kept tokens' former places, ascending, then -1
+ *   new_len    DEVICE int32 [batch], out: n; not kv_len itself
+ *   kv_len, page_table, max_kv   as for the attention; nothing in the lists is trusted
+ * Keys stay rotated by the positions that they were appended at, which the next append goes on counting from; a window of
+ * later attention calls counts places.  A token's new place differs from head to head.
+ *   workspace  as above; batq_kv_paged_evict_workspace() bytes are enough for every call of at most that batch, max_kv and budget
+ * BATQ_ERR_SHAPE: also for batch * kv_heads from 2^22 on, or from 2^24 / (min(budget, max_kv) / 64 + 1). */
+size_t batq_kv_paged_evict_workspace(const batq_paged_cache* cache, int batch, int max_kv, int budget);
+batq_status batq_kv_paged_evict(const batq_paged_cache* cache, int cache_bits, float* score, const int32_t* kv_len,
+                                const int32_t* page_table, int table_width, const int32_t* out_table, int out_width, int batch,
+                                int max_kv, int budget, int first, int last, int32_t* keep, int32_t* new_len, void* workspace,
+                                size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------
  * Low-rank adapters of many requests beside a shared projection:

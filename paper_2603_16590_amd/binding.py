@@ -80,6 +80,13 @@ SYMBOLS = {
     "batq_kv_paged_append": (_i, [_vp, _vp, _vp, _vp, _vp, _i64, _i, _vp, _i64, _vp, _i64, _vp, _i64, _i, _vp, _vp, _i, _vp]),
     "batq_paged_attention_workspace": (_sz, [_vp, _i, _i, _i, _i, _i]),
     "batq_paged_attention": (_i, [_vp, _vp, _vp, _i64, _i, C.c_float, _i, _i, _vp, _i64, _vp, _vp, _sz, _vp]),
+    "batq_kv_paged_code_bytes_ex": (_sz, [_i, _i, _i, _i, _i]),
+    "batq_kv_paged_append_ex": (_i, [_vp, _i, _vp, _vp, _vp, _vp, _i64, _i, _vp, _i64, _vp, _i64, _vp, _i64, _i, _vp, _vp, _i, _vp]),
+    "batq_paged_attention_ex": (_i, [_vp, _i, _vp, _vp, _i64, _i, C.c_float, _i, _i, _vp, _i64, _vp, _vp, _sz, _vp]),
+    "batq_kv_paged_score_workspace": (_sz, [_vp, _i, _i, _i, _i, _i]),
+    "batq_kv_paged_score": (_i, [_vp, _i, _vp, _vp, _i64, _i, C.c_float, _i, _i, _vp, _vp, _i, _vp, _sz, _vp]),
+    "batq_kv_paged_evict_workspace": (_sz, [_vp, _i, _i, _i]),
+    "batq_kv_paged_evict": (_i, [_vp, _i, _vp, _vp, _vp, _i, _vp, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _sz, _vp]),
     "batq_lora_workspace": (_sz, [_i, _i, _i, _i, _i]),
     "batq_lora_add": (_i, [_vp, _i, _i, _i, _i64, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _i64, _vp, _i64, _i, _vp, _sz, _vp]),
 }
@@ -621,7 +628,7 @@ def batq_linear_ex(t: Transform, w: Weight, X, act_bits: int = 4, row_scale=None
     return Y
 
 
-# ---- serving: paged 8-bit cache, attention over it, low-rank adapters
+# ---- serving: paged cache, attention over it, scores and eviction of its tokens, low-rank adapters
 class _CacheDesc(C.Structure):
     """batq_paged_cache of include/batq.h."""
     _fields_ = [("num_pages", _i), ("page_size", _i), ("kv_heads", _i), ("head_dim", _i),
@@ -681,17 +688,17 @@ def _scratch(t, dev: int) -> int:
 
 
 class PagedCache:
-    """The arrays of a paged MXFP8 key/value cache (batq_paged_cache): ``k_codes`` and ``v_codes``
-    [pages, kv_heads, page_size, head_dim], ``k_scales`` and ``v_scales`` [pages, kv_heads, head_dim / 32, page_size],
-    uint8.  Allocated on the current device, or ``tensors`` in that order: codes, scales of the keys, of the values.
+    """The arrays of a paged MXFP8 (``bits`` 8) or MXFP4 (4) key/value cache (batq_paged_cache): ``k_codes`` and ``v_codes``
+    [pages, kv_heads, page_size, head_dim], of 4 bits head_dim / 2, ``k_scales`` and ``v_scales`` [pages, kv_heads,
+    head_dim / 32, page_size], uint8.  Allocated on the current device, or ``tensors`` in that order: codes, scales of the keys, of the values.
     What it holds is fixed when it is made (calls pass the arrays' addresses): arrays and sizes cannot be assigned, and a call on a
     cache whose arrays' memory has been moved or freed since is refused.  Other arrays: another PagedCache."""
 
-    def __init__(self, num_pages: int, page_size: int, kv_heads: int, head_dim: int, tensors=None):
+    def __init__(self, num_pages: int, page_size: int, kv_heads: int, head_dim: int, tensors=None, bits: int = 8):
         import torch
-        if not lib.batq_kv_paged_code_bytes(num_pages, page_size, kv_heads, head_dim):
-            raise ValueError(f"a paged cache of {num_pages} pages of {page_size} tokens, {kv_heads} heads of {head_dim} channels is not supported")
-        codes, scales = (num_pages, kv_heads, page_size, head_dim), (num_pages, kv_heads, head_dim // 32, page_size)
+        if not lib.batq_kv_paged_code_bytes_ex(num_pages, page_size, kv_heads, head_dim, bits):
+            raise ValueError(f"a paged cache of {num_pages} pages of {page_size} tokens, {kv_heads} heads of {head_dim} channels in {bits} bits is not supported")
+        codes, scales = (num_pages, kv_heads, page_size, head_dim * bits // 8), (num_pages, kv_heads, head_dim // 32, page_size)
         if tensors is None:
             tensors = [torch.zeros(s, dtype=torch.uint8, device="cuda") for s in (codes, scales, codes, scales)]
         device = _device()
@@ -699,11 +706,11 @@ class PagedCache:
             _list(t, torch.uint8, shape, device, "cache")
         k_codes, k_scales, v_codes, v_scales = tensors
         at = [t.data_ptr() for t in tensors]
-        self.__dict__.update(num_pages=num_pages, page_size=page_size, kv_heads=kv_heads, head_dim=head_dim, device=device,
+        self.__dict__.update(num_pages=num_pages, page_size=page_size, kv_heads=kv_heads, head_dim=head_dim, bits=bits, device=device,
                              k_codes=k_codes, k_scales=k_scales, v_codes=v_codes, v_scales=v_scales,
                              _at=at, _d=_CacheDesc(num_pages, page_size, kv_heads, head_dim, *at))
 
-    _HELD = frozenset(("num_pages", "page_size", "kv_heads", "head_dim", "device", "k_codes", "k_scales", "v_codes", "v_scales", "_at", "_d"))
+    _HELD = frozenset(("num_pages", "page_size", "kv_heads", "head_dim", "bits", "device", "k_codes", "k_scales", "v_codes", "v_scales", "_at", "_d"))
 
     def __setattr__(self, name, value):
         if name in self._HELD:
@@ -743,7 +750,7 @@ def batq_kv_paged_append(cache: PagedCache, k, v, slots, positions=None, q=None,
             q_out = torch.empty((M, q_heads * D), dtype=torch.bfloat16, device=q.device)
         ldq_out = _rows(q_out, M, q_heads * D, torch.bfloat16, dev, "q_out")
         p_q, p_q_out = q.data_ptr(), q_out.data_ptr()
-    _check(lib.batq_kv_paged_append(cache.desc(dev), None if tk is None else tk.handle, None if tv is None else tv.handle, r, p_q,
+    _check(lib.batq_kv_paged_append_ex(cache.desc(dev), cache.bits, None if tk is None else tk.handle, None if tv is None else tv.handle, r, p_q,
                                     ldq, q_heads, p_q_out, ldq_out, k.data_ptr(), ldk, v.data_ptr(), ldv, _dtype_code(k), p_pos,
                                     p_slots, M, torch._C._cuda_getCurrentRawStream(dev)), "batq_kv_paged_append")
     return q_out
@@ -775,12 +782,79 @@ def batq_paged_attention(cache: PagedCache, q, cu_q, kv_len, page_table, max_q: 
         workspace = torch.empty((max(n, 16),), dtype=torch.uint8, device=q.device)
     b = _PagedBatch(_list(cu_q, torch.int32, (batch + 1,), dev, "cu_q"), _list(kv_len, torch.int32, (batch,), dev, "kv_len"),
                     _list(page_table, torch.int32, (batch, table_width), dev, "page_table"), batch, table_width, T, max_q, max_kv)
-    _check(lib.batq_paged_attention(cache.desc(dev), C.byref(b), q.data_ptr(), ldq, q_heads, D ** -0.5 if scale is None else scale,
+    _check(lib.batq_paged_attention_ex(cache.desc(dev), cache.bits, C.byref(b), q.data_ptr(), ldq, q_heads, D ** -0.5 if scale is None else scale,
                                     causal, window, out.data_ptr(), ldo,
                                     None if lse is None else _list(lse, torch.float32, (T, q_heads), dev, "lse"),
                                     _scratch(workspace, dev), workspace.nbytes, torch._C._cuda_getCurrentRawStream(dev)),
            "batq_paged_attention")
     return out
+
+
+def batq_kv_paged_score_workspace(cache: PagedCache, q_heads: int, batch: int, total_q: int, max_q: int, max_kv: int) -> int:
+    """Bytes of scratch that every batq_kv_paged_score call within these bounds can run with on the current device."""
+    return int(lib.batq_kv_paged_score_workspace(C.byref(cache._d), q_heads, batch, total_q, max_q, max_kv))
+
+
+def _score_array(score, cache: PagedCache, dev: int) -> int:
+    import torch
+    return _list(score, torch.float32, (cache.num_pages, cache.kv_heads, cache.page_size), dev, "score")
+
+
+def batq_kv_paged_score(cache: PagedCache, q, lse, score, cu_q, kv_len, page_table, max_q: int, max_kv: int,
+                        scale: Optional[float] = None, causal: bool = True, window: int = 0, add: bool = False, workspace=None):
+    """What each cached token receives of the attention of the batch (q, lists, scale, causal, window as in
+    batq_paged_attention; lse: fp32 [total_q, q_heads], as it returned it): the softmax weights summed over the queries and the
+    query heads of a key head, into ``score`` (fp32 [pages, kv_heads, page_size]).  add: to what the tokens there have, except the
+    queries' own, which are new.  Returns score."""
+    import torch
+    if q.dim() != 2 or page_table.dim() != 2:
+        raise ValueError("expected q [total_q, q_heads * head_dim] and page_table [batch, width]")
+    dev, D = _device(), cache.head_dim
+    T, width = q.shape
+    batch, table_width = page_table.shape
+    q_heads = width // D
+    ldq = _rows(q, T, q_heads * D, torch.bfloat16, dev, "q")
+    if workspace is None:
+        n = batq_kv_paged_score_workspace(cache, q_heads, batch, T, max_q, max_kv)
+        workspace = torch.empty((max(n, 16),), dtype=torch.uint8, device=q.device)
+    b = _PagedBatch(_list(cu_q, torch.int32, (batch + 1,), dev, "cu_q"), _list(kv_len, torch.int32, (batch,), dev, "kv_len"),
+                    _list(page_table, torch.int32, (batch, table_width), dev, "page_table"), batch, table_width, T, max_q, max_kv)
+    _check(lib.batq_kv_paged_score(cache.desc(dev), cache.bits, C.byref(b), q.data_ptr(), ldq, q_heads, D ** -0.5 if scale is None else scale,
+                                   causal, window, _list(lse, torch.float32, (T, q_heads), dev, "lse"), _score_array(score, cache, dev), add,
+                                   _scratch(workspace, dev), workspace.nbytes, torch._C._cuda_getCurrentRawStream(dev)), "batq_kv_paged_score")
+    return score
+
+
+def batq_kv_paged_evict_workspace(cache: PagedCache, batch: int, max_kv: int, budget: int) -> int:
+    """Bytes of scratch that every batq_kv_paged_evict call within these bounds can run with on the current device."""
+    return int(lib.batq_kv_paged_evict_workspace(C.byref(cache._d), batch, max_kv, budget))
+
+
+def batq_kv_paged_evict(cache: PagedCache, score, kv_len, page_table, out_table, max_kv: int, budget: int, first: int = 0,
+                        last: int = 0, keep=None, new_len=None, workspace=None):
+    """Keep, of each sequence (kv_len: int32 [batch], page_table: int32 [batch, width]) and key head, the ``first`` tokens, the
+    ``last`` ones and those with the largest scores between them, ``budget`` in all, and move them in their order to the pages of
+    out_table (int32 [batch, out width], none of them in use).  Returns (keep, new_len): int32 [batch, kv_heads, budget] former
+    places of the kept tokens, then -1; int32 [batch] lengths."""
+    import torch
+    if page_table.dim() != 2 or out_table.dim() != 2:
+        raise ValueError("expected page_table [batch, width] and out_table [batch, out width]")
+    dev = _device()
+    (batch, table_width), out_width = page_table.shape, out_table.shape[1]
+    if keep is None:
+        keep = torch.empty((batch, cache.kv_heads, budget), dtype=torch.int32, device=page_table.device)
+    if new_len is None:
+        new_len = torch.empty((batch,), dtype=torch.int32, device=page_table.device)
+    if workspace is None:
+        n = batq_kv_paged_evict_workspace(cache, batch, max_kv, budget)
+        workspace = torch.empty((max(n, 16),), dtype=torch.uint8, device=page_table.device)
+    _check(lib.batq_kv_paged_evict(cache.desc(dev), cache.bits, _score_array(score, cache, dev), _list(kv_len, torch.int32, (batch,), dev, "kv_len"),
+                                   _list(page_table, torch.int32, (batch, table_width), dev, "page_table"), table_width,
+                                   _list(out_table, torch.int32, (batch, out_width), dev, "out_table"), out_width, batch, max_kv, budget,
+                                   first, last, _list(keep, torch.int32, (batch, cache.kv_heads, budget), dev, "keep"),
+                                   _list(new_len, torch.int32, (batch,), dev, "new_len"), _scratch(workspace, dev), workspace.nbytes,
+                                   torch._C._cuda_getCurrentRawStream(dev)), "batq_kv_paged_evict")
+    return keep, new_len
 
 
 def batq_lora_workspace(M: int, K: int, N: int, rank: int, adapters: int) -> int:

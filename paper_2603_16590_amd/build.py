@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbatq.so")
 CEILINGS = os.path.join(HERE, "batq_ceilings")     # standalone tool: measured chip ceilings
 SOURCES = ["batq_api.hip", "quant_act.hip", "prep_weight.hip", "gemm_mxfp4.hip", "kv_cache.hip",
-           "paged_append.hip", "paged_attention.hip", "lora.hip"]
+           "paged_append.hip", "paged_attention.hip", "paged_score.hip", "paged_evict.hip", "lora.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -854,7 +854,9 @@ batq_status batq_row_rms_scale(const void* X, batq_dtype xdtype, int M, int K, i
     return BATQ_OK;
 }
 
-// ---- paged 8-bit cache
+// ---- paged cache
+static batq_status check_cache_bits(int bits) { return bits == 4 || bits == 8 ? BATQ_OK : BATQ_ERR_UNSUPPORTED; }
+
 static batq_status check_paged_dims(int num_pages, int page_size, int kv_heads, int head_dim) {
     if (head_dim != 64 && head_dim != 128) return BATQ_ERR_UNSUPPORTED;
     if (num_pages < 1 || kv_heads < 1 || kv_heads > 4096 || page_size < 16 || page_size > 256 ||
@@ -877,6 +879,11 @@ size_t batq_kv_paged_code_bytes(int num_pages, int page_size, int kv_heads, int 
     return (size_t)num_pages * page_size * kv_heads * head_dim;
 }
 
+size_t batq_kv_paged_code_bytes_ex(int num_pages, int page_size, int kv_heads, int head_dim, int cache_bits) {
+    if (check_cache_bits(cache_bits) != BATQ_OK) return 0;
+    return batq_kv_paged_code_bytes(num_pages, page_size, kv_heads, head_dim) / 8 * cache_bits;
+}
+
 size_t batq_kv_paged_scale_bytes(int num_pages, int page_size, int kv_heads, int head_dim) {
     return batq_kv_paged_code_bytes(num_pages, page_size, kv_heads, head_dim) / 32;
 }
@@ -886,7 +893,16 @@ batq_status batq_kv_paged_append(const batq_paged_cache* cache, const batq_trans
                                  int64_t ldq_out, const void* k, int64_t ldk, const void* v, int64_t ldv,
                                  batq_dtype xdtype, const int32_t* positions, const int64_t* slots, int M,
                                  void* stream) {
+    return batq_kv_paged_append_ex(cache, 8, tk, tv, rope, q, ldq, q_heads, q_out, ldq_out, k, ldk, v, ldv, xdtype, positions,
+                                   slots, M, stream);
+}
+
+batq_status batq_kv_paged_append_ex(const batq_paged_cache* cache, int cache_bits, const batq_transform* tk,
+                                    const batq_transform* tv, const batq_rope* rope, const void* q, int64_t ldq, int q_heads,
+                                    void* q_out, int64_t ldq_out, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                    batq_dtype xdtype, const int32_t* positions, const int64_t* slots, int M, void* stream) {
     if (batq_status st = check_paged_cache(cache); st != BATQ_OK) return st;
+    if (batq_status st = check_cache_bits(cache_bits); st != BATQ_OK) return st;
     if (!dtype_ok(xdtype)) return BATQ_ERR_DTYPE;
     const int D = cache->head_dim, width = cache->kv_heads * D;
     if (M < 0 || M > (1 << 30) || ldk < width || ldv < width || q_heads < 0 || q_heads > (1 << 19) || q_heads % cache->kv_heads != 0)
@@ -911,7 +927,7 @@ batq_status batq_kv_paged_append(const batq_paged_cache* cache, const batq_trans
                         q_out == q || q_out == k || q_out == v))
         return BATQ_ERR_SHAPE;
     if (batq_status st = check_device(); st != BATQ_OK) return st;
-    BATQ_HIP(batq::launch_kv_paged_append(*cache, tk, tv, rope, q, ldq, q_heads, q_out, ldq_out, k, ldk, v, ldv, xdtype,
+    BATQ_HIP(batq::launch_kv_paged_append(*cache, cache_bits, tk, tv, rope, q, ldq, q_heads, q_out, ldq_out, k, ldk, v, ldv, xdtype,
                                           positions, slots, M, static_cast<hipStream_t>(stream)));
     return BATQ_OK;
 }
@@ -950,9 +966,16 @@ size_t batq_paged_attention_workspace(const batq_paged_cache* cache, int q_heads
 batq_status batq_paged_attention(const batq_paged_cache* cache, const batq_paged_batch* b, const void* q, int64_t ldq,
                                  int q_heads, float scale, int causal, int window, void* out, int64_t ldo, float* lse,
                                  void* workspace, size_t workspace_bytes, void* stream) {
+    return batq_paged_attention_ex(cache, 8, b, q, ldq, q_heads, scale, causal, window, out, ldo, lse, workspace, workspace_bytes, stream);
+}
+
+batq_status batq_paged_attention_ex(const batq_paged_cache* cache, int cache_bits, const batq_paged_batch* b, const void* q,
+                                    int64_t ldq, int q_heads, float scale, int causal, int window, void* out, int64_t ldo,
+                                    float* lse, void* workspace, size_t workspace_bytes, void* stream) {
     if (!b) return BATQ_ERR_NULL;
     if (batq_status st = check_attention_dims(cache, q_heads, b->batch, b->total_q, b->max_q, b->max_kv); st != BATQ_OK) return st;
     if (batq_status st = check_paged_cache(cache); st != BATQ_OK) return st;
+    if (batq_status st = check_cache_bits(cache_bits); st != BATQ_OK) return st;
     const int64_t width = (int64_t)q_heads * cache->head_dim;
     if (ldq < width || ldo < width || b->table_width < 0 || window < 0) return BATQ_ERR_SHAPE;
     if (!(scale > 0.0f) || !(scale < 2.0e38f)) return BATQ_ERR_SHAPE;          // (times log2 e it is finite)
@@ -968,8 +991,92 @@ batq_status batq_paged_attention(const batq_paged_cache* cache, const batq_paged
     if (!cus) return BATQ_ERR_DEVICE;
     const size_t need = batq::paged_attention_part_bytes(*cache, q_heads, b->batch, b->total_q, b->max_q, b->max_kv, cus);
     if (need > workspace_bytes || (need > 0 && !workspace)) return BATQ_ERR_WORKSPACE;
-    BATQ_HIP(batq::launch_paged_attention(*cache, *b, q, ldq, q_heads, scale, causal != 0, window, out, ldo, lse, workspace,
+    BATQ_HIP(batq::launch_paged_attention(*cache, cache_bits, *b, q, ldq, q_heads, scale, causal != 0, window, out, ldo, lse, workspace,
                                           static_cast<hipStream_t>(stream)));
+    return BATQ_OK;
+}
+
+// ---- scores of cached tokens
+static batq_status check_score_dims(const batq_paged_cache* c, int q_heads, int batch, int total_q, int max_q, int max_kv) {
+    if (batq_status st = check_attention_dims(c, q_heads, batch, total_q, max_q, max_kv); st != BATQ_OK) return st;
+    // workgroups of 256 for every 256 tokens of a (sequence, key head) pair, and as many parts of its rows as keep this many
+    if ((int64_t)batch * c->kv_heads * (max_kv / 256 + 1) >= 1 << 24) return BATQ_ERR_SHAPE;
+    return BATQ_OK;
+}
+
+size_t batq_kv_paged_score_workspace(const batq_paged_cache* cache, int q_heads, int batch, int total_q, int max_q, int max_kv) {
+    if (check_score_dims(cache, q_heads, batch, total_q, max_q, max_kv) != BATQ_OK) return 0;
+    const int cus = current_compute_units();
+    return cus ? batq::paged_score_workspace_bytes(*cache, q_heads, batch, total_q, max_q, max_kv, cus) : 0;
+}
+
+batq_status batq_kv_paged_score(const batq_paged_cache* cache, int cache_bits, const batq_paged_batch* b, const void* q,
+                                int64_t ldq, int q_heads, float scale, int causal, int window, const float* lse, float* score,
+                                int add, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!b) return BATQ_ERR_NULL;
+    if (batq_status st = check_score_dims(cache, q_heads, b->batch, b->total_q, b->max_q, b->max_kv); st != BATQ_OK) return st;
+    if (batq_status st = check_paged_cache(cache); st != BATQ_OK) return st;
+    if (batq_status st = check_cache_bits(cache_bits); st != BATQ_OK) return st;
+    if (ldq < (int64_t)q_heads * cache->head_dim || b->table_width < 0 || window < 0) return BATQ_ERR_SHAPE;
+    if (!(scale > 0.0f) || !(scale < 2.0e38f)) return BATQ_ERR_SHAPE;
+    if (b->batch == 0 || b->max_kv == 0 || b->table_width == 0) return BATQ_OK;
+    if (!b->cu_q || !b->kv_len || !b->page_table || !score || (b->total_q > 0 && (!q || !lse))) return BATQ_ERR_NULL;
+    if (!aligned16(q) || (ldq * 2) % 16 != 0 ||
+        ((reinterpret_cast<uintptr_t>(b->cu_q) | reinterpret_cast<uintptr_t>(b->kv_len) | reinterpret_cast<uintptr_t>(b->page_table) |
+          reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(score)) & 3u) != 0 ||
+        (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
+        return BATQ_ERR_SHAPE;
+    if (batq_status st = check_device(); st != BATQ_OK) return st;
+    const int cus = current_compute_units();
+    if (!cus) return BATQ_ERR_DEVICE;
+    const size_t need = batq::paged_score_part_bytes(*cache, q_heads, b->batch, b->total_q, b->max_q, b->max_kv, cus);
+    if (need > workspace_bytes || (need > 0 && !workspace)) return BATQ_ERR_WORKSPACE;
+    BATQ_HIP(batq::launch_kv_paged_score(*cache, cache_bits, *b, q, ldq, q_heads, scale, causal != 0, window, lse, score, add != 0,
+                                         workspace, static_cast<hipStream_t>(stream)));
+    return BATQ_OK;
+}
+
+// ---- eviction
+static batq_status check_evict_dims(const batq_paged_cache* c, int batch, int max_kv, int budget) {
+    if (!c) return BATQ_ERR_NULL;
+    if (batq_status st = check_paged_dims(c->num_pages, c->page_size, c->kv_heads, c->head_dim); st != BATQ_OK) return st;
+    if (batch < 0 || batch > (1 << 20) || max_kv < 0 || max_kv > (1 << 30) || budget < 1) return BATQ_ERR_SHAPE;
+    // a launch has fewer than 2^32 threads: workgroups of 1024 for a (sequence, key head) pair, of 256 for 64 of its kept tokens
+    const int64_t pairs = (int64_t)batch * c->kv_heads, kept = budget < max_kv ? budget : max_kv;
+    if (pairs >= 1 << 22 || pairs * (kept / 64 + 1) >= 1 << 24) return BATQ_ERR_SHAPE;
+    return BATQ_OK;
+}
+
+size_t batq_kv_paged_evict_workspace(const batq_paged_cache* cache, int batch, int max_kv, int budget) {
+    if (check_evict_dims(cache, batch, max_kv, budget) != BATQ_OK) return 0;
+    const int cus = current_compute_units();
+    return cus ? batq::paged_evict_workspace_bytes(*cache, batch, max_kv, budget, cus) : 0;
+}
+
+batq_status batq_kv_paged_evict(const batq_paged_cache* cache, int cache_bits, float* score, const int32_t* kv_len,
+                                const int32_t* page_table, int table_width, const int32_t* out_table, int out_width, int batch,
+                                int max_kv, int budget, int first, int last, int32_t* keep, int32_t* new_len, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+    if (batq_status st = check_evict_dims(cache, batch, max_kv, budget); st != BATQ_OK) return st;
+    if (batq_status st = check_paged_cache(cache); st != BATQ_OK) return st;
+    if (batq_status st = check_cache_bits(cache_bits); st != BATQ_OK) return st;
+    if (table_width < 0 || out_width < 0 || first < 0 || last < 0 || (int64_t)first + last > budget) return BATQ_ERR_SHAPE;
+    const int64_t held = (int64_t)table_width * cache->page_size;
+    const int64_t most = budget < max_kv ? budget : max_kv;
+    if ((int64_t)out_width * cache->page_size < (most < held ? most : held)) return BATQ_ERR_SHAPE;
+    if (batch == 0) return BATQ_OK;
+    if (!score || !kv_len || !keep || !new_len || (table_width > 0 && !page_table) || (out_width > 0 && !out_table)) return BATQ_ERR_NULL;
+    if (((reinterpret_cast<uintptr_t>(score) | reinterpret_cast<uintptr_t>(kv_len) | reinterpret_cast<uintptr_t>(page_table) |
+          reinterpret_cast<uintptr_t>(out_table) | reinterpret_cast<uintptr_t>(keep) | reinterpret_cast<uintptr_t>(new_len)) & 3u) != 0 ||
+        (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || new_len == kv_len || (page_table && page_table == out_table))
+        return BATQ_ERR_SHAPE;
+    if (batq_status st = check_device(); st != BATQ_OK) return st;
+    const int cus = current_compute_units();
+    if (!cus) return BATQ_ERR_DEVICE;
+    const size_t need = batq::paged_evict_workspace_bytes(*cache, batch, max_kv, budget, cus);
+    if (need > workspace_bytes || (need > 0 && !workspace)) return BATQ_ERR_WORKSPACE;
+    BATQ_HIP(batq::launch_kv_paged_evict(*cache, cache_bits, score, kv_len, page_table, table_width, out_table, out_width, batch, max_kv,
+                                         budget, first, last, keep, new_len, workspace, static_cast<hipStream_t>(stream)));
     return BATQ_OK;
 }
 

@@ -126,7 +126,8 @@ hipError_t launch_scales_to_internal(const uint8_t* canon, uint8_t* internal, in
 hipError_t launch_scales_to_canonical(const uint8_t* internal, uint8_t* canon, int rows, int nb, hipStream_t stream);
 
 // Paged cache and the operators on it (arguments checked by the C ABI).
-hipError_t launch_kv_paged_append(const batq_paged_cache& c, const batq_transform* tk, const batq_transform* tv,
+// bits: 4 or 8, the width of the cache's codes.
+hipError_t launch_kv_paged_append(const batq_paged_cache& c, int bits, const batq_transform* tk, const batq_transform* tv,
                                   const batq_rope* rope, const void* q, int64_t ldq, int q_heads, void* q_out,
                                   int64_t ldq_out, const void* k, int64_t ldk, const void* v, int64_t ldv,
                                   batq_dtype xdtype, const int32_t* positions, const int64_t* slots, int M,
@@ -135,9 +136,20 @@ size_t paged_attention_part_bytes(const batq_paged_cache& c, int q_heads, int ba
                                   int compute_units);      // what a call takes of its workspace
 size_t paged_attention_workspace_bytes(const batq_paged_cache& c, int q_heads, int batch, int total_q, int max_q,
                                        int max_kv, int compute_units);
-hipError_t launch_paged_attention(const batq_paged_cache& c, const batq_paged_batch& b, const void* q, int64_t ldq,
+hipError_t launch_paged_attention(const batq_paged_cache& c, int bits, const batq_paged_batch& b, const void* q, int64_t ldq,
                                   int q_heads, float scale, bool causal, int window, void* out, int64_t ldo, float* lse,
                                   void* workspace, hipStream_t stream);
+size_t paged_score_part_bytes(const batq_paged_cache& c, int q_heads, int batch, int total_q, int max_q, int max_kv,
+                              int compute_units);          // what a call takes of its workspace
+size_t paged_score_workspace_bytes(const batq_paged_cache& c, int q_heads, int batch, int total_q, int max_q, int max_kv,
+                                   int compute_units);
+hipError_t launch_kv_paged_score(const batq_paged_cache& c, int bits, const batq_paged_batch& b, const void* q, int64_t ldq,
+                                 int q_heads, float scale, bool causal, int window, const float* lse, float* score, bool add,
+                                 void* workspace, hipStream_t stream);
+size_t paged_evict_workspace_bytes(const batq_paged_cache& c, int batch, int max_kv, int budget, int compute_units);
+hipError_t launch_kv_paged_evict(const batq_paged_cache& c, int bits, float* score, const int32_t* kv_len, const int32_t* page_table,
+                                 int table_width, const int32_t* out_table, int out_width, int batch, int max_kv, int budget,
+                                 int first, int last, int32_t* keep, int32_t* new_len, void* workspace, hipStream_t stream);
 size_t lora_parts_bytes(int M, int K, int N, int rank, int adapters);       // what a call takes of its workspace
 size_t lora_workspace_bytes(int M, int K, int rank);
 hipError_t launch_lora_add(const void* X, batq_dtype xdtype, int M, int K, int64_t ldx, const void* A, const void* B,

@@ -1,6 +1,6 @@
 // What happens to the queries, keys and values of new tokens between the fused projection and the attention: rotation
 // by position, the block transforms (Sec. 3.2: P_k and P_v transform the key and value cache head by head, queries
-// take T_k^-T), MXFP8 (Sec. 2) and the scatter into the pages of the cache.  gfx950 only.
+// take T_k^-T), MXFP8 or MXFP4 (Sec. 2) and the scatter into the pages of the cache.  gfx950 only.
 #include "batq_internal.h"
 #include "mxfp4_device.h"
 
@@ -127,9 +127,22 @@ __device__ __forceinline__ void transform16(float (&y)[16], const bf16x8 (&t)[6]
     for (int r = 0; r < 16; ++r) y[r] = acc[r];
 }
 
+// 16 codes of BITS bits.
+template <int BITS>
+struct Codes16;
+template <>
+struct Codes16<8> {
+    typedef uint4 type;
+};
+template <>
+struct Codes16<4> {
+    typedef uint2 type;
+};
+
 // Clips and quantises the lane's half of a block; returns the codes, and the scale byte in *scale.  `clip` is 1 for no clipping,
 // or with `minmax` the ratio of the block's minimum beside clip_max of its maximum.
-__device__ __forceinline__ uint4 quantise16(float (&y)[16], bool minmax, float clip, float clip_max, uint32_t* scale) {
+template <int BITS>
+__device__ __forceinline__ typename Codes16<BITS>::type quantise16(float (&y)[16], bool minmax, float clip, float clip_max, uint32_t* scale) {
     const int lane = threadIdx.x & 63;
     auto other_half = [&](float x) -> float {
         return __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute((lane ^ 32) << 2, __builtin_bit_cast(int, x)));
@@ -154,11 +167,15 @@ __device__ __forceinline__ uint4 quantise16(float (&y)[16], bool minmax, float c
         for (int r = 1; r < 16; ++r) x = __builtin_fmaxf(x, __builtin_fabsf(y[r]));
         bound = __builtin_fmaxf(x, other_half(x)) * clip;
     }
-    const uint32_t sb = e8m0_of_bound_fp8(bound);
+    const uint32_t sb = BITS == 8 ? e8m0_of_bound_fp8(bound) : e8m0_of_bound(bound);
     const float sc = scale_operand(sb);
-    const uint2 o0 = encode8_fp8(y, bound, sb, sc), o1 = encode8_fp8(y + 8, bound, sb, sc);
     *scale = sb;
-    return uint4{o0.x, o0.y, o1.x, o1.y};
+    if constexpr (BITS == 8) {
+        const uint2 o0 = encode8_fp8(y, bound, sb, sc), o1 = encode8_fp8(y + 8, bound, sb, sc);
+        return uint4{o0.x, o0.y, o1.x, o1.y};
+    } else {
+        return uint2{encode8(y, bound, sc), encode8(y + 8, bound, sc)};
+    }
 }
 
 // Head number `head` of a token's queries, keys and values, in that order.
@@ -174,10 +191,11 @@ __device__ __forceinline__ Kind kind_of(const AppendArgs& a, int* head) {
 // 5.0).  One wave per (32 tokens, MX block of a head).  Lane l holds channels
 // 16 (l / 32) .. + 15 of the block for token l % 32, before the transform and after it (the handle's split operands are
 // stored so that the matrix instruction's results come in the order of its operands).
-template <typename XT, int D>
+template <typename XT, int D, int BITS>
 __global__ void __launch_bounds__(256)
 append_few(const AppendArgs a) {
     constexpr int kBlocks = D / 32;
+    typedef typename Codes16<BITS>::type Codes;
     const int lane = threadIdx.x & 63, l32 = lane & 31, kg = lane >> 5;
     const int per_tile = (a.q_heads + 2 * a.kv_heads) * kBlocks;
     const int tiles = (a.M + 31) >> 5;
@@ -223,10 +241,10 @@ append_few(const AppendArgs a) {
         return;
     }
     uint32_t sb;
-    const uint4 codes = quantise16(y, clips_max, clip, clip_max, &sb);
+    const Codes codes = quantise16<BITS>(y, clips_max, clip, clip_max, &sb);
     if (!live || slot < 0 || slot >= a.num_slots) return;
     const int64_t off = slot & ((1 << a.page_shift) - 1), ph = (slot >> a.page_shift) * a.kv_heads + head;
-    *reinterpret_cast<uint4*>((kind == kKey ? a.k_codes : a.v_codes) + (((ph << a.page_shift) + off) * D + b * 32 + 16 * kg)) = codes;
+    *reinterpret_cast<Codes*>((kind == kKey ? a.k_codes : a.v_codes) + (((ph << a.page_shift) + off) * D + b * 32 + 16 * kg) * BITS / 8) = codes;
     if (kg == 0) (kind == kKey ? a.k_scales : a.v_scales)[((ph * kBlocks + b) << a.page_shift) + off] = (uint8_t)sb;
 }
 
@@ -248,11 +266,12 @@ constexpr int many_lds() { return 4 * 2 * 32 * D * (int)sizeof(XT) + 32 * 512; }
 // pairs a lane holds (interleaved, or whole blocks apart); arithmetic as in append_few, same bits.  Measured: 8192 tokens of
 // 32 + 2 x 8 heads of 128 channels in bf16, all transformed: 53 us (184 MB in and out, 3.5 TB/s); a wait at the top of each
 // tile, behind the last one's stores, 69 us; equal ranges of tiles over all workgroups instead of whole ones, the same 53.
-template <typename XT, int D>
+template <typename XT, int D, int BITS>
 __global__ void __launch_bounds__(256, sizeof(XT) == 4 && D == 128 ? 1 : 2)
 append_many(const AppendArgs a) {
     constexpr int kBlocks = D / 32, kSize = (int)sizeof(XT), kCh = D * kSize / 16, kRows = 64 / kCh, kLoads = 32 / kRows, kTile = 32 * kCh * 16;
-    constexpr int kQCh = D / 8, kCCh = D / 16;              // 16-byte chunks of a row of queries out, of codes
+    constexpr int kQCh = D / 8, kCCh = D * BITS / 128;      // 16-byte chunks of a row of queries out, of codes
+    typedef typename Codes16<BITS>::type Codes;
     extern __shared__ __align__(16) uint8_t s_raw[];
     typedef __attribute__((address_space(3))) uint8_t lds_byte;
     int lane = threadIdx.x & 63;
@@ -398,9 +417,9 @@ append_many(const AppendArgs a) {
                 for (int h = 0; h < 2; ++h) *reinterpret_cast<bf16x8*>(x_at + (own ^ (32 * kSize * b + 16 * h))) = to_bf16(y + 8 * h);
             } else {
                 uint32_t sb;
-                const uint4 codes = quantise16(y, clips_max, clip[b], clip_max[b], &sb);
+                const Codes codes = quantise16<BITS>(y, clips_max, clip[b], clip_max[b], &sb);
                 scale_bytes |= sb << (8 * b);
-                *reinterpret_cast<uint4*>(x_at + (own ^ (32 * kSize * b))) = codes;
+                *reinterpret_cast<Codes*>(x_at + (own ^ (32 * kSize * b))) = codes;
             }
             __builtin_amdgcn_sched_barrier(0);              // block by block: interleaved, they would not fit the registers
         };
@@ -458,11 +477,18 @@ append_many(const AppendArgs a) {
             if (live && kg == 0)
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) (kind == kKey ? a.k_scales : a.v_scales)[((ph * kBlocks + b) << a.page_shift) + off] = (uint8_t)(scale_bytes >> (8 * b));
-            const int64_t to = live ? ((ph << a.page_shift) + off) * D : -1;
+            const int64_t to = live ? ((ph << a.page_shift) + off) * (D * BITS / 8) : -1;
 #pragma unroll
             for (int i = 0; i < kCCh / 2; ++i) {
                 const int r = i * (64 / kCCh) + lane / kCCh, c = lane % kCCh;
-                const u32x4 v = *reinterpret_cast<const u32x4*>(x_at + (at(r, kCh) ^ ((c & 1) * 16 * kSize) ^ ((c >> 1) * 32 * kSize)));
+                u32x4 v;
+                if constexpr (BITS == 8) {
+                    v = *reinterpret_cast<const u32x4*>(x_at + (at(r, kCh) ^ ((c & 1) * 16 * kSize) ^ ((c >> 1) * 32 * kSize)));
+                } else {                                    // a chunk is a block: the codes of its two lanes
+                    const uint2 v0 = *reinterpret_cast<const uint2*>(x_at + (at(r, kCh) ^ (c * 32 * kSize)));
+                    const uint2 v1 = *reinterpret_cast<const uint2*>(x_at + (at(r, kCh) ^ (c * 32 * kSize) ^ (16 * kSize)));
+                    v = u32x4{v0.x, v0.y, v1.x, v1.y};
+                }
                 const int64_t from = (int64_t)(((uint64_t)(uint32_t)__shfl((int)(to >> 32), r) << 32) | (uint32_t)__shfl((int)to, r));
                 if (from >= 0) *reinterpret_cast<u32x4*>((kind == kKey ? a.k_codes : a.v_codes) + from + c * 16) = v;
             }
@@ -471,7 +497,7 @@ append_many(const AppendArgs a) {
     }
 }
 
-template <typename XT, int D>
+template <typename XT, int D, int BITS>
 hipError_t launch_append(AppendArgs& a, hipStream_t stream) {
     const int tiles = (int)(((int64_t)a.M + 31) / 32), heads = a.q_heads + 2 * a.kv_heads;
     const int64_t units = (int64_t)tiles * heads * (D / 32);
@@ -481,7 +507,7 @@ hipError_t launch_append(AppendArgs& a, hipStream_t stream) {
     // append_few up to 2048 units of 32 tokens x 32 channels (head_dim 128: 256 tokens of 32 + 2 x 8 heads 6.7 us beside 7.9,
     // 384 tokens 8.6 beside 7.9) or 1024 (head_dim 64: 384 tokens of 28 + 2 x 4 heads 4.9 beside 5.5, 512 tokens 6.3 beside 5.5)
     if (units <= 16 * D || !fits) {
-        append_few<XT, D><<<(unsigned)((units + 3) / 4), 256, 0, stream>>>(a);
+        append_few<XT, D, BITS><<<(unsigned)((units + 3) / 4), 256, 0, stream>>>(a);
         return hipGetLastError();
     }
     int dev = 0;
@@ -491,7 +517,7 @@ hipError_t launch_append(AppendArgs& a, hipStream_t stream) {
     if (e != hipSuccess) return e;
     constexpr int lds = many_lds<XT, D>();
     if constexpr (lds > 65536)
-        if (e = ensure_dynamic_lds<&append_many<XT, D>>(dev, lds); e != hipSuccess) return e;
+        if (e = ensure_dynamic_lds<&append_many<XT, D, BITS>>(dev, lds); e != hipSuccess) return e;
     // tiles of a workgroup: two workgroups to a compute unit at a time, in whole rounds
     const int groups = (heads + 3) / 4;
     int64_t n = ((int64_t)tiles * groups + 2 * cus - 1) / (2 * cus);
@@ -499,13 +525,19 @@ hipError_t launch_append(AppendArgs& a, hipStream_t stream) {
     if (n > 16) n = 16;
     a.tiles_wg = (int)n;
     const int64_t grid = (tiles + n - 1) / n * groups;
-    append_many<XT, D><<<(unsigned)grid, 256, lds, stream>>>(a);
+    append_many<XT, D, BITS><<<(unsigned)grid, 256, lds, stream>>>(a);
     return hipGetLastError();
+}
+
+template <int BITS>
+hipError_t launch_append(AppendArgs& a, batq_dtype xdtype, int head_dim, hipStream_t stream) {
+    if (xdtype == BATQ_BF16) return head_dim == 64 ? launch_append<uint16_t, 64, BITS>(a, stream) : launch_append<uint16_t, 128, BITS>(a, stream);
+    return head_dim == 64 ? launch_append<float, 64, BITS>(a, stream) : launch_append<float, 128, BITS>(a, stream);
 }
 
 }  // namespace
 
-hipError_t launch_kv_paged_append(const batq_paged_cache& c, const batq_transform* tk, const batq_transform* tv,
+hipError_t launch_kv_paged_append(const batq_paged_cache& c, int bits, const batq_transform* tk, const batq_transform* tv,
                                   const batq_rope* rope, const void* q, int64_t ldq, int q_heads, void* q_out,
                                   int64_t ldq_out, const void* k, int64_t ldk, const void* v, int64_t ldv,
                                   batq_dtype xdtype, const int32_t* positions, const int64_t* slots, int M,
@@ -526,8 +558,7 @@ hipError_t launch_kv_paged_append(const batq_paged_cache& c, const batq_transfor
     a.num_slots = (int64_t)c.num_pages * c.page_size;
     a.q_heads = q_heads, a.kv_heads = c.kv_heads, a.group = q_heads ? q_heads / c.kv_heads : 1;
     a.page_shift = __builtin_ctz((unsigned)c.page_size);
-    if (xdtype == BATQ_BF16) return c.head_dim == 64 ? launch_append<uint16_t, 64>(a, stream) : launch_append<uint16_t, 128>(a, stream);
-    return c.head_dim == 64 ? launch_append<float, 64>(a, stream) : launch_append<float, 128>(a, stream);
+    return bits == 8 ? launch_append<8>(a, xdtype, c.head_dim, stream) : launch_append<4>(a, xdtype, c.head_dim, stream);
 }
 
 }  // namespace batq

@@ -1,4 +1,4 @@
-// Attention over the paged MXFP8 cache: one pass over a sequence's keys and values with the running maximum and sum
+// Attention over the paged cache of MXFP8 or MXFP4 (BITS 8 or 4): one pass over a sequence's keys and values with the running maximum and sum
 // of the softmax.  gfx950 only.
 //
 // Both kernels compute S^T = K Q^T and O^T = V^T P^T: the instruction's result layout then has a lane hold scores of one
@@ -8,25 +8,19 @@
 
 #include "batq_internal.h"
 #include "mxfp4_device.h"
+#include "paged_device.h"
 
 namespace batq {
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float v16f __attribute__((ext_vector_type(16)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-struct AttnArgs {
+struct AttnArgs : PagedLists {
     const uint16_t* q;
     int64_t ldq, ldo;
     uint16_t* out;
     float* lse;
     const uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
-    const int32_t *cu_q, *kv_len, *page_table;
-    int batch, table_width, total_q, max_q, max_kv, num_pages, page_shift, q_heads, kv_heads, group;
-    int causal, window;
     float scale;                                            // times log2 e: scores are kept in units of ln 2
     // sequences of at most few_rows rows (query tokens x heads of a group) belong to attend_few, the others to
     // attend_many; parts of few_len and many_len tokens
@@ -38,30 +32,6 @@ struct AttnArgs {
     float *many_o, *many_ml;                                // likewise [row of q][query head][part]
 };
 
-// First token that the window leaves to a query at `pos`, which may be far below zero (more queries than tokens) beside a
-// window of any size.
-__device__ __forceinline__ int first_seen(const AttnArgs& a, int pos) { return a.window && pos >= a.window ? pos - a.window + 1 : 0; }
-
-// Sequence b as the kernels take it: nothing in the lists is trusted.
-struct Seq {
-    int begin, n, len;                                      // first row, queries served, tokens
-    int first_pos;                                          // position of the first query
-    int t_lo, t_hi;                                         // tokens that some query may see
-};
-
-__device__ __forceinline__ Seq sequence(const AttnArgs& a, int b) {
-    Seq s;
-    s.begin = a.cu_q[b];
-    const int end = a.cu_q[b + 1];
-    const int n = (s.begin < 0 || end > a.total_q || end < s.begin) ? 0 : end - s.begin;
-    s.n = min(n, a.max_q);
-    s.len = (int)min((int64_t)max(0, min(a.kv_len[b], a.max_kv)), (int64_t)a.table_width << a.page_shift);
-    s.first_pos = s.len - n;
-    s.t_hi = a.causal ? max(0, min(s.len, s.first_pos + s.n)) : s.len;
-    s.t_lo = min(s.t_hi, first_seen(a, s.first_pos));
-    return s;
-}
-
 // Tokens [lo, hi) that some row of a workgroup sees, and the parts of part_len tokens that they are cut into (counted
 // from the block of 64 with the first of them; at least one, which writes the zeros of rows that see nothing).
 struct TokenRange {
@@ -72,14 +42,6 @@ __device__ __forceinline__ int range_parts(const TokenRange& t, int part_len) {
 }
 __device__ __forceinline__ int live_parts(const Seq& s, int part_len) { return range_parts(TokenRange{s.t_lo, s.t_hi}, part_len); }
 
-__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
-
-__device__ __forceinline__ uint32_t cvt_lo(uint32_t w, float sc) {
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, sc, false));
-}
-__device__ __forceinline__ uint32_t cvt_hi(uint32_t w, float sc) {
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, sc, true));
-}
 // The low (high) halves of x and y: transposes a 2 x 2 tile of 16-bit numbers.
 __device__ __forceinline__ uint32_t low_halves(uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x05040100u); }
 __device__ __forceinline__ uint32_t high_halves(uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x07060302u); }
@@ -112,10 +74,12 @@ __device__ __forceinline__ float shuffle_xor(float x, int d) { return __shfl_xor
 // The weights go in as two bf16 terms (2^-16): the products are not the bound here.  Measured: 4 sequences of about 131072 tokens, 28 query
 // and 4 key heads of 128: 73 us (367 MB, 5.0 TB/s, a large copy's rate); 64 sequences of up to 8192, 32 and 8 heads: 36 us.
 // Blocks of 64 tokens at two waves per SIMD: 40 us instead of 36; four waves per SIMD spill: 50 us.
-template <int D, int NT>
+template <int D, int NT, int BITS>
 __global__ void __launch_bounds__(256, NT == 1 ? 3 : 2)
 attend_few(const AttnArgs a) {
     constexpr int kC = D / 4, kV = D / 16, kU = D / 32;      // channels of a key lane, of a value lane, products per tile
+    constexpr int kToken = D * BITS / 8;                    // bytes of a token's codes
+    constexpr int kKw = kC * BITS / 32, kVw = kV * BITS >= 32 ? kV * BITS / 32 : 1;      // words of a lane's key, of its values
     constexpr int kRow = D + 4;                             // floats of a row in LDS (spread over the banks)
     __shared__ float s_o[4][16][kRow];
     __shared__ float s_m[4][NT * 16], s_l[4][NT * 16];
@@ -136,9 +100,9 @@ attend_few(const AttnArgs a) {
     const int pages = t_begin < t_end ? table[min((t_begin + 16 * lane) >> a.page_shift, last_page)] : 0;
     auto entry = [&](int t) { return __shfl(pages, (t - t_begin) >> 4); };
 
-    u32x4 kw[2][kC / 16];
+    uint32_t kw[2][kKw];
     uint32_t ks;
-    uint32_t vw[8][kV / 4];
+    uint32_t vw[8][kVw];
     u32x2 vs;
     bool v_ok = false;
     auto load_k = [&](int t) {
@@ -147,11 +111,9 @@ attend_few(const AttnArgs a) {
         page = (uint32_t)page < (uint32_t)a.num_pages ? page : 0;
         const int off = t & page_mask;
         const int64_t ph = (int64_t)page * a.kv_heads + h;
-        const uint8_t* p = a.k_codes + ((ph << a.page_shift) + off) * D + g * kC;
+        const uint8_t* p = a.k_codes + ((ph << a.page_shift) + off) * kToken + g * (kToken / 4);
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int c = 0; c < kC / 16; ++c) kw[i][c] = *reinterpret_cast<const u32x4*>(p + i * D + c * 16);
+        for (int i = 0; i < 2; ++i) load_words<kKw>(kw[i], p + i * kToken);
         ks = *reinterpret_cast<const uint16_t*>(a.k_scales + ((ph * (D / 32) + g * kC / 32) << a.page_shift) + off);
     };
     auto load_v = [&](int t) {
@@ -161,15 +123,11 @@ attend_few(const AttnArgs a) {
         page = v_ok ? page : 0;
         const int off = t & page_mask;
         const int64_t ph = (int64_t)page * a.kv_heads + h;
-        const uint8_t* p = a.v_codes + ((ph << a.page_shift) + off) * D + n * kV;
+        const uint8_t* p = a.v_codes + ((ph << a.page_shift) + off) * kToken + n * (kToken / 16);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if constexpr (kV == 8) {
-                const u32x2 w = *reinterpret_cast<const u32x2*>(p + i * D);
-                vw[i][0] = w[0], vw[i][kV / 4 - 1] = w[1];
-            } else {
-                vw[i][0] = *reinterpret_cast<const uint32_t*>(p + i * D);
-            }
+            if constexpr (kV * BITS >= 32) load_words<kVw>(vw[i], p + i * kToken);
+            else vw[i][0] = *reinterpret_cast<const uint16_t*>(p + i * kToken);
         }
         vs = *reinterpret_cast<const u32x2*>(a.v_scales + ((ph * (D / 32) + n * kV / 32) << a.page_shift) + off);
     };
@@ -212,10 +170,7 @@ attend_few(const AttnArgs a) {
             const float kscale = scale_byte(ks, i);
             bf16x8 kf[kU];
 #pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                const uint32_t w0 = kw[i][u / 2][2 * (u & 1)], w1 = kw[i][u / 2][2 * (u & 1) + 1];
-                kf[u] = __builtin_bit_cast(bf16x8, u32x4{cvt_lo(w0, kscale), cvt_hi(w0, kscale), cvt_lo(w1, kscale), cvt_hi(w1, kscale)});
-            }
+            for (int u = 0; u < kU; ++u) kf[u] = cvt_eight<BITS>(kw[i] + u * BITS / 4, kscale);
 #pragma unroll
             for (int x = 0; x < NT; ++x) {
                 sc[x][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -243,16 +198,17 @@ attend_few(const AttnArgs a) {
                 const int tok = t + 8 * g + i;
                 if (!(v_ok && tok >= s.t_lo && tok < s.t_hi)) {
 #pragma unroll
-                    for (int c = 0; c < kV / 4; ++c) vw[i][c] = 0u;
+                    for (int c = 0; c < kVw; ++c) vw[i][c] = 0u;
                     vs[i / 4] = (vs[i / 4] & ~(0xFFu << (8 * (i & 3)))) | (127u << (8 * (i & 3)));
                 }
             }
             if (s.n > 1) {                                  // (one query: the tokens left are seen by all rows)
                 uint32_t any = odd_scales(vs[0]) | odd_scales(vs[1]);
+                if constexpr (BITS == 8)                    // (no code of 4 bits is NaN)
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
+                    for (int i = 0; i < 8; ++i)
 #pragma unroll
-                    for (int c = 0; c < kV / 4; ++c) any |= odd_codes(vw[i][c]);
+                        for (int c = 0; c < kVw; ++c) any |= odd_codes(vw[i][c]);
                 odd = __ballot(any != 0) != 0;
             }
         }
@@ -290,8 +246,8 @@ attend_few(const AttnArgs a) {
             for (int e = 0; e < 4; ++e) {
                 const int i0 = 2 * e, i1 = i0 + 1;
                 const float s0 = scale_byte(vs[i0 / 4], i0 & 3), s1 = scale_byte(vs[i1 / 4], i1 & 3);
-                const uint32_t a0 = cvt_lo(vw[i0][c], s0), b0 = cvt_lo(vw[i1][c], s1);
-                const uint32_t a1 = cvt_hi(vw[i0][c], s0), b1 = cvt_hi(vw[i1][c], s1);
+                const uint32_t a0 = cvt_pair<BITS>(vw[i0], 2 * c, s0), b0 = cvt_pair<BITS>(vw[i1], 2 * c, s1);
+                const uint32_t a1 = cvt_pair<BITS>(vw[i0], 2 * c + 1, s0), b1 = cvt_pair<BITS>(vw[i1], 2 * c + 1, s1);
                 f[0][e] = low_halves(a0, b0), f[1][e] = high_halves(a0, b0);
                 f[2][e] = low_halves(a1, b1), f[3][e] = high_halves(a1, b1);
             }
@@ -503,10 +459,11 @@ __device__ __forceinline__ void find_tile(const AttnArgs& a, int x, int* b, int*
 
 constexpr int kDeep = 6;                                    // operands that are read ahead of their product
 
-template <int D>
+template <int D, int BITS>
 __global__ void __launch_bounds__(512, 2)
 attend_many(const AttnArgs a) {
     constexpr int kU = D / 16, kCb = D / 32, kHalf = 64 * D * 2;
+    constexpr int kToken = D * BITS / 8;                    // bytes of a token's codes
     extern __shared__ __align__(16) uint8_t lds[];
     uint8_t* const s_k = lds;                               // [2][64][D] bf16
     uint8_t* const s_v = lds + 2 * kHalf;                   // [2][D][64] bf16
@@ -560,26 +517,26 @@ attend_many(const AttnArgs a) {
     const int tok0 = D == 128 ? wave * 8 : (wave & 3) * 16; // the wave's first token of the tile
     const int k_tok = lane / kKc, k_c = lane % kKc;         // from there: this lane's key, its 16 channels
     const int v_tok = lane / kVc * 4, v_c = lane % kVc;     // tokens v_tok .. + 3, channels 4 v_c .. + 3
-    const uint32_t k_lane = lane * 16, ks_lane = ((uint32_t)(k_c / 2) << a.page_shift) + k_tok;
-    const uint32_t v_lane = v_tok * D + v_c * 4, vs_lane = ((uint32_t)(v_c / 8) << a.page_shift) + v_tok;
+    const uint32_t k_lane = lane * (2 * BITS), ks_lane = ((uint32_t)(k_c / 2) << a.page_shift) + k_tok;
+    const uint32_t v_lane = v_tok * kToken + v_c * (BITS / 2), vs_lane = ((uint32_t)(v_c / 8) << a.page_shift) + v_tok;
     auto entry = [&](int t) {                               // page of the wave's tokens of the tile that starts with t
         return __builtin_amdgcn_readfirstlane(table[min((t + tok0) >> a.page_shift, last_page)]);
     };
-    u32x4 kw = {};
+    uint32_t kw[BITS / 2] = {};
     uint32_t kscale = 0, vw[4] = {}, vscale = 0;
     bool there = false;
     auto request = [&](int t, int page) {
         there = (uint32_t)page < (uint32_t)a.num_pages;
         const int64_t ph = (int64_t)(there ? page : 0) * a.kv_heads + h;
         const int off = (t + tok0) & page_mask;
-        const int64_t codes = ((ph << a.page_shift) + off) * D, scales = ((ph * (D / 32)) << a.page_shift) + off;
+        const int64_t codes = ((ph << a.page_shift) + off) * kToken, scales = ((ph * (D / 32)) << a.page_shift) + off;
         if (do_k) {
-            kw = *reinterpret_cast<const u32x4*>(a.k_codes + codes + k_lane);
+            load_words<BITS / 2>(kw, a.k_codes + codes + k_lane);
             kscale = a.k_scales[scales + ks_lane];
         }
         if (do_v) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) vw[e] = *reinterpret_cast<const uint32_t*>(a.v_codes + codes + v_lane + e * D);
+            for (int e = 0; e < 4; ++e) vw[e] = load_four<BITS>(a.v_codes + codes + v_lane + e * kToken);
             vscale = *reinterpret_cast<const uint32_t*>(a.v_scales + scales + vs_lane);
         }
     };
@@ -598,8 +555,7 @@ attend_many(const AttnArgs a) {
             const float sc = scale_operand(kscale);
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                *reinterpret_cast<u32x4*>(s_k + buf * kHalf + k_to[e]) =
-                    u32x4{cvt_lo(kw[2 * e], sc), cvt_hi(kw[2 * e], sc), cvt_lo(kw[2 * e + 1], sc), cvt_hi(kw[2 * e + 1], sc)};
+                *reinterpret_cast<bf16x8*>(s_k + buf * kHalf + k_to[e]) = cvt_eight<BITS>(kw + e * (BITS / 4), sc);
             if (k_c == 0 && ((tok0 + k_tok) & 15) == 0) s_ok[buf * 4 + (tok0 + k_tok) / 16] = there;
         }
         if (do_v) {
@@ -618,9 +574,9 @@ attend_many(const AttnArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float sc = scale_byte(vscale, e);
-                lo[e] = cvt_lo(vw[e], sc), hi[e] = cvt_hi(vw[e], sc);
+                lo[e] = cvt_pair<BITS>(vw + e, 0, sc), hi[e] = cvt_pair<BITS>(vw + e, 1, sc);
             }
-            if (partly_seen(t) && __ballot((odd_scales(vscale) | odd_codes(vw[0]) | odd_codes(vw[1]) | odd_codes(vw[2]) | odd_codes(vw[3])) != 0)) {
+            if (partly_seen(t) && __ballot((odd_scales(vscale) | (BITS == 8 ? odd_codes(vw[0]) | odd_codes(vw[1]) | odd_codes(vw[2]) | odd_codes(vw[3]) : 0u)) != 0)) {
                 odd = true;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) lo[e] &= ~odd_halves(lo[e]), hi[e] &= ~odd_halves(hi[e]);
@@ -732,14 +688,14 @@ attend_many(const AttnArgs a) {
             if (!partly_seen(tok & ~63) || tok < range.lo || (uint32_t)pg >= (uint32_t)a.num_pages) continue;
             const bool sees = tok >= row_lo && tok < row_hi;
             const int64_t ph = (int64_t)pg * a.kv_heads + h;
-            const uint8_t* p = a.v_codes + ((ph << a.page_shift) + (tok & page_mask)) * D + 4 * hh;
+            const uint8_t* p = a.v_codes + ((ph << a.page_shift) + (tok & page_mask)) * kToken + hh * (BITS / 2);
 #pragma unroll
             for (int c = 0; c < kCb; ++c) {
                 const float sc = scale_operand(a.v_scales[((ph * (D / 32) + c) << a.page_shift) + (tok & page_mask)]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const uint32_t w = *reinterpret_cast<const uint32_t*>(p + 32 * c + 8 * e);
-                    const uint32_t x = odd_halves(cvt_lo(w, sc)), y = odd_halves(cvt_hi(w, sc));
+                    const uint32_t w = load_four<BITS>(p + (32 * c + 8 * e) * BITS / 8);
+                    const uint32_t x = odd_halves(cvt_pair<BITS>(&w, 0, sc)), y = odd_halves(cvt_pair<BITS>(&w, 1, sc));
                     const uint32_t hit[4] = {x & 0xFFFFu, x >> 16, y & 0xFFFFu, y >> 16};
 #pragma unroll
                     for (int k = 0; k < 4; ++k) o[c][4 * e + k] += sees && hit[k] ? __builtin_nanf("") : 0.0f;
@@ -909,17 +865,17 @@ Plan plan(int head_dim, int group, int kv_heads, int batch, int total_q, int max
 int64_t few_units(const Plan& p, int batch, int kv_heads) { return p.max_parts > 1 ? (int64_t)batch * kv_heads * p.part_rows * p.max_parts : 0; }
 int64_t many_units(const Plan& p, int total_q, int q_heads) { return p.many_parts > 1 ? (int64_t)total_q * q_heads * p.many_parts : 0; }
 
-template <int D>
+template <int D, int BITS>
 hipError_t launch_attention(const AttnArgs& a, const Plan& p, int dev, hipStream_t stream) {
     if (p.many) {
-        if (hipError_t e = ensure_dynamic_lds<&attend_many<D>>(dev, many_lds<D>()); e != hipSuccess) return e;
-        attend_many<D><<<(unsigned)p.many_tiles * p.many_parts * a.kv_heads, 512, many_lds<D>(), stream>>>(a);
+        if (hipError_t e = ensure_dynamic_lds<&attend_many<D, BITS>>(dev, many_lds<D>()); e != hipSuccess) return e;
+        attend_many<D, BITS><<<(unsigned)p.many_tiles * p.many_parts * a.kv_heads, 512, many_lds<D>(), stream>>>(a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     if (p.few) {
         const unsigned units = (unsigned)a.batch * a.kv_heads * p.max_parts;
-        if (p.few_rows == 16) attend_few<D, 1><<<units, 256, 0, stream>>>(a);
-        else attend_few<D, 2><<<units, 256, 0, stream>>>(a);
+        if (p.few_rows == 16) attend_few<D, 1, BITS><<<units, 256, 0, stream>>>(a);
+        else attend_few<D, 2, BITS><<<units, 256, 0, stream>>>(a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     const unsigned few = p.max_parts > 1 ? (unsigned)a.batch * a.kv_heads * p.part_rows : 0;
@@ -962,7 +918,7 @@ size_t paged_attention_workspace_bytes(const batq_paged_cache& c, int q_heads, i
     return (size_t)units * (c.head_dim + 2) * 4;
 }
 
-hipError_t launch_paged_attention(const batq_paged_cache& c, const batq_paged_batch& b, const void* q, int64_t ldq,
+hipError_t launch_paged_attention(const batq_paged_cache& c, int bits, const batq_paged_batch& b, const void* q, int64_t ldq,
                                   int q_heads, float scale, bool causal, int window, void* out, int64_t ldo, float* lse,
                                   void* workspace, hipStream_t stream) {
     int dev = 0;
@@ -975,13 +931,10 @@ hipError_t launch_paged_attention(const batq_paged_cache& c, const batq_paged_ba
     Plan p = plan(c.head_dim, q_heads / c.kv_heads, c.kv_heads, b.batch, b.total_q, b.max_q, b.max_kv, causal ? window : 0, cus);
     if (part_bytes(p, c, q_heads, b.batch, b.total_q) > part_bytes(full, c, q_heads, b.batch, b.total_q)) p = full;
     AttnArgs a = {};
+    set_lists(a, c, b, q_heads, causal, window);
     a.q = static_cast<const uint16_t*>(q), a.ldq = ldq, a.ldo = ldo, a.out = static_cast<uint16_t*>(out), a.lse = lse;
     a.k_codes = c.k_codes, a.k_scales = c.k_scales, a.v_codes = c.v_codes, a.v_scales = c.v_scales;
-    a.cu_q = b.cu_q, a.kv_len = b.kv_len, a.page_table = b.page_table, a.batch = b.batch, a.table_width = b.table_width;
-    a.total_q = b.total_q, a.max_q = b.max_q, a.max_kv = b.max_kv, a.num_pages = c.num_pages;
-    a.page_shift = __builtin_ctz((unsigned)c.page_size);
-    a.q_heads = q_heads, a.kv_heads = c.kv_heads, a.group = q_heads / c.kv_heads;
-    a.causal = causal, a.window = window, a.scale = scale * 1.4426950408889634f;
+    a.scale = scale * 1.4426950408889634f;
     a.few_rows = p.few_rows, a.few_len = p.few_len, a.max_parts = p.max_parts, a.part_rows = p.part_rows;
     a.many_len = p.many_len, a.many_parts = p.many_parts;
     const size_t few = (size_t)few_units(p, b.batch, c.kv_heads), many = (size_t)many_units(p, b.total_q, q_heads);
@@ -989,7 +942,8 @@ hipError_t launch_paged_attention(const batq_paged_cache& c, const batq_paged_ba
     a.part_ml = a.part_o + few * c.head_dim;
     a.many_o = a.part_ml + few * 2;
     a.many_ml = a.many_o + many * c.head_dim;
-    return c.head_dim == 64 ? launch_attention<64>(a, p, dev, stream) : launch_attention<128>(a, p, dev, stream);
+    if (bits == 8) return c.head_dim == 64 ? launch_attention<64, 8>(a, p, dev, stream) : launch_attention<128, 8>(a, p, dev, stream);
+    return c.head_dim == 64 ? launch_attention<64, 4>(a, p, dev, stream) : launch_attention<128, 4>(a, p, dev, stream);
 }
 
 }  // namespace batq

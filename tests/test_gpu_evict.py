@@ -1,0 +1,496 @@
+"""Scores of cached tokens and eviction by them (batq_kv_paged_score, batq_kv_paged_evict), against plain 64-bit statements, and a
+decoder that lives within a budget of tokens."""
+import numpy as np
+import pytest
+
+from gpu_util import require_gpu, to_dev, y_to_f32
+import budget_ref as br
+import serving_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    require_gpu()
+    import paper_2603_16590_amd as b
+    return b
+
+
+def dev(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def make_cache(B, arrays, bits):
+    pages, heads, page, D = arrays[0].shape
+    return B.PagedCache(pages, page, heads, D * 8 // bits, tensors=[dev(a) for a in arrays], bits=bits)
+
+
+def host(cache):
+    return [t.cpu().numpy() for t in (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)]
+
+
+def lse_of(arrays, bits, q, cu, lens, table, page, causal, window, T):
+    """fp32 lse of the attention, 7 in rows of no sequence."""
+    kv = br.values(*arrays[:2], bits)
+    x = ref.attention(kv, np.zeros_like(kv), q, cu, lens, table, page, kv.shape[-1] ** -0.5, causal, window, T)[1]
+    return np.where(np.isnan(x) & (np.arange(T) >= cu[-1])[:, None], 7.0, x).astype(np.float32)
+
+
+def run_score(B, cache, qd, lse, had, cu, lens, table, max_q=None, max_kv=None, **kw):
+    import torch
+    score = dev(had)
+    B.batq_kv_paged_score(cache, qd, dev(lse), score, dev(cu), dev(lens), dev(table), int(np.diff(cu).max()) if max_q is None else max_q,
+                          int(max(lens)) if max_kv is None else max_kv, **kw)
+    torch.cuda.synchronize()
+    return score.cpu().numpy()
+
+
+SCORE = [
+    # lens, query counts, q heads, kv heads, D, page, window
+    ([1], [1], 1, 1, 64, 16, 0),
+    ([1, 15, 16, 17, 63, 64, 65, 129], [1] * 8, 8, 2, 128, 16, 0),
+    ([0, 5, 0, 300], [1, 1, 2, 1], 7, 1, 128, 32, 0),
+    ([700, 3, 1025], [1, 1, 1], 28, 4, 64, 64, 0),
+    ([513, 40], [3, 2], 8, 4, 64, 256, 0),
+    ([200, 90], [5, 7], 6, 2, 128, 16, 33),
+    ([333], [333], 3, 3, 64, 32, 0),
+    ([290], [290], 8, 1, 128, 16, 0),
+    ([130, 64, 257, 1], [130, 1, 100, 1], 14, 2, 128, 64, 0),
+    ([200, 140], [70, 140], 4, 4, 128, 32, 1),
+    ([500], [129], 2, 1, 64, 16, 100),
+    ([700, 600], [0, 2], 128, 1, 128, 16, 0),               # a sequence without queries
+    ([5, 9], [9, 20], 4, 2, 64, 16, 0),                     # more queries than tokens
+    ([3000, 200], [64, 64], 4, 1, 128, 64, 0),
+    ([900], [900], 16, 2, 64, 64, 301),
+]
+
+
+@pytest.mark.parametrize("lens,qs,hq,hkv,D,page,window", SCORE)
+@pytest.mark.parametrize("bits,causal,add", [(4, True, False), (8, True, True), (4, False, True)])
+def test_score(B, lens, qs, hq, hkv, D, page, window, bits, causal, add):
+    rng = np.random.default_rng(sum(lens) + sum(qs) + hq)
+    arrays, qbits, q, cu, lens, table, T = br.batch_case(rng, lens, qs, hq, hkv, D, page, bits, spare=2)
+    lse = lse_of(arrays, bits, q, cu, lens, table, page, causal, window, T)
+    had = rng.uniform(0, 3, (arrays[0].shape[0], hkv, page)).astype(np.float32)
+    got = run_score(B, make_cache(B, arrays, bits), to_dev(qbits, "bf16"), lse, had, cu, lens, table, causal=causal, window=window, add=add)
+    want = br.score(br.values(*arrays[:2], bits), q, lse, had, cu, lens, table, page, D ** -0.5, causal, window, add)
+    br.assert_score(got, want, had)
+
+
+def test_scores_add_up_to_the_number_of_rows(B):
+    """The weights of a row that sees something add up to 1: with the library's own lse, over all tokens of a key head."""
+    import torch
+    rng = np.random.default_rng(1)
+    hq, hkv, D, page = 12, 3, 128, 32
+    arrays, qbits, q, cu, lens, table, T = br.batch_case(rng, [1200, 77, 300], [200, 77, 1], hq, hkv, D, page, 4)
+    cache, qd = make_cache(B, arrays, 4), to_dev(qbits, "bf16")
+    lse = torch.empty((T, hq), device="cuda")
+    B.batq_paged_attention(cache, qd, dev(cu), dev(lens), dev(table), 200, 1200, lse=lse)
+    score = torch.full((arrays[0].shape[0], hkv, page), -1.0, device="cuda")
+    B.batq_kv_paged_score(cache, qd, lse, score, dev(cu), dev(lens), dev(table), 200, 1200)
+    got = score.double().cpu().numpy()
+    for b, n in enumerate(np.diff(cu)):
+        t = np.arange(lens[b])
+        total = got[table[b, t // page], :, t % page].sum(0)
+        assert np.all(np.abs(total / (n * hq / hkv) - 1) < 1e-4)
+
+
+def test_score_of_some_queries_and_other_scales(B):
+    """The last queries of a prompt alone (their rows of q and lse), column ranges of wider tensors, a scale."""
+    import torch
+    rng = np.random.default_rng(2)
+    hq, hkv, D, page, scale = 8, 2, 64, 16, 0.3
+    arrays, qbits, q, cu, lens, table, T = br.batch_case(rng, [400, 90], [60, 32], hq, hkv, D, page, 8)
+    kv = br.values(*arrays[:2], 8)
+    lse = ref.attention(kv, np.zeros_like(kv), q, cu, lens, table, page, scale, True, 0, T)[1].astype(np.float32)
+    rows = np.concatenate([np.arange(cu[b + 1] - 32, cu[b + 1]) for b in range(2)])
+    cu2 = np.array([0, 32, 64], np.int32)
+    wide = torch.zeros((64, hq * D + 64), dtype=torch.bfloat16, device="cuda")
+    wide[:, : hq * D] = to_dev(qbits, "bf16")[torch.from_numpy(rows).cuda()]
+    had = np.full((arrays[0].shape[0], hkv, page), 5.0, np.float32)
+    got = run_score(B, make_cache(B, arrays, 8), wide[:, : hq * D], lse[rows], had, cu2, lens, table, scale=scale)
+    br.assert_score(got, br.score(kv, q[rows], lse[rows], had, cu2, lens, table, page, scale, True, 0, False), had)
+
+
+def test_score_does_not_trust_its_lists(B):
+    """Pages outside the cache, lengths past the table, negative ones, bounds below what the lists say, rows outside q."""
+    rng = np.random.default_rng(6)
+    hq, hkv, D, page = 4, 2, 128, 16
+    arrays, qbits, q, cu, lens, table, T = br.batch_case(rng, [100, 40, 64, 90], [1, 3, 20, 1], hq, hkv, D, page, 4, spare=2)
+    kv, qd = br.values(*arrays[:2], 4), to_dev(qbits, "bf16")
+    table[0, 2], table[2, 0], table[2, 3], table[1, 0] = -1, 10 ** 6, -2 ** 31, 2 ** 31 - 1
+    table[3, :] = -1
+    cache = make_cache(B, arrays, 4)
+    lse = np.nan_to_num(lse_of(arrays, 4, q, cu, lens, table, page, True, 0, T), neginf=-np.inf)
+    had = rng.uniform(0, 3, (arrays[0].shape[0], hkv, page)).astype(np.float32)
+    for add in (False, True):
+        got = run_score(B, cache, qd, lse, had, cu, lens, table, max_kv=128, add=add)
+        br.assert_score(got, br.score(kv, q, lse, had, cu, lens, table, page, D ** -0.5, True, 0, add), had)
+        # the first two queries of each; tokens up to 50
+        got = run_score(B, cache, qd, lse, had, cu, lens, table, max_q=2, max_kv=50, add=add)
+        br.assert_score(got, br.score(kv, q, lse, had, cu, np.minimum(lens, 50), table, page, D ** -0.5, True, 0, add, max_q=2), had)
+        longer = lens.copy()
+        longer[1], longer[3] = -5, 10 ** 9
+        got = run_score(B, cache, qd, lse, had, cu, longer, table, max_kv=10 ** 6, add=add)
+        eff = np.array([100, 0, 64, table.shape[1] * page])
+        br.assert_score(got, br.score(kv, q, lse, had, cu, eff, table, page, D ** -0.5, True, 0, add), had)
+        for broken in ([0, 1, 4, 24, 10 ** 6], [0, -1, 4, 24, 25]):
+            got = run_score(B, cache, qd, lse, had, np.array(broken, np.int32), lens, table, max_q=20, max_kv=128, add=add)
+            t = np.arange(16, 64 - 20)                      # sequence 2 keeps its rows (0 and 3 are pages that do not exist)
+            want = br.score(kv, q, lse, had, cu, lens, table, page, D ** -0.5, True, 0, add)
+            t = t[(t // page == 1) | (t // page == 2)]
+            at = (table[2, t // page], slice(None), t % page)
+            assert np.all(np.abs(got[at] - want[0][at]) <= want[1][at])
+
+
+def test_score_of_keys_and_rows_that_are_not_finite(B):
+    """A NaN key makes the lse of the rows that see it NaN, and with it the scores of all tokens that they see; other tokens' stay."""
+    rng = np.random.default_rng(7)
+    hq, hkv, D, page = 4, 2, 64, 16
+    arrays, qbits, q, cu, lens, table, T = br.batch_case(rng, [200, 90], [120, 1], hq, hkv, D, page, 4)
+    arrays[1][table[0, 150 // page], 1, 0, 150 % page] = 255
+    lse = lse_of(arrays, 4, q, cu, lens, table, page, True, 30, T)
+    assert np.isnan(lse).any()
+    had = np.ones((arrays[0].shape[0], hkv, page), np.float32)
+    got = run_score(B, make_cache(B, arrays, 4), to_dev(qbits, "bf16"), lse, had, cu, lens, table, window=30)
+    want, tol = br.score(br.values(*arrays[:2], 4), q, lse, had, cu, lens, table, page, D ** -0.5, True, 30, False)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.isnan(want).any() and not np.isnan(want).all()
+    fine = ~np.isnan(want)
+    br.assert_score(np.where(fine, got, 0.0), (np.where(fine, want, 0.0), np.where(fine, tol, 0.0)), np.where(fine, had, 0.0))
+
+
+# ---------------------------------------------------------------------------------------- eviction
+EVICT = [
+    # lens, kv heads, D, page, budget, first, last
+    ([1], 1, 64, 16, 1, 0, 0),
+    ([2], 1, 64, 16, 1, 0, 0),
+    ([40, 17, 0, 16, 300], 2, 128, 16, 16, 1, 3),
+    ([40, 17, 0, 16, 300], 3, 64, 32, 17, 0, 0),
+    ([1000, 999, 5], 2, 64, 64, 333, 4, 100),
+    ([100], 2, 128, 16, 64, 32, 32),                        # nothing left to choose
+    ([100, 70], 1, 128, 256, 64, 64, 0),
+    ([100, 70], 1, 64, 16, 64, 0, 64),
+    ([2500, 2049], 2, 64, 16, 2048, 4, 64),
+    ([70, 80], 2, 64, 16, 200, 4, 64),                      # all stay
+    ([5000], 1, 64, 128, 1, 0, 0),
+    ([9000, 4097], 1, 64, 32, 1025, 1, 1),
+]
+
+
+def evict_case(rng, lens, hkv, D, page, budget, bits):
+    lens = np.array(lens)
+    fresh = -(-np.minimum(lens, budget) // page)
+    arrays, _, _, _, lens, table, _ = br.batch_case(rng, lens, np.zeros(len(lens), int), 1 * hkv, hkv, D, page, bits, more_pages=int(fresh.sum()) + 2)
+    free = np.setdiff1d(np.arange(arrays[0].shape[0]), table)
+    rng.shuffle(free)
+    out_table = np.full((len(lens), max(1, int(fresh.max()))), -9, np.int32)
+    at = 0
+    for b, n in enumerate(fresh):
+        out_table[b, :n] = free[at: at + n]
+        at += n
+    return arrays, lens, table, out_table
+
+
+def scores_for(rng, kind, shape):
+    x = rng.standard_normal(shape).astype(np.float32)
+    if kind == "sums":                                      # what sums of weights look like
+        x = np.exp(3 * x - 4).astype(np.float32)
+    elif kind == "ties":
+        x = np.round(2 * x).astype(np.float32) * np.float32(0.25)
+        x[x == 0] *= np.float32(-1.0)                       # some zeros are -0
+    elif kind == "same":
+        x[...] = 0.5
+    elif kind == "close":                                   # all bits but the last ones are the same
+        x = (np.float32(1.0).view(np.uint32) + rng.integers(0, 40, shape, dtype=np.uint32)).astype(np.uint32).view(np.float32)
+    elif kind == "odd":
+        x[rng.random(shape) < 0.2] = np.nan
+        x[rng.random(shape) < 0.1] = np.inf
+        x[rng.random(shape) < 0.1] = -np.inf
+        x[rng.random(shape) < 0.05] = -np.nan
+        x[rng.random(shape) < 0.05] = np.float32(1e-42)
+    return x
+
+
+def run_evict(B, cache, score, lens, table, out_table, budget, first, last, max_kv=None, **kw):
+    import torch
+    ds = dev(score)
+    keep, new_len = B.batq_kv_paged_evict(cache, ds, dev(lens), dev(table), dev(out_table), int(max(lens)) if max_kv is None else max_kv,
+                                          budget, first, last, **kw)
+    torch.cuda.synchronize()
+    return host(cache), ds.cpu().numpy(), keep.cpu().numpy(), new_len.cpu().numpy()
+
+
+def assert_evicted(got, want):
+    assert np.array_equal(got[3], want[3]) and np.array_equal(got[2], want[2])
+    for g, w, name in zip(got[0], want[0], ("k codes", "k scales", "v codes", "v scales")):
+        assert np.array_equal(g, w), name
+    assert np.array_equal(got[1].view(np.uint32), want[1].view(np.uint32))
+
+
+@pytest.mark.parametrize("lens,hkv,D,page,budget,first,last", EVICT)
+@pytest.mark.parametrize("kind,bits", [("sums", 4), ("ties", 8), ("same", 4), ("close", 8), ("odd", 4)])
+def test_evict(B, lens, hkv, D, page, budget, first, last, kind, bits):
+    rng = np.random.default_rng(sum(lens) + budget)
+    arrays, lens, table, out_table = evict_case(rng, lens, hkv, D, page, budget, bits)
+    score = scores_for(rng, kind, (arrays[0].shape[0], hkv, page))
+    got = run_evict(B, make_cache(B, arrays, bits), score, lens, table, out_table, budget, first, last)
+    assert_evicted(got, br.evict(arrays, score, lens, table, out_table, budget, first, last))
+
+
+def test_evict_of_a_long_sequence(B):
+    rng = np.random.default_rng(3)
+    arrays, lens, table, out_table = evict_case(rng, [70000, 33], 2, 64, 256, 20000, 4)
+    score = scores_for(rng, "sums", (arrays[0].shape[0], 2, 256))
+    got = run_evict(B, make_cache(B, arrays, 4), score, lens, table, out_table, 20000, 3, 500)
+    assert_evicted(got, br.evict(arrays, score, lens, table, out_table, 20000, 3, 500))
+
+
+def test_evict_does_not_trust_its_lists(B):
+    """Pages outside the cache on either side, lengths past the table, past max_kv, negative ones."""
+    rng = np.random.default_rng(4)
+    hkv, D, page, budget = 2, 64, 16, 40
+    arrays, lens, table, out_table = evict_case(rng, [100, 64, 90, 48], hkv, D, page, budget, 4)
+    table[0, 1], table[0, 3], table[1, :], table[2, 5], out_table[2, 1], out_table[3, 0] = -1, 10 ** 6, -2 ** 31, 2 ** 31 - 1, -3, 10 ** 8
+    score = scores_for(rng, "odd", (arrays[0].shape[0], hkv, page))
+    got = run_evict(B, make_cache(B, arrays, 4), score, lens, table, out_table, budget, 2, 5)
+    assert_evicted(got, br.evict(arrays, score, lens, table, out_table, budget, 2, 5))
+    told = np.array([10 ** 9, 64, -7, 48], np.int32)
+    eff = np.array([table.shape[1] * page, 64, 0, 48])
+    got = run_evict(B, make_cache(B, arrays, 4), score, told, table, out_table, budget, 2, 5, max_kv=10 ** 6)
+    assert_evicted(got, br.evict(arrays, score, eff, table, out_table, budget, 2, 5))
+    got = run_evict(B, make_cache(B, arrays, 4), score, lens, table, out_table, budget, 2, 5, max_kv=50)
+    assert_evicted(got, br.evict(arrays, score, np.minimum(lens, 50), table, out_table, budget, 2, 5))
+
+
+def test_evict_from_shared_pages(B):
+    """Two sequences with a common prefix: its pages are read by both and stay as they are."""
+    rng = np.random.default_rng(5)
+    hkv, D, page, budget = 1, 128, 16, 20
+    arrays, lens, table, out_table = evict_case(rng, [80, 60], hkv, D, page, budget, 8)
+    table[1, :3] = table[0, :3]
+    score = scores_for(rng, "sums", (arrays[0].shape[0], hkv, page))
+    got = run_evict(B, make_cache(B, arrays, 8), score, lens, table, out_table, budget, 1, 2)
+    assert_evicted(got, br.evict(arrays, score, lens, table, out_table, budget, 1, 2))
+
+
+def test_offsets_past_four_gigabytes(B):
+    """Codes and scores at either end of a pool of 4.3 GB per array."""
+    import torch
+    rng = np.random.default_rng(8)
+    hq, hkv, D, page, L, budget = 4, 2, 128, 256, 500, 300
+    pages = (1 << 32) // (page * D * hkv) + 1000
+    cache = B.PagedCache(pages, page, hkv, D, bits=8)
+    ids, out_ids = np.array([[pages - 1, 3]], np.int32), np.array([[5, pages - 2]], np.int32)
+    X = to_dev(ref.bf16_values(rng, L, 2 * hkv * D)[0], "bf16")
+    t = np.arange(L)
+    B.batq_kv_paged_append(cache, X[:, : hkv * D], X[:, hkv * D:], dev(ids[0].astype(np.int64)[t // page] * page + t % page))
+    both = torch.tensor(np.concatenate([ids[0], out_ids[0]]).astype(np.int64), device="cuda")
+    score = torch.zeros((pages, hkv, page), device="cuda")
+    qbits, q = ref.bf16_values(rng, 2, hq * D)
+    lse, cu, lens = torch.empty((2, hq), device="cuda"), np.array([0, 2], np.int32), np.array([L], np.int32)
+    small = [a[both].cpu().numpy() for a in (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)]
+    B.batq_paged_attention(cache, to_dev(qbits, "bf16"), dev(cu), dev(lens), dev(ids), 2, L, lse=lse)
+    B.batq_kv_paged_score(cache, to_dev(qbits, "bf16"), lse, score, dev(cu), dev(lens), dev(ids), 2, L)
+    had = np.zeros((4, hkv, page), np.float32)
+    got = score[both].cpu().numpy()
+    br.assert_score(got, br.score(br.values(*small[:2], 8), q.reshape(2, hq, D).astype(np.float64), lse.cpu().numpy(), had, cu, lens,
+                                  np.array([[0, 1]]), page, D ** -0.5, True, 0, False), had)
+    keep, new_len = B.batq_kv_paged_evict(cache, score, dev(lens), dev(ids), dev(out_ids), L, budget, 4, 50)
+    torch.cuda.synchronize()
+    after = [a[both].cpu().numpy() for a in (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)]
+    want = br.evict(small, got, lens, np.array([[0, 1]]), np.array([[2, 3]]), budget, 4, 50)
+    assert_evicted((after, score[both].cpu().numpy(), keep.cpu().numpy(), new_len.cpu().numpy()), want)
+
+
+def test_repeatable_on_streams_and_in_graphs(B):
+    """Same bits on another stream with a workspace full of anything, and from replays of a graph of score and eviction with eager work
+    and other lengths in between."""
+    import torch
+    rng = np.random.default_rng(9)
+    hq, hkv, D, page, budget = 8, 2, 128, 16, 256
+    lens0 = [3000, 700, 90]
+    arrays, lens, table, out_table = evict_case(rng, lens0, hkv, D, page, budget, 4)
+    cu, T = np.array([0, 300, 301, 303], np.int32), 303
+    qd = to_dev(ref.bf16_values(rng, T, hq * D)[0], "bf16")
+    dlens, dtable, dout, dcu = dev(lens), dev(table), dev(out_table), dev(cu)
+    cache = make_cache(B, arrays, 4)
+    had = dev(rng.uniform(0, 1, (arrays[0].shape[0], hkv, page)).astype(np.float32))
+    lse = torch.empty((T, hq), device="cuda")
+    ws1 = torch.full((max(256, B.batq_kv_paged_score_workspace(cache, hq, 3, T, 300, 3000)),), 0xFF, dtype=torch.uint8, device="cuda")
+    ws2 = torch.full((max(256, B.batq_kv_paged_evict_workspace(cache, 3, 3000, budget)),), 0xFF, dtype=torch.uint8, device="cuda")
+
+    def step(score, keep, new_len):
+        B.batq_paged_attention(cache, qd, dcu, dlens, dtable, 300, 3000, lse=lse)
+        B.batq_kv_paged_score(cache, qd, lse, score, dcu, dlens, dtable, 300, 3000, add=True, workspace=ws1)
+        B.batq_kv_paged_evict(cache, score, dlens, dtable, dout, 3000, budget, 4, 16, keep=keep, new_len=new_len, workspace=ws2)
+
+    def fresh():
+        return had.clone(), torch.zeros((3, hkv, budget), dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+
+    want = fresh()
+    step(*want)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = fresh()
+    with torch.cuda.stream(side):
+        side.wait_stream(torch.cuda.default_stream())
+        step(*got)
+    side.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    g, held = torch.cuda.CUDAGraph(), fresh()
+    with torch.cuda.graph(g, stream=side):
+        step(*held)
+    for rep in range(3):
+        dlens.copy_(torch.tensor([3000 - 500 * rep, 700 - rep, 90 - rep], dtype=torch.int32))
+        want = fresh()
+        step(*want)
+        codes = host(cache)
+        junk = torch.randn(300, 300, device="cuda") @ torch.randn(300, 300, device="cuda")
+        held[0].copy_(had)
+        held[1].fill_(-5)
+        ws1.fill_(0x7F), ws2.fill_(0x7F)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(held, want)), rep
+        assert all(np.array_equal(x, y) for x, y in zip(codes, host(cache)))
+        assert bool(torch.isfinite(junk).all())
+
+
+def test_two_evictions_and_scores_at_once(B):
+    """Calls on two streams with caches and workspaces of their own do not meet."""
+    import torch
+    rng = np.random.default_rng(10)
+    hq, hkv, D, page, budget = 4, 1, 64, 16, 100
+    sides = []
+    for lens in ([4000, 50], [130, 2222, 700]):
+        arrays, lens, table, out_table = evict_case(rng, lens, hkv, D, page, budget, 4)
+        n = len(lens)
+        cu = np.arange(0, 40 * n + 1, 40).astype(np.int32)
+        score = scores_for(rng, "sums", (arrays[0].shape[0], hkv, page))
+        sides.append((make_cache(B, arrays, 4), to_dev(ref.bf16_values(rng, 40 * n, hq * D)[0], "bf16"), torch.zeros((40 * n, hq), device="cuda"),
+                      dev(score), dev(cu), dev(lens), dev(table), dev(out_table), int(max(lens)), torch.cuda.Stream()))
+
+    def run(s):
+        score = s[3].clone()
+        B.batq_kv_paged_score(s[0], s[1], s[2], score, s[4], s[5], s[6], 40, s[8], add=True)
+        return (score,) + B.batq_kv_paged_evict(s[0], score, s[5], s[6], s[7], s[8], budget, 1, 10)
+
+    want = [run(s) for s in sides]
+    torch.cuda.synchronize()
+    for rep in range(3):
+        got = []
+        for s in sides:
+            with torch.cuda.stream(s[9]):
+                got.append([run(s) for _ in range(3)][-1])
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for a, b in zip(got, want) for x, y in zip(a, b)), rep
+
+
+def test_binding_refuses_what_does_not_fit(B):
+    import torch
+    cache = B.PagedCache(6, 16, 2, 64, bits=4)
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    q, lse = torch.zeros((3, 256), dtype=torch.bfloat16, device="cuda"), torch.zeros((3, 4), device="cuda")
+    score = torch.zeros((6, 2, 16), device="cuda")
+    good = (cache, q, lse, score, i32(0, 3), i32(5), i32(0, 1).view(1, 2), 3, 5)
+    B.batq_kv_paged_score(*good)
+    for k, bad in ((1, q.float()), (1, q.cpu()), (2, lse[:2]), (2, lse.double()), (3, score[:5]), (3, score.half()), (3, score.cpu()),
+                   (4, i32(0, 3).long()), (5, i32(5).cpu()), (6, i32(0, 1))):
+        with pytest.raises(ValueError):
+            B.batq_kv_paged_score(*good[:k], bad, *good[k + 1:])
+    good = (cache, score, i32(25), i32(0, 1).view(1, 2), i32(2).view(1, 1), 32, 10)
+    B.batq_kv_paged_evict(*good)
+    for k, bad in ((1, score[:5]), (2, i32(5).long()), (3, i32(0, 1)), (4, i32(2))):
+        with pytest.raises(ValueError):
+            B.batq_kv_paged_evict(*good[:k], bad, *good[k + 1:])
+    with pytest.raises(B.BatqError):
+        B.batq_kv_paged_evict(*good, first=6, last=5)       # more than the budget
+    with pytest.raises(B.BatqError):
+        B.batq_kv_paged_evict(*good[:-1], 30)               # out_table has room for 16
+    with pytest.raises(B.BatqError):
+        B.batq_kv_paged_evict(*good, new_len=good[2])
+    with pytest.raises(ValueError):
+        B.batq_kv_paged_evict(*good, keep=torch.zeros((1, 2, 9), dtype=torch.int32, device="cuda"))
+    with pytest.raises(ValueError):
+        B.PagedCache(6, 16, 2, 64, tensors=[cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales])    # 8 bits
+
+
+# ---------------------------------------------------------------------------------------- together
+@pytest.mark.parametrize("bits", [4, 8])
+def test_decoding_within_a_budget(B, bits):
+    """Two prompts are appended, attended and scored, cut down to a budget, and decoded on: append, attention, score a step, an
+    eviction into fresh pages whenever a sequence has grown by half of the budget.  Every call is checked against its statement on what
+    the cache holds then."""
+    import torch
+    rng = np.random.default_rng(12)
+    hq, hkv, D, page, budget, first, last = 4, 2, 64, 16, 32, 2, 8
+    pages, width = 24, 6
+    cache = B.PagedCache(pages, page, hkv, D, bits=bits)
+    score = torch.full((pages, hkv, page), 1e9, device="cuda")        # whatever the pages' last owners have left
+    G, P = (np.eye(4) + 0.05 * rng.standard_normal((4, 4))).astype(np.float32), (np.eye(8) + 0.05 * rng.standard_normal((hkv * D // 32, 8, 8))).astype(np.float32)
+    tk = B.Transform(hkv * D, G, P, None)
+    rope = dev(ref.rope_table(400, D))
+    free = list(rng.permutation(pages))
+    table = np.full((2, width), -1, np.int32)
+    lens, pos = np.zeros(2, np.int64), np.zeros(2, np.int64)
+
+    def grow(n):
+        for b in range(2):
+            for i in range(-(-int(lens[b] + n[b]) // page)):
+                if table[b, i] < 0:
+                    table[b, i] = free.pop()
+
+    def step(n):
+        """n[b] new tokens of each sequence."""
+        nonlocal lens, pos
+        grow(n)
+        M = int(sum(n))
+        X = to_dev(ref.bf16_values(rng, M, (hq + 2 * hkv) * D)[0], "bf16")
+        q, k, v = X.split((hq * D, hkv * D, hkv * D), 1)
+        at = np.concatenate([lens[b] + np.arange(n[b]) for b in range(2)])
+        owner = np.repeat([0, 1], n)
+        slots = table[owner, at // page].astype(np.int64) * page + at % page
+        p = np.concatenate([pos[b] + np.arange(n[b]) for b in range(2)]).astype(np.int32)
+        qr = B.batq_kv_paged_append(cache, k, v, dev(slots), dev(p), q=q, rope=rope, tk=tk)
+        lens, pos = lens + n, pos + n
+        cu, l32 = np.array([0, n[0], M], np.int32), lens.astype(np.int32)
+        lse = torch.empty((M, hq), device="cuda")
+        had = score.cpu().numpy()
+        out = B.batq_paged_attention(cache, qr, dev(cu), dev(l32), dev(table), max(n), width * page, lse=lse)
+        B.batq_kv_paged_score(cache, qr, lse, score, dev(cu), dev(l32), dev(table), max(n), width * page, add=True)
+        torch.cuda.synchronize()
+        arrays = host(cache)
+        kv, vv = br.values(*arrays[:2], bits), br.values(*arrays[2:], bits)
+        qf = y_to_f32(qr).astype(np.float64).reshape(M, hq, D)
+        want = ref.attention(kv, vv, qf, cu, l32, table, page, D ** -0.5, True, 0, M)
+        ref.assert_attention(y_to_f32(out).astype(np.float64).reshape(M, hq, D), lse.cpu().numpy().astype(np.float64), want)
+        got = score.cpu().numpy()
+        br.assert_score(got, br.score(kv, qf, lse.cpu().numpy(), had, cu, l32, table, page, D ** -0.5, True, 0, True), had)
+
+    def evict():
+        nonlocal lens
+        kept = np.minimum(lens, budget)
+        out_table = np.full((2, budget // page), -1, np.int32)
+        for b in range(2):
+            out_table[b, : -(-int(kept[b]) // page)] = [free.pop() for _ in range(-(-int(kept[b]) // page))]
+        before, had = host(cache), score.cpu().numpy()
+        keep, new_len = B.batq_kv_paged_evict(cache, score, dev(lens.astype(np.int32)), dev(table), dev(out_table), width * page, budget, first, last)
+        torch.cuda.synchronize()
+        assert_evicted((host(cache), score.cpu().numpy(), keep.cpu().numpy(), new_len.cpu().numpy()),
+                       br.evict(before, had, lens, table, out_table, budget, first, last))
+        free.extend(int(x) for x in table[table >= 0])
+        table[...] = -1
+        table[:, : budget // page] = out_table
+        lens = new_len.cpu().numpy().astype(np.int64)
+
+    step([70, 25])
+    evict()
+    assert list(lens) == [32, 25]
+    for i in range(40):
+        step([1, 1])
+        if max(lens) >= budget + 16:
+            evict()
+    assert list(pos) == [110, 65] and max(lens) < budget + 16
