@@ -1050,7 +1050,7 @@ static batq_status check_evict_dims(const batq_paged_cache* c, int batch, int ma
 size_t batq_kv_paged_evict_workspace(const batq_paged_cache* cache, int batch, int max_kv, int budget) {
     if (check_evict_dims(cache, batch, max_kv, budget) != BATQ_OK) return 0;
     const int cus = current_compute_units();
-    return cus ? batq::paged_evict_workspace_bytes(*cache, batch, max_kv, budget, cus) : 0;
+    return cus ? batq::paged_evict_workspace_bytes(*cache, batch, max_kv, cus) : 0;
 }
 
 batq_status batq_kv_paged_evict(const batq_paged_cache* cache, int cache_bits, float* score, const int32_t* kv_len,
@@ -1073,7 +1073,7 @@ batq_status batq_kv_paged_evict(const batq_paged_cache* cache, int cache_bits, f
     if (batq_status st = check_device(); st != BATQ_OK) return st;
     const int cus = current_compute_units();
     if (!cus) return BATQ_ERR_DEVICE;
-    const size_t need = batq::paged_evict_workspace_bytes(*cache, batch, max_kv, budget, cus);
+    const size_t need = batq::paged_evict_part_bytes(*cache, batch, max_kv, cus);
     if (need > workspace_bytes || (need > 0 && !workspace)) return BATQ_ERR_WORKSPACE;
     BATQ_HIP(batq::launch_kv_paged_evict(*cache, cache_bits, score, kv_len, page_table, table_width, out_table, out_width, batch, max_kv,
                                          budget, first, last, keep, new_len, workspace, static_cast<hipStream_t>(stream)));

@@ -13,6 +13,9 @@ struct EvictArgs {
     float* score;
     int32_t *keep, *new_len;
     uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    int team_chunks;                                        // of a (sequence, key head), where several workgroups choose
+    uint32_t* team;                                         // [sequence][key head][3][kBins] histograms
+    int2* team_counts;                                      // [sequence][key head][chunk] keys above the border, on it
 };
 
 __device__ __forceinline__ int tokens_of(const EvictArgs& a, int b) {
@@ -26,89 +29,254 @@ __device__ __forceinline__ uint32_t order_of(float x) {
     return u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u);
 }
 
-constexpr int kWaves = 16;
+// The border between what stays and what goes is the k-th largest key, found eleven bits at a time from the highest: a histogram
+// of the keys that begin with the bits found so far, and the bin in which the k-th is.  Equal keys stay in the order of their tokens.
+constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 2048, kCopies = 8;
+__device__ __forceinline__ int shift_of(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+__device__ __forceinline__ uint32_t bin_of(uint32_t key, int pass) { return (key >> shift_of(pass)) & (pass == 2 ? 1023u : 2047u); }
+// Whether a key begins with the bits found before the pass.
+__device__ __forceinline__ bool begins(uint32_t key, uint32_t found, int pass) { return pass == 0 || ((key ^ found) >> shift_of(pass - 1)) == 0; }
 
-// A workgroup to a (sequence, key head): the k-th largest key by its bytes from the highest, each from a histogram of the
-// keys that share the bytes above it, then one pass in order that lists what stays.
-__global__ void __launch_bounds__(64 * kWaves)
-select_kernel(const EvictArgs a) {
-    __shared__ uint32_t s_hist[kWaves][256];
-    __shared__ uint32_t s_prefix, s_left;
-    __shared__ int s_gt[kWaves], s_eq[kWaves];
+// The bits found so far and how many of the keys that begin with them stay, of how many there are.
+struct Found {
+    uint32_t bits, left, all;
+};
+
+// Of the bins' counts (thread i: bins 2047 - 2i and 2046 - 2i in c) the one with the left-th key from the largest, by a workgroup.
+__device__ __forceinline__ Found pick_bin(uint32_t c0, uint32_t c1, Found f, int pass) {
+    __shared__ uint32_t s_sum[kWaves];
+    __shared__ Found s_found;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int h = blockIdx.x % a.kv_heads, b = blockIdx.x / a.kv_heads;
-    const int len = tokens_of(a, b), n = min(len, a.budget);
-    int32_t* const keep = a.keep + (size_t)blockIdx.x * a.budget;
-    if (h == 0 && tid == 0) a.new_len[b] = n;
-    for (int j = n + tid; j < a.budget; j += 64 * kWaves) keep[j] = -1;
-    if (n == len) {
-        for (int j = tid; j < n; j += 64 * kWaves) keep[j] = j;
-        return;
+    uint32_t upto = c0 + c1;                                // keys in this thread's bins and larger ones of the wave
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t v = __shfl_up(upto, d);
+        if (lane >= d) upto += v;
     }
-    const int32_t* table = a.page_table + (size_t)b * a.table_width;
-    const int page_mask = (1 << a.page_shift) - 1;
-    auto key = [&](int t) -> uint32_t {
-        const int page = table[t >> a.page_shift];
-        if ((uint32_t)page >= (uint32_t)a.num_pages) return 0u;
-        return order_of(a.score[(((int64_t)page * a.kv_heads + h) << a.page_shift) + (t & page_mask)]);
+    if (lane == 63) s_sum[wave] = upto;
+    __syncthreads();
+    uint32_t before = upto - c0 - c1;
+    for (int w = 0; w < wave; ++w) before += s_sum[w];
+    const uint32_t top = kBins - 1 - 2 * tid;
+    if (before < f.left && before + c0 >= f.left) s_found = Found{f.bits | top << shift_of(pass), f.left - before, c0};
+    before += c0;
+    if (before < f.left && before + c1 >= f.left) s_found = Found{f.bits | (top - 1) << shift_of(pass), f.left - before, c1};
+    __syncthreads();
+    return s_found;
+}
+
+// A (sequence, key head)'s tokens and their keys, four neighbours at a time (a page holds a multiple of them): the order of the scores,
+// with the largest key of all for the first and the last tokens, which stay in any case.
+struct Tokens {
+    const int32_t* table;
+    const float* score;
+    int len, first, hi;                                     // tokens [first, hi) are chosen from
+    int h, num_pages, kv_heads, page_shift;
+    // Behind the last token come the smallest keys: there are more tokens than stay, so that none of them is reached.
+    __device__ __forceinline__ u32x4 keys(int t) const {
+        typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
+        u32x4 u = {0u, 0u, 0u, 0u};
+        if (t >= len) return u;
+        const int page = table[t >> page_shift];
+        const bool there = (uint32_t)page < (uint32_t)num_pages;
+        const f32x4 v = *reinterpret_cast<const f32x4*>(score + (((int64_t)(there ? page : 0) * kv_heads + h) << page_shift) + (t & ((1 << page_shift) - 1)));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] = there ? order_of(v[e]) : 0u;
+        if (t < first || t + 4 > hi)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[e] = t + e >= len ? 0u : t + e < first || t + e >= hi ? 0xFFFFFFFFu : u[e];
+        return u;
+    }
+};
+__device__ __forceinline__ Tokens tokens_of_pair(const EvictArgs& a, int pair) {
+    const int h = pair % a.kv_heads, b = pair / a.kv_heads, len = tokens_of(a, b);
+    return Tokens{a.page_table + (size_t)b * a.table_width, a.score, len, a.first, len - a.last, h, a.num_pages, a.kv_heads, a.page_shift};
+}
+
+// The length, the end of the list, and all of it for a sequence that stays whole, by one workgroup of a pair.  Returns whether that is all.
+__device__ __forceinline__ bool list_whole(const EvictArgs& a, const Tokens& x, int pair) {
+    int32_t* const keep = a.keep + (size_t)pair * a.budget;
+    const int n = min(x.len, a.budget);
+    if (x.h == 0 && threadIdx.x == 0) a.new_len[pair / a.kv_heads] = n;
+    for (int j = n + threadIdx.x; j < a.budget; j += kThreads) keep[j] = -1;
+    if (n < x.len) return false;
+    for (int j = threadIdx.x; j < n; j += kThreads) keep[j] = j;
+    return true;
+}
+
+__device__ __forceinline__ void count_bins(const u32x4& u, uint32_t found, int pass, uint32_t* hist) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (begins(u[e], found, pass)) atomicAdd(&hist[bin_of(u[e], pass) * kCopies + (threadIdx.x & (kCopies - 1))], 1u);
+}
+__device__ __forceinline__ void clear_bins(uint32_t* hist) {
+    for (int i = threadIdx.x; i < kBins * kCopies / 4; i += kThreads) reinterpret_cast<u32x4*>(hist)[i] = u32x4{0u, 0u, 0u, 0u};
+}
+__device__ __forceinline__ uint32_t bin_count(const uint32_t* hist, int bin) {
+    const u32x4* p = reinterpret_cast<const u32x4*>(hist + bin * kCopies);
+    const u32x4 v = p[0] + p[1];
+    return v[0] + v[1] + v[2] + v[3];
+}
+
+// A wave's keys above the border, and on it (in all lanes).
+__device__ __forceinline__ void count_keys(const u32x4& u, uint32_t border, int* gt, int* eq) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) *gt += __builtin_popcountll(__ballot(u[e] > border)), *eq += __builtin_popcountll(__ballot(u[e] == border));
+}
+// 256 keys of a wave in order (lane l has tokens t .. t + 3): lists those above the border and, of those on it, the ones with fewer than
+// `left` before them.
+__device__ __forceinline__ void list_keys(const u32x4& u, int t, uint32_t border, int left, int* at, int* equal, int32_t* keep) {
+    const uint64_t below = (1ull << (threadIdx.x & 63)) - 1;
+    uint64_t m_eq[4], m[4];
+    int before = *equal, all = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m_eq[e] = __ballot(u[e] == border), before += __builtin_popcountll(m_eq[e] & below), all += __builtin_popcountll(m_eq[e]);
+    bool stays[4];
+    int place = *at, sum = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        stays[e] = u[e] > border || (u[e] == border && before < left);
+        before += u[e] == border;
+        m[e] = __ballot(stays[e]);
+        place += __builtin_popcountll(m[e] & below), sum += __builtin_popcountll(m[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (stays[e]) keep[place++] = t + e;
+    *at += sum, *equal += all;
+}
+
+// A workgroup to a (sequence, key head).  KEYS > 0: up to KEYS keys a thread, read once and held in registers; 0: read in every pass.
+// A wave has a run of neighbouring tokens.  Copies of the histogram keep lanes with equal bits apart (most scores share their exponent).
+template <int KEYS>
+__global__ void __launch_bounds__(kThreads)
+select_kernel(const EvictArgs a) {
+    __shared__ uint32_t s_hist[kBins * kCopies];
+    __shared__ int s_gt[kWaves], s_eq[kWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pair = blockIdx.x;
+    const Tokens x = tokens_of_pair(a, pair);
+    const int run = KEYS ? KEYS / 4 : (x.len + 4 * kThreads - 1) / (4 * kThreads), t0 = wave * run * 256 + 4 * lane;      // of 256 tokens
+    u32x4 held[KEYS ? KEYS / 4 : 1];
+    if constexpr (KEYS > 0)
+#pragma unroll
+        for (int k = 0; k < KEYS / 4; ++k) held[k] = x.keys(t0 + 256 * k);
+    if (list_whole(a, x, pair)) return;
+    auto each = [&](auto f) {                               // f(keys, token)
+        if constexpr (KEYS > 0) {
+#pragma unroll
+            for (int k = 0; k < KEYS / 4; ++k) f(held[k], t0 + 256 * k);
+        } else {
+            for (int k = 0; k < run; ++k) f(x.keys(t0 + 256 * k), t0 + 256 * k);
+        }
     };
-    const int lo = a.first, hi = len - a.last;              // the tokens between them are chosen from: more than are kept
-    uint32_t prefix = 0, left = a.budget - a.first - a.last;     // of the keys that begin with prefix, `left` stay
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        for (int i = tid; i < kWaves * 256; i += 64 * kWaves) (&s_hist[0][0])[i] = 0u;
-        __syncthreads();
-        for (int t = lo + tid; t < hi; t += 64 * kWaves) {
-            const uint32_t u = key(t);
-            if (shift == 24 || (u >> (shift + 8)) == prefix) atomicAdd(&s_hist[wave][(u >> shift) & 255u], 1u);
-        }
-        __syncthreads();
-        if (wave == 0) {
-            uint32_t c[4] = {}, sum = 0;                    // lane's bins, from the largest: 255 - 4 lane ..
+    Found f = {0u, (uint32_t)a.budget, 0u};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                for (int w = 0; w < kWaves; ++w) c[i] += s_hist[w][255 - 4 * lane - i];
-                sum += c[i];
-            }
-            uint32_t before = sum;                          // keys in larger bins than this lane's
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t v = __shfl_up(before, d);
-                if (lane >= d) before += v;
-            }
-            before -= sum;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (before < left && before + c[i] >= left) s_prefix = prefix << 8 | (uint32_t)(255 - 4 * lane - i), s_left = left - before;
-                before += c[i];
-            }
-            if (left == 0 && lane == 0) s_prefix = 0xFFFFFFFFu >> shift, s_left = 0;    // nothing is above it
-        }
+    for (int pass = 0; pass < 3; ++pass) {
+        if (f.left == f.all) break;                         // (all of them stay: the border is right below their bits)
+        clear_bins(s_hist);
         __syncthreads();
-        prefix = s_prefix, left = s_left;
+        each([&](const u32x4& u, int) { count_bins(u, f.bits, pass, s_hist); });
+        __syncthreads();
+        f = pick_bin(bin_count(s_hist, kBins - 1 - 2 * tid), bin_count(s_hist, kBins - 2 - 2 * tid), f, pass);
     }
-    const uint32_t border = prefix;                         // `left` of the keys that are equal to it stay, the first ones
-    int at = 0, equal = 0;                                  // kept and equal ones so far
-    for (int t0 = 0; t0 < len; t0 += 64 * kWaves) {
-        const int t = t0 + tid;
-        bool sure = t < len && (t < lo || t >= hi), eq = false;
-        if (t < len && !sure) {
-            const uint32_t u = key(t);
-            sure = u > border, eq = u == border;
+    if (f.left == f.all) f = Found{f.bits - 1, 0u, 0u};      // (not 0: below the largest `budget` keys there are others)
+    const int left = (int)f.left;
+    int gt = 0, eq = 0;
+    each([&](const u32x4& u, int) { count_keys(u, f.bits, &gt, &eq); });
+    if (lane == 0) s_gt[wave] = gt, s_eq[wave] = eq;
+    __syncthreads();
+    int at = 0, equal = 0;
+    for (int w = 0; w < wave; ++w) at += s_gt[w] + max(0, min(s_eq[w], left - equal)), equal += s_eq[w];
+    int32_t* const keep = a.keep + (size_t)pair * a.budget;
+    each([&](const u32x4& u, int t) { list_keys(u, t, f.bits, left, &at, &equal, keep); });
+}
+
+// Long sequences of few pairs: a workgroup to a chunk of tokens, with a launch for every pass.  The histograms of all passes and the
+// chunks' counts are in the workspace; every workgroup picks the passes' bins again.
+constexpr int kChunkKeys = 8, kChunk = kThreads * kChunkKeys, kTeamWords = 3 * kBins;
+
+__device__ __forceinline__ Found found_before(const EvictArgs& a, int pair, int passes) {
+    Found f = {0u, (uint32_t)a.budget, 0u};
+    uint2 c[3];
+#pragma unroll
+    for (int p = 0; p < 3; ++p)                             // (bins 2046 - 2i and 2047 - 2i)
+        if (p < passes) c[p] = *reinterpret_cast<const uint2*>(a.team + (size_t)pair * kTeamWords + p * kBins + kBins - 2 - 2 * threadIdx.x);
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+        if (p < passes) f = pick_bin(c[p].y, c[p].x, f, p);
+    return f;
+}
+
+__global__ void __launch_bounds__(256)
+team_clear(const EvictArgs a) {
+    const size_t n = (size_t)a.batch * a.kv_heads * kTeamWords / 4;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256)
+        reinterpret_cast<u32x4*>(a.team)[i] = u32x4{0u, 0u, 0u, 0u};
+}
+
+__global__ void __launch_bounds__(kThreads)
+team_histogram(const EvictArgs a, int pass) {
+    __shared__ uint32_t s_hist[kBins * kCopies];
+    const int tid = threadIdx.x, pair = blockIdx.x / a.team_chunks, chunk = blockIdx.x % a.team_chunks;
+    const Tokens x = tokens_of_pair(a, pair);
+    if (pass == 0 && chunk == 0) list_whole(a, x, pair);
+    const int t0 = chunk * kChunk + (tid >> 6) * kChunkKeys * 64 + 4 * (tid & 63);
+    if (x.len <= a.budget || chunk * kChunk >= x.len) return;
+    u32x4 u[kChunkKeys / 4];
+#pragma unroll
+    for (int k = 0; k < kChunkKeys / 4; ++k) u[k] = x.keys(t0 + 256 * k);
+    clear_bins(s_hist);
+    const Found f = found_before(a, pair, pass);
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kChunkKeys / 4; ++k) count_bins(u[k], f.bits, pass, s_hist);
+    __syncthreads();
+    uint32_t* const hist = a.team + (size_t)pair * kTeamWords + pass * kBins;
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+        if (const uint32_t c = bin_count(s_hist, tid + e * kThreads)) atomicAdd(&hist[tid + e * kThreads], c);
+}
+
+// LIST false: counts each chunk's keys above the border and on it; true: lists what stays.
+template <bool LIST>
+__global__ void __launch_bounds__(kThreads)
+team_list(const EvictArgs a) {
+    __shared__ int s_gt[kWaves], s_eq[kWaves], s_before[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pair = blockIdx.x / a.team_chunks, chunk = blockIdx.x % a.team_chunks;
+    const Tokens x = tokens_of_pair(a, pair);
+    if (x.len <= a.budget || chunk * kChunk >= x.len) return;
+    const int t0 = chunk * kChunk + wave * kChunkKeys * 64 + 4 * lane;
+    u32x4 u[kChunkKeys / 4];
+#pragma unroll
+    for (int k = 0; k < kChunkKeys / 4; ++k) u[k] = x.keys(t0 + 256 * k);
+    int2* const counts = a.team_counts + (size_t)pair * a.team_chunks;
+    int g = 0, e = 0;
+    if (LIST && wave == 0)
+        for (int c = lane; c < chunk; c += 64) g += counts[c].x, e += counts[c].y;
+    const Found f = found_before(a, pair, 3);
+    const int left = (int)f.left;
+    int gt = 0, eq = 0;
+#pragma unroll
+    for (int k = 0; k < kChunkKeys / 4; ++k) count_keys(u[k], f.bits, &gt, &eq);
+    if (lane == 0) s_gt[wave] = gt, s_eq[wave] = eq;
+    if (LIST && wave == 0) {                                // of the chunks before this one
+#pragma unroll
+        for (int d = 32; d; d >>= 1) g += __shfl_xor(g, d), e += __shfl_xor(e, d);
+        if (lane == 0) s_before[0] = g, s_before[1] = e;
+    }
+    __syncthreads();
+    if constexpr (!LIST) {
+        if (tid == 0) {
+            int2 c = {0, 0};
+            for (int w = 0; w < kWaves; ++w) c.x += s_gt[w], c.y += s_eq[w];
+            counts[chunk] = c;
         }
-        const uint64_t m_sure = __ballot(sure), m_eq = __ballot(eq);
-        __syncthreads();
-        if (lane == 0) s_gt[wave] = __builtin_popcountll(m_sure), s_eq[wave] = __builtin_popcountll(m_eq);
-        __syncthreads();
-        int mine = 0, mine_eq = 0;
-        for (int w = 0; w < kWaves; ++w) {
-            const int taken = max(0, min(s_eq[w], (int)left - equal));
-            if (w == wave) mine = at, mine_eq = equal;
-            at += s_gt[w] + taken, equal += s_eq[w];
-        }
-        const uint64_t below = (1ull << lane) - 1;
-        const bool stays_eq = eq && mine_eq + __builtin_popcountll(m_eq & below) < (int)left;
-        const uint64_t m = m_sure | __ballot(stays_eq);
-        if (sure || stays_eq) keep[mine + __builtin_popcountll(m & below)] = t;
+    } else {
+        int equal = s_before[1], at = s_before[0] + min(equal, left);
+        for (int w = 0; w < wave; ++w) at += s_gt[w] + max(0, min(s_eq[w], left - equal)), equal += s_eq[w];
+        int32_t* const keep = a.keep + (size_t)pair * a.budget;
+#pragma unroll
+        for (int k = 0; k < kChunkKeys / 4; ++k) list_keys(u[k], t0 + 256 * k, f.bits, left, &at, &equal, keep);
     }
 }
 
@@ -165,13 +333,60 @@ hipError_t launch_move(const EvictArgs& a, hipStream_t stream) {
     return hipGetLastError();
 }
 
+// Whether several workgroups choose for a (sequence, key head): where a workgroup's registers do not hold its keys and there are
+// too few pairs to fill the card.
+constexpr int kHeldKeys = 32;
+bool teams(int64_t pairs, int max_kv, int compute_units) { return max_kv > kHeldKeys * kThreads && pairs < 4 * compute_units; }
+
+int64_t team_bytes(int64_t pairs, int max_kv) {
+    return pairs * (kTeamWords * 4 + (int64_t)((max_kv + kChunk - 1) / kChunk) * 8);
+}
+
+hipError_t launch_select(const EvictArgs& a, bool team, hipStream_t stream) {
+    const unsigned pairs = (unsigned)a.batch * a.kv_heads;
+    if (team) {
+        team_clear<<<(unsigned)((size_t)pairs * kTeamWords / 4 / 256), 256, 0, stream>>>(a);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        for (int pass = 0; pass < 3; ++pass) {
+            team_histogram<<<pairs * a.team_chunks, kThreads, 0, stream>>>(a, pass);
+            if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        }
+        team_list<false><<<pairs * a.team_chunks, kThreads, 0, stream>>>(a);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        team_list<true><<<pairs * a.team_chunks, kThreads, 0, stream>>>(a);
+    } else if (a.max_kv <= 4 * kThreads) {
+        select_kernel<4><<<pairs, kThreads, 0, stream>>>(a);
+    } else if (a.max_kv <= 16 * kThreads) {
+        select_kernel<16><<<pairs, kThreads, 0, stream>>>(a);
+    } else if (a.max_kv <= kHeldKeys * kThreads) {
+        select_kernel<kHeldKeys><<<pairs, kThreads, 0, stream>>>(a);
+    } else {
+        select_kernel<0><<<pairs, kThreads, 0, stream>>>(a);
+    }
+    return hipGetLastError();
+}
+
 }  // namespace
 
-size_t paged_evict_workspace_bytes(const batq_paged_cache& c, int batch, int max_kv, int budget, int compute_units) { return 0; }
+size_t paged_evict_part_bytes(const batq_paged_cache& c, int batch, int max_kv, int compute_units) {
+    const int64_t pairs = (int64_t)batch * c.kv_heads;
+    return teams(pairs, max_kv, compute_units) ? (size_t)team_bytes(pairs, max_kv) : 0;
+}
+
+// At least the former for every smaller call: of up to as many pairs as teams are used for.
+size_t paged_evict_workspace_bytes(const batq_paged_cache& c, int batch, int max_kv, int compute_units) {
+    int64_t pairs = (int64_t)batch * c.kv_heads;
+    if (pairs >= 4 * compute_units) pairs = 4 * compute_units - 1;
+    return teams(pairs, max_kv, compute_units) ? (size_t)team_bytes(pairs, max_kv) : 0;
+}
 
 hipError_t launch_kv_paged_evict(const batq_paged_cache& c, int bits, float* score, const int32_t* kv_len, const int32_t* page_table,
                                  int table_width, const int32_t* out_table, int out_width, int batch, int max_kv, int budget,
                                  int first, int last, int32_t* keep, int32_t* new_len, void* workspace, hipStream_t stream) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    const int cus = e == hipSuccess ? device_compute_units(dev, &e) : 0;
+    if (e != hipSuccess) return e;
     EvictArgs a = {};
     a.kv_len = kv_len, a.page_table = page_table, a.out_table = out_table, a.batch = batch, a.table_width = table_width;
     a.out_width = out_width, a.max_kv = max_kv, a.num_pages = c.num_pages, a.page_shift = __builtin_ctz((unsigned)c.page_size);
@@ -179,8 +394,10 @@ hipError_t launch_kv_paged_evict(const batq_paged_cache& c, int bits, float* sco
     a.chunks = ((budget < max_kv ? budget : max_kv) + kMove - 1) / kMove;
     a.score = score, a.keep = keep, a.new_len = new_len;
     a.k_codes = c.k_codes, a.k_scales = c.k_scales, a.v_codes = c.v_codes, a.v_scales = c.v_scales;
-    select_kernel<<<(unsigned)batch * c.kv_heads, 64 * kWaves, 0, stream>>>(a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess || a.chunks == 0) return e;
+    const int64_t pairs = (int64_t)batch * c.kv_heads;
+    a.team_chunks = (max_kv + kChunk - 1) / kChunk;
+    a.team = static_cast<uint32_t*>(workspace), a.team_counts = reinterpret_cast<int2*>(a.team + pairs * kTeamWords);
+    if (e = launch_select(a, teams(pairs, max_kv, cus), stream); e != hipSuccess || a.chunks == 0) return e;
     if (bits == 8) return c.head_dim == 64 ? launch_move<64, 8>(a, stream) : launch_move<128, 8>(a, stream);
     return c.head_dim == 64 ? launch_move<64, 4>(a, stream) : launch_move<128, 4>(a, stream);
 }

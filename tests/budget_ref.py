@@ -114,12 +114,12 @@ def evict(arrays, score_, lens, table, out_table, budget, first, last):
             rank[(t < first) | (t >= L - last)] = L + 1
             kept = np.sort(np.argsort(-rank, kind="stable")[:n])
             keep[b, h, :n] = kept
-            for j, src in enumerate(kept):
-                dst = out_table[b][j // page]
-                if not known[src] or not 0 <= dst < pages:
-                    continue
-                for i in (0, 2):
-                    got[i][dst, h, j % page] = arrays[i][ids[src], h, src % page]
-                    got[i + 1][dst, h, :, j % page] = arrays[i + 1][ids[src], h, :, src % page]
-                sc[dst, h, j % page] = score_[ids[src], h, src % page]
+            j = np.arange(n)
+            dst = out_table[b][j // page] if n else j
+            moved = known[kept] & (dst >= 0) & (dst < pages)
+            j, src, dst = j[moved], kept[moved], dst[moved]
+            for i in (0, 2):
+                got[i][dst, h, j % page] = arrays[i][ids[src], h, src % page]
+                got[i + 1][dst, h, :, j % page] = arrays[i + 1][ids[src], h, :, src % page]
+            sc[dst, h, j % page] = score_[ids[src], h, src % page]
     return got, sc, keep, new_len

@@ -239,12 +239,44 @@ def test_evict(B, lens, hkv, D, page, budget, first, last, kind, bits):
     assert_evicted(got, br.evict(arrays, score, lens, table, out_table, budget, first, last))
 
 
-def test_evict_of_a_long_sequence(B):
-    rng = np.random.default_rng(3)
-    arrays, lens, table, out_table = evict_case(rng, [70000, 33], 2, 64, 256, 20000, 4)
-    score = scores_for(rng, "sums", (arrays[0].shape[0], 2, 256))
-    got = run_evict(B, make_cache(B, arrays, 4), score, lens, table, out_table, 20000, 3, 500)
-    assert_evicted(got, br.evict(arrays, score, lens, table, out_table, 20000, 3, 500))
+@pytest.mark.parametrize("lens,hkv,budget,first,last,kind", [
+    ([20000, 33], 2, 5000, 3, 500, "ties"),                 # a workgroup's registers
+    ([70000, 33, 40000], 2, 20000, 3, 500, "sums"),         # several workgroups to a (sequence, key head)
+    ([70000, 100, 0], 1, 100, 0, 0, "same"), ([66000], 3, 8000, 4000, 4000, "close"), ([65537, 70000], 1, 33000, 1, 0, "odd"),
+    ([36000, 500], 600, 60, 1, 5, "ties")])                 # many pairs of long sequences
+def test_evict_of_long_sequences(B, lens, hkv, budget, first, last, kind):
+    rng = np.random.default_rng(3 + budget)
+    arrays, lens, table, out_table = evict_case(rng, lens, hkv, 64, 256, budget, 4)
+    score = scores_for(rng, kind, (arrays[0].shape[0], hkv, 256))
+    got = run_evict(B, make_cache(B, arrays, 4), score, lens, table, out_table, budget, first, last)
+    assert_evicted(got, br.evict(arrays, score, lens, table, out_table, budget, first, last))
+
+
+def test_a_workspace_serves_every_smaller_call(B):
+    """Sizes grow with every bound, and a call runs with what its bounds ask for, full of anything."""
+    import torch
+    rng = np.random.default_rng(14)
+    for D, hq, hkv in ((128, 32, 8), (64, 16, 2), (128, 128, 1), (64, 3, 3)):
+        cache = B.PagedCache(2, 16, hkv, D, bits=4)
+        for _ in range(400):
+            big = [int(np.exp(rng.uniform(0, np.log(n)))) for n in (200, 8192, 8192, 200000)]
+            small = [int(rng.integers(1, n + 1)) if rng.random() < 0.7 else n for n in big]
+            assert B.batq_kv_paged_score_workspace(cache, hq, *small) <= B.batq_kv_paged_score_workspace(cache, hq, *big), (small, big)
+            e = [B.batq_kv_paged_evict_workspace(cache, x[0], x[3], x[1]) for x in (small, big)]
+            assert e[0] <= e[1], (small, big)
+    hq, hkv, D, page = 8, 2, 64, 16
+    lens, qs = [3000, 2500, 300, 900], [1500, 40, 300, 1]
+    arrays, qbits, q, cu, lens, table, T = br.batch_case(rng, lens, qs, hq, hkv, D, page, 4)
+    kv, qd = br.values(*arrays[:2], 4), to_dev(qbits, "bf16")
+    lse = lse_of(arrays, 4, q, cu, lens, table, page, True, 0, T)
+    cache, had = make_cache(B, arrays, 4), np.ones((arrays[0].shape[0], hkv, page), np.float32)
+    ws = torch.full((B.batq_kv_paged_score_workspace(cache, hq, 4, T, 1500, 3000),), 0xFF, dtype=torch.uint8, device="cuda")
+    assert ws.numel()
+    for rows in ([0, 1, 2, 3], [0], [1], [2, 3], [0, 3]):
+        sel = np.concatenate([np.arange(cu[b], cu[b + 1]) for b in rows])
+        c = np.concatenate([[0], np.cumsum([cu[b + 1] - cu[b] for b in rows])]).astype(np.int32)
+        got = run_score(B, cache, qd[torch.from_numpy(sel).cuda()].contiguous(), lse[sel], had, c, lens[rows], table[rows], workspace=ws)
+        br.assert_score(got, br.score(kv, q[sel], lse[sel], had, c, lens[rows], table[rows], page, D ** -0.5, True, 0, False), had)
 
 
 def test_evict_does_not_trust_its_lists(B):
