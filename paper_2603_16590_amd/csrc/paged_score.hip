@@ -42,7 +42,7 @@ __device__ __forceinline__ float ref_of(float lse) { return lse == -INFINITY ? I
 template <int D, int NT, int BITS>
 __global__ void __launch_bounds__(256)
 score_few(const ScoreArgs a) {
-    constexpr int kC = D / 4, kU = D / 32, kToken = D * BITS / 8, kKw = kC * BITS / 32;
+    constexpr int kC = D / 4, kU = D / 32, kToken = D * BITS / 8, kKw = kC * BITS / 32, kStages = 2;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, g = lane >> 4;
     // the first parts of all sequences, then the second ones ..: short sequences have few, and workgroups go to the dies in turn
@@ -57,29 +57,30 @@ score_few(const ScoreArgs a) {
     const int page_mask = (1 << a.page_shift) - 1, last_page = (s.len - 1) >> a.page_shift;
     // lane i holds the page of tokens t_begin + 16 i .. + 15 (a part is at most 1024 long)
     const int pages = table[min((t_begin + 16 * lane) >> a.page_shift, last_page)];
-    uint32_t kw[2][kKw];
-    uint32_t ks = 0;
-    f32x2 old = {0.0f, 0.0f};
-    float* to = nullptr;
-    bool there = false;
-    auto request = [&](int t) {
+    // blocks t, t + 128, .. are requested kStages ahead
+    uint32_t kw[kStages][2][kKw];
+    uint32_t ks[kStages];
+    f32x2 old[kStages];
+    float* to[kStages];
+    bool there[kStages];
+    auto request = [&](int t, int st) {
         t += 2 * n;
         int page = __shfl(pages, (t - t_begin) >> 4);
-        there = (uint32_t)page < (uint32_t)a.num_pages;
-        page = there ? page : 0;
+        there[st] = (uint32_t)page < (uint32_t)a.num_pages;
+        page = there[st] ? page : 0;
         const int off = t & page_mask;
         const int64_t ph = (int64_t)page * a.kv_heads + h;
         const uint8_t* p = a.k_codes + ((ph << a.page_shift) + off) * kToken + g * (kToken / 4);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) load_words<kKw>(kw[i], p + i * kToken);
-        ks = *reinterpret_cast<const uint16_t*>(a.k_scales + ((ph * (D / 32) + g * kC / 32) << a.page_shift) + off);
-        to = a.score + (ph << a.page_shift) + off;
-        if (a.add) {
-            old[0] = to[0], old[1] = to[1];                 // (a page holds an even number of tokens)
-        }
+        for (int i = 0; i < 2; ++i) load_words<kKw>(kw[st][i], p + i * kToken);
+        ks[st] = *reinterpret_cast<const uint16_t*>(a.k_scales + ((ph * (D / 32) + g * kC / 32) << a.page_shift) + off);
+        to[st] = a.score + (ph << a.page_shift) + off;
+        if (a.add) old[st][0] = to[st][0], old[st][1] = to[st][1];      // (a page holds an even number of tokens)
     };
     int t = t_begin + wave * 32;
-    if (t < t_end) request(t);
+#pragma unroll
+    for (int st = 0; st < kStages; ++st)
+        if (t + 128 * st < t_end) request(t + 128 * st, st);
 
     bf16x8 qf[NT][kU];
     float ref[NT][4];
@@ -103,14 +104,17 @@ score_few(const ScoreArgs a) {
     const bool full = rows == NT * 16;
     const int all_hi = !full ? 0 : a.causal ? min(s.len, s.first_pos + 1) : s.len;
     const int all_lo = first_seen(a, s.first_pos + s.n - 1);
-    for (; t < t_end; t += 128) {
+    while (t < t_end)
+#pragma unroll
+    for (int st = 0; st < kStages; ++st) {
+        if (st > 0 && t >= t_end) break;
         f32x4 sc[NT][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const float kscale = scale_operand((ks >> (8 * i)) & 0xFFu);
+            const float kscale = scale_operand((ks[st] >> (8 * i)) & 0xFFu);
             bf16x8 kf[kU];
 #pragma unroll
-            for (int u = 0; u < kU; ++u) kf[u] = cvt_eight<BITS>(kw[i] + u * BITS / 4, kscale);
+            for (int u = 0; u < kU; ++u) kf[u] = cvt_eight<BITS>(kw[st][i] + u * BITS / 4, kscale);
 #pragma unroll
             for (int x = 0; x < NT; ++x) {
                 sc[x][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -118,10 +122,10 @@ score_few(const ScoreArgs a) {
                 for (int u = 0; u < kU; ++u) sc[x][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[x][u], kf[u], sc[x][i], 0, 0, 0);
             }
         }
-        float* const at = to;
-        const f32x2 had = old;
-        const bool stored = there;
-        if (t + 128 < t_end) request(t + 128);
+        float* const at = to[st];
+        const f32x2 had = old[st];
+        const bool stored = there[st];
+        if (t + 128 * kStages < t_end) request(t + 128 * kStages, st);
         const bool whole = t >= all_lo && t + 32 <= all_hi;
         float sum[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -147,6 +151,7 @@ score_few(const ScoreArgs a) {
             if (tok < t_end) at[0] = v[0];
             if (tok + 1 < t_end) at[1] = v[1];
         }
+        t += 128;
     }
 }
 
@@ -447,11 +452,12 @@ struct ScorePlan {
 // and 383 us, of 16384 1211, 1106, 1072; prompt of 512 in parts of 1024, 512, 256 rows 44, 26, 18 us, of 2048 55, 46, 50).
 constexpr int kUnits = 16, kLeastRows = 512;
 
-ScorePlan score_plan(int group, int kv_heads, int batch, int max_q, int max_kv, int compute_units) {
+ScorePlan score_plan(int group, int kv_heads, int batch, int total_q, int max_q, int max_kv, int compute_units) {
     ScorePlan p = {};
     const int64_t rows = (int64_t)max_q * group, pairs = (int64_t)batch * kv_heads;
     p.many = rows > 32;
-    p.few = !p.many || batch > 1;
+    // (where one sequence of few rows would leave more queries than the others may have, there is none)
+    p.few = !p.many || (int64_t)total_q <= (int64_t)(batch - 1) * max_q + 32 / group;
     p.few_rows = !p.few ? -1 : rows > 16 ? 32 : 16;
     int64_t len = (pairs * max_kv / (4 * compute_units) + 255) & ~int64_t(255);
     len = len < 256 ? 256 : len > 1024 ? 1024 : len;
@@ -493,7 +499,7 @@ hipError_t launch_score(const ScoreArgs& a, const ScorePlan& p, hipStream_t stre
 }  // namespace
 
 size_t paged_score_part_bytes(const batq_paged_cache& c, int q_heads, int batch, int total_q, int max_q, int max_kv, int compute_units) {
-    const ScorePlan p = score_plan(q_heads / c.kv_heads, c.kv_heads, batch, max_q, max_kv, compute_units);
+    const ScorePlan p = score_plan(q_heads / c.kv_heads, c.kv_heads, batch, total_q, max_q, max_kv, compute_units);
     return p.parts > 1 ? (size_t)batch * c.kv_heads * p.key_tiles * p.parts * kTileTokens * 4 : 0;
 }
 
@@ -511,7 +517,7 @@ hipError_t launch_kv_paged_score(const batq_paged_cache& c, int bits, const batq
     hipError_t e = hipGetDevice(&dev);
     const int cus = e == hipSuccess ? device_compute_units(dev, &e) : 0;
     if (e != hipSuccess) return e;
-    const ScorePlan p = score_plan(q_heads / c.kv_heads, c.kv_heads, b.batch, b.max_q, b.max_kv, cus);
+    const ScorePlan p = score_plan(q_heads / c.kv_heads, c.kv_heads, b.batch, b.total_q, b.max_q, b.max_kv, cus);
     ScoreArgs a = {};
     set_lists(a, c, b, q_heads, causal, window);
     a.q = static_cast<const uint16_t*>(q), a.ldq = ldq, a.lse = lse, a.score = score, a.add = add;
