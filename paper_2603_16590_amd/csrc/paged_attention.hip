@@ -332,39 +332,41 @@ attend_few(const AttnArgs a) {
     }
 }
 
-// Joins the parts of a row: W waves take the parts in turn, eight in flight each, and are added in wave order; `at` is the
-// row's first part.  Every wave of the workgroup takes part.
+// Joins the parts of a row: W waves take the parts in turn, or for W = 0 half a wave takes them all, eight in flight each, and
+// they are added in wave order; `at` is the row's first part.  Every wave of the workgroup takes part (W = 0: `parts` is 0 where there is
+// nothing to join).
 template <int D, int W>
 __device__ __forceinline__ void join_row(const AttnArgs& a, const float* part_o, const float* part_ml, size_t at, int parts,
                                          size_t row, int head) {
-    __shared__ float s_v[W][D], s_sum[W];
-    const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int kLanes = W == 0 ? 32 : 64, kC = D / kLanes, kStep = W == 0 ? 1 : W;
+    __shared__ float s_v[W ? W : 1][D], s_sum[W ? W : 1];
+    const int lane = threadIdx.x & (kLanes - 1), wave = W <= 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     float top = -INFINITY;
-    for (int p = lane; p < parts; p += 64) top = __builtin_fmaxf(top, part_ml[2 * (at + p)]);
+    for (int p = lane; p < parts; p += kLanes) top = __builtin_fmaxf(top, part_ml[2 * (at + p)]);
 #pragma unroll
-    for (int d = 32; d; d >>= 1) top = __builtin_fmaxf(top, shuffle_xor(top, d));
+    for (int d = kLanes / 2; d; d >>= 1) top = __builtin_fmaxf(top, shuffle_xor(top, d));
     const float ref = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, v[D / 64] = {};
-    for (int p0 = wave; p0 < parts; p0 += 8 * W) {          // parts p0, p0 + W, .. p0 + 7 W; past the end: the last one, weight 0
-        float x[8][D / 64], m[8], l[8];
+    float sum = 0.0f, v[kC] = {};
+    for (int p0 = wave; p0 < parts; p0 += 8 * kStep) {      // parts p0, p0 + W, .. p0 + 7 W; past the end: the last one, weight 0
+        float x[8][kC], m[8], l[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const size_t p = at + min(p0 + W * j, parts - 1);
+            const size_t p = at + min(p0 + kStep * j, parts - 1);
             m[j] = part_ml[2 * p], l[j] = part_ml[2 * p + 1];
 #pragma unroll
-            for (int c = 0; c < D / 64; ++c) x[j][c] = part_o[p * D + lane * (D / 64) + c];
+            for (int c = 0; c < kC; ++c) x[j][c] = part_o[p * D + lane * kC + c];
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float f = p0 + W * j < parts ? exp2_(m[j] - ref) : 0.0f;
+            const float f = p0 + kStep * j < parts ? exp2_(m[j] - ref) : 0.0f;
             sum = __builtin_fmaf(f, l[j], sum);
 #pragma unroll
-            for (int c = 0; c < D / 64; ++c) v[c] = __builtin_fmaf(f, x[j][c], v[c]);
+            for (int c = 0; c < kC; ++c) v[c] = __builtin_fmaf(f, x[j][c], v[c]);
         }
     }
     if constexpr (W > 1) {
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) s_v[wave][lane * (D / 64) + c] = v[c];
+        for (int c = 0; c < kC; ++c) s_v[wave][lane * kC + c] = v[c];
         if (lane == 0) s_sum[wave] = sum;
         __syncthreads();
         if (wave > 0) return;
@@ -372,13 +374,14 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const float* part_o,
         for (int w = 1; w < W; ++w) {
             sum += s_sum[w];
 #pragma unroll
-            for (int c = 0; c < D / 64; ++c) v[c] += s_v[w][lane * (D / 64) + c];
+            for (int c = 0; c < kC; ++c) v[c] += s_v[w][lane * kC + c];
         }
     }
+    if (W == 0 && parts == 0) return;
     const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-    __bf16* o = reinterpret_cast<__bf16*>(a.out + row * a.ldo + (size_t)head * D + lane * (D / 64));
+    __bf16* o = reinterpret_cast<__bf16*>(a.out + row * a.ldo + (size_t)head * D + lane * kC);
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c) o[c] = (__bf16)(v[c] * inv);
+    for (int c = 0; c < kC; ++c) o[c] = (__bf16)(v[c] * inv);
     if (a.lse && lane == 0) a.lse[row * a.q_heads + head] = sum != 0.0f ? (top + __log2f(sum)) * 0.69314718055994531f : -INFINITY;
 }
 
@@ -742,38 +745,48 @@ __device__ __forceinline__ void join_few(const AttnArgs& a, unsigned unit) {
     join_row<D, 4>(a, a.part_o, a.part_ml, (size_t)unit * a.max_parts, parts, (size_t)s.begin + r / a.group, h * a.group + r % a.group);
 }
 
-// A (row of q, query head) of a sequence with many rows: by a wave, there are many of them, of few parts.
+// Two (row of q, query head) pairs of sequences with many rows, by a wave's halves: there are many of them, of few parts.  The wave
+// looks for the first one's sequence; the second one's is mostly the same, else it is looked for too.
 template <int D>
-__device__ __forceinline__ void join_many(const AttnArgs& a, int unit) {
+__device__ __forceinline__ void join_many(const AttnArgs& a, unsigned pair) {
     const int lane = threadIdx.x & 63;
-    const int row = unit / a.q_heads, head = unit - row * a.q_heads;
-    if (row >= a.total_q) return;
-    int b = -1;                                             // the row's sequence: lanes look at 64 of them at a time
-    for (int b0 = 0; b0 < a.batch && b < 0; b0 += 64) {
-        bool mine = false;
-        if (b0 + lane < a.batch) {
-            const int begin = a.cu_q[b0 + lane], end = a.cu_q[b0 + lane + 1];
-            mine = begin >= 0 && end <= a.total_q && row >= begin && row < end;
+    const int64_t units = (int64_t)a.total_q * a.q_heads, unit = 2 * (int64_t)pair + (lane >> 5);
+    const int row = (int)(unit / a.q_heads), head = (int)(unit - (int64_t)row * a.q_heads);
+    int b = -1;                                             // the half's sequence
+    for (int half = 0; half < 2; ++half) {
+        const int r = __builtin_amdgcn_readfirstlane(__shfl(row, 32 * half));
+        if (half == 1 && r == __builtin_amdgcn_readfirstlane(row)) break;
+        int found = -1;
+        for (int b0 = 0; b0 < a.batch && found < 0; b0 += 64) {      // lanes look at 64 sequences at a time
+            bool mine = false;
+            if (b0 + lane < a.batch) {
+                const int begin = a.cu_q[b0 + lane], end = a.cu_q[b0 + lane + 1];
+                mine = begin >= 0 && end <= a.total_q && r >= begin && r < end;
+            }
+            const uint64_t m = __ballot(mine);
+            if (m) found = b0 + __builtin_ctzll(m);
         }
-        const uint64_t found = __ballot(mine);
-        if (found) b = b0 + __builtin_ctzll(found);
+        if (half == 0 || lane >= 32) b = found;
     }
-    if (b < 0) return;
-    const Seq s = sequence(a, b);
-    const int rows = s.n * a.group, i = row - s.begin;
-    if (i >= s.n || rows <= a.few_rows) return;
-    const TokenRange t = tile_tokens(a, s, (i * a.group + head % a.group) / kManyRows);
-    const int parts = range_parts(t, a.many_len);
-    if (parts == 1) return;
-    join_row<D, 1>(a, a.many_o, a.many_ml, ((size_t)row * a.q_heads + head) * a.many_parts, parts, (size_t)row, head);
+    int parts = 0;
+    if (b >= 0 && unit < units) {
+        const Seq s = sequence(a, b);
+        const int rows = s.n * a.group, i = row - s.begin;
+        if (i < s.n && rows > a.few_rows) {
+            parts = range_parts(tile_tokens(a, s, (i * a.group + head % a.group) / kManyRows), a.many_len);
+            if (parts == 1) parts = 0;                      // (it has been written)
+        }
+    }
+    if (__ballot(parts != 0) == 0) return;
+    join_row<D, 0>(a, a.many_o, a.many_ml, (size_t)unit * a.many_parts, parts, (size_t)row, head);
 }
 
-// Joins what both kernels have cut: the first `few` workgroups take a row each, the others four.
+// Joins what both kernels have cut: the first `few` workgroups take a row each, the others eight.
 template <int D>
 __global__ void __launch_bounds__(256)
 join_parts(const AttnArgs a, unsigned few) {
     if (blockIdx.x < few) join_few<D>(a, blockIdx.x);
-    else join_many<D>(a, (int)((blockIdx.x - few) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)));
+    else join_many<D>(a, (blockIdx.x - few) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
 }
 
 }  // namespace
@@ -879,7 +892,7 @@ hipError_t launch_attention(const AttnArgs& a, const Plan& p, int dev, hipStream
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     const unsigned few = p.max_parts > 1 ? (unsigned)a.batch * a.kv_heads * p.part_rows : 0;
-    const unsigned many = p.many_parts > 1 ? ((unsigned)a.total_q * a.q_heads + 3) / 4 : 0;
+    const unsigned many = p.many_parts > 1 ? ((unsigned)a.total_q * a.q_heads + 7) / 8 : 0;
     if (few + many == 0) return hipSuccess;
     join_parts<D><<<few + many, 256, 0, stream>>>(a, few);
     return hipGetLastError();
