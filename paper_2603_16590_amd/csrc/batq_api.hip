@@ -1041,9 +1041,9 @@ static batq_status check_evict_dims(const batq_paged_cache* c, int batch, int ma
     if (!c) return BATQ_ERR_NULL;
     if (batq_status st = check_paged_dims(c->num_pages, c->page_size, c->kv_heads, c->head_dim); st != BATQ_OK) return st;
     if (batch < 0 || batch > (1 << 20) || max_kv < 0 || max_kv > (1 << 30) || budget < 1) return BATQ_ERR_SHAPE;
-    // a launch has fewer than 2^32 threads: workgroups of 1024 for a (sequence, key head) pair, of 256 for 64 of its kept tokens
+    // a launch has fewer than 2^32 threads: workgroups of 1024 for 8192 tokens of a (sequence, key head) pair, of 256 for 64 kept ones
     const int64_t pairs = (int64_t)batch * c->kv_heads, kept = budget < max_kv ? budget : max_kv;
-    if (pairs >= 1 << 22 || pairs * (kept / 64 + 1) >= 1 << 24) return BATQ_ERR_SHAPE;
+    if (pairs * (max_kv / 8192 + 1) >= 1 << 22 || pairs * (kept / 64 + 1) >= 1 << 24) return BATQ_ERR_SHAPE;
     return BATQ_OK;
 }
 
@@ -1068,7 +1068,8 @@ batq_status batq_kv_paged_evict(const batq_paged_cache* cache, int cache_bits, f
     if (!score || !kv_len || !keep || !new_len || (table_width > 0 && !page_table) || (out_width > 0 && !out_table)) return BATQ_ERR_NULL;
     if (((reinterpret_cast<uintptr_t>(score) | reinterpret_cast<uintptr_t>(kv_len) | reinterpret_cast<uintptr_t>(page_table) |
           reinterpret_cast<uintptr_t>(out_table) | reinterpret_cast<uintptr_t>(keep) | reinterpret_cast<uintptr_t>(new_len)) & 3u) != 0 ||
-        (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || new_len == kv_len || (page_table && page_table == out_table))
+        (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || (new_len < kv_len + batch && kv_len < new_len + batch) ||
+        (page_table && page_table == out_table))
         return BATQ_ERR_SHAPE;
     if (batq_status st = check_device(); st != BATQ_OK) return st;
     const int cus = current_compute_units();

@@ -220,8 +220,7 @@ attend_few(const AttnArgs a) {
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) mx = __builtin_fmaxf(mx, sc[x][i][r]);
-            mx = __builtin_fmaxf(mx, shuffle_xor(mx, 16));
-            mx = __builtin_fmaxf(mx, shuffle_xor(mx, 32)) * a.scale;
+            mx = larger(across32(larger(across16(mx)))) * a.scale;
             if (__ballot(mx > m[x] + 8.0f)) {
                 const float m2 = __builtin_fmaxf(m[x], mx);
                 const float f = m2 == -INFINITY ? 0.0f : exp2_(m[x] - m2);

@@ -46,6 +46,21 @@ __device__ __forceinline__ Seq sequence(const PagedLists& a, int b) {
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// x of the lane and of the lane 16 (32) away, in one order for both, without LDS's latency.
+struct Two {
+    float a, b;
+};
+__device__ __forceinline__ Two across16(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return Two{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ Two across32(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return Two{__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ float larger(const Two& t) { return __builtin_fmaxf(t.a, t.b); }
+__device__ __forceinline__ float total(const Two& t) { return t.a + t.b; }
+
 // Two values of a word of four E4M3 codes as bf16.
 __device__ __forceinline__ uint32_t cvt_lo(uint32_t w, float sc) {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, sc, false));

@@ -142,8 +142,7 @@ score_few(const ScoreArgs a) {
                     }
                     sum[i] += w;
                 }
-            sum[i] += __shfl_xor(sum[i], 16);
-            sum[i] += __shfl_xor(sum[i], 32);
+            sum[i] = total(across32(total(across16(sum[i]))));
         }
         if (g == 0 && stored) {
             const int tok = t + 2 * n;

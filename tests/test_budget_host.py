@@ -76,7 +76,7 @@ def test_evict_refusals(B):
                      (dict(out_width=1), 2), (dict(budget=40), 2), (dict(score=None), 1), (dict(kv_len=None), 1), (dict(table=None), 1),
                      (dict(out=None), 1), (dict(keep=None), 1), (dict(new_len=None), 1), (dict(score=P + 2), 2), (dict(kv_len=P + 1), 2),
                      (dict(table=P + 2), 2), (dict(out=P + 2), 2), (dict(keep=P + 2), 2), (dict(new_len=P + 2), 2), (dict(new_len=P), 2),
-                     (dict(out=P), 2), (dict(ws=P + 128), 2), (dict(batch=1 << 21), 2), (dict(batch=1 << 20, max_kv=1 << 20, budget=1 << 20), 2)):
+                     (dict(out=P), 2), (dict(new_len=P + 4), 2), (dict(new_len=P - 4), 2), (dict(ws=P + 128), 2), (dict(batch=1 << 20, max_kv=8192 * 2), 2), (dict(batch=1 << 20, max_kv=1 << 20, budget=1 << 20), 2)):
         assert evict(B, ok, **kw) == want, kw
     assert evict(B, ok, batch=0, score=None, kv_len=None, table=None, out=None, keep=None, new_len=None) == 0
     assert B.lib.batq_kv_paged_evict_workspace(None, 1, 100, 10) == 0

@@ -145,6 +145,61 @@ def test_score_does_not_trust_its_lists(B):
             assert np.all(np.abs(got[at] - want[0][at]) <= want[1][at])
 
 
+def test_scores_of_a_large_ragged_batch(B):
+    """More sequences than a wave has lanes: chunks and single tokens in any order, empty ones among them, sequences without queries; parts
+    of rows in some."""
+    rng = np.random.default_rng(15)
+    hq, hkv, D, page, n = 8, 2, 64, 16, 150
+    lens = rng.integers(0, 90, n)
+    qs = np.where(rng.random(n) < 0.2, rng.integers(0, 60, n), 1)
+    qs[[0, 70, 149]], lens[[0, 70, 149]] = [0, 420, 95], [400, 700, 95]
+    arrays, qbits, q, cu, lens, table, T = br.batch_case(rng, lens, qs, hq, hkv, D, page, 4, spare=1)
+    kv = br.values(*arrays[:2], 4)
+    for window, add in ((0, True), (40, False)):
+        lse = lse_of(arrays, 4, q, cu, lens, table, page, True, window, T)
+        had = rng.uniform(0, 3, (arrays[0].shape[0], hkv, page)).astype(np.float32)
+        got = run_score(B, make_cache(B, arrays, 4), to_dev(qbits, "bf16"), lse, had, cu, lens, table, window=window, add=add)
+        br.assert_score(got, br.score(kv, q, lse, had, cu, lens, table, page, D ** -0.5, True, window, add), had)
+
+
+@pytest.mark.parametrize("qs,max_q", [([300, 2], None), ([40, 3, 500], 45)])
+def test_few_rows_beside_many(B, qs, max_q):
+    """Sequences of few rows beside one of many, also where the bound on queries hides some of them."""
+    rng = np.random.default_rng(16)
+    hq, hkv, D, page = 4, 1, 128, 32
+    lens = [700, 900, 600][: len(qs)]
+    arrays, qbits, q, cu, lens, table, T = br.batch_case(rng, lens, qs, hq, hkv, D, page, 8)
+    lse = lse_of(arrays, 8, q, cu, lens, table, page, True, 0, T)
+    had = np.ones((arrays[0].shape[0], hkv, page), np.float32)
+    got = run_score(B, make_cache(B, arrays, 8), to_dev(qbits, "bf16"), lse, had, cu, lens, table, max_q=max_q, add=True)
+    br.assert_score(got, br.score(br.values(*arrays[:2], 8), q, lse, had, cu, lens, table, page, D ** -0.5, True, 0, True, max_q=max_q), had)
+
+
+def test_score_arrays_at_any_word(B):
+    """Scores that begin at a multiple of 4 bytes, no more: scoring and eviction."""
+    import torch
+    rng = np.random.default_rng(17)
+    hq, hkv, D, page, budget = 4, 2, 64, 16, 70
+    arrays, lens, table, out_table = evict_case(rng, [200, 90, 333], hkv, D, page, budget, 4)
+    cu, T = np.array([0, 1, 2, 40], np.int32), 40
+    qd = to_dev(ref.bf16_values(rng, T, hq * D)[0], "bf16")
+    lse = dev(rng.uniform(3, 6, (T, hq)).astype(np.float32))
+    had = scores_for(rng, "sums", (arrays[0].shape[0], hkv, page))
+    results = []
+    for shift in (0, 1, 2, 3):
+        cache = make_cache(B, arrays, 4)
+        store = torch.full((had.size + 8,), 9.0, device="cuda")
+        score = store[shift: shift + had.size].view(had.shape)
+        score.copy_(dev(had))
+        B.batq_kv_paged_score(cache, qd, lse, score, dev(cu), dev(lens), dev(table), 38, 333, add=True)
+        keep, new_len = B.batq_kv_paged_evict(cache, score, dev(lens), dev(table), dev(out_table), 333, budget, 2, 5)
+        torch.cuda.synchronize()
+        assert bool((store[:shift] == 9.0).all()) and bool((store[shift + had.size:] == 9.0).all())
+        results.append([score.clone(), keep, new_len] + [t.clone() for t in (cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales)])
+    for r in results[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(r, results[0]))
+
+
 def test_score_of_keys_and_rows_that_are_not_finite(B):
     """A NaN key makes the lse of the rows that see it NaN, and with it the scores of all tokens that they see; other tokens' stay."""
     rng = np.random.default_rng(7)
@@ -242,14 +297,32 @@ def test_evict(B, lens, hkv, D, page, budget, first, last, kind, bits):
 @pytest.mark.parametrize("lens,hkv,budget,first,last,kind", [
     ([20000, 33], 2, 5000, 3, 500, "ties"),                 # a workgroup's registers
     ([70000, 33, 40000], 2, 20000, 3, 500, "sums"),         # several workgroups to a (sequence, key head)
-    ([70000, 100, 0], 1, 100, 0, 0, "same"), ([66000], 3, 8000, 4000, 4000, "close"), ([65537, 70000], 1, 33000, 1, 0, "odd"),
-    ([36000, 500], 600, 60, 1, 5, "ties")])                 # many pairs of long sequences
+    ([70000, 100, 0], 1, 100, 0, 0, "same"), ([66000], 3, 8000, 4000, 4000, "close"), ([65537, 70000], 1, 33000, 1, 0, "odd")])
 def test_evict_of_long_sequences(B, lens, hkv, budget, first, last, kind):
     rng = np.random.default_rng(3 + budget)
     arrays, lens, table, out_table = evict_case(rng, lens, hkv, 64, 256, budget, 4)
     score = scores_for(rng, kind, (arrays[0].shape[0], hkv, 256))
     got = run_evict(B, make_cache(B, arrays, 4), score, lens, table, out_table, budget, first, last)
     assert_evicted(got, br.evict(arrays, score, lens, table, out_table, budget, first, last))
+
+
+def test_evict_of_many_long_sequences(B):
+    """So many (sequence, key head) pairs of long sequences that a workgroup each fills the card: 260 that share their pages."""
+    import torch
+    rng = np.random.default_rng(18)
+    hkv, D, page, L, budget, n = 4, 64, 256, 33000, 40, 260
+    arrays, lens, table, out_table = evict_case(rng, [L] + [budget] * (n - 1), hkv, D, page, budget, 4)
+    score = scores_for(rng, "ties", (arrays[0].shape[0], hkv, page))
+    want = br.evict(arrays, score, lens[:1], table[:1], out_table[:1], budget, 1, 5)
+    cache, ds = make_cache(B, arrays, 4), dev(score)
+    keep, new_len = B.batq_kv_paged_evict(cache, ds, dev(np.full(n, L, np.int32)), dev(np.repeat(table[:1], n, 0)), dev(out_table), L, budget, 1, 5)
+    torch.cuda.synchronize()
+    assert bool((new_len == budget).all()) and np.array_equal(keep.cpu().numpy(), np.repeat(want[2], n, 0))
+    first, rest = out_table[0, 0], torch.from_numpy(out_table[1:, 0].astype(np.int64)).cuda()
+    for got, w in zip(host(cache), want[0]):
+        assert np.array_equal(got[first], w[first])
+    for t in (cache.k_codes, cache.v_codes, ds):
+        assert bool((t[rest][:, :, :budget] == t[int(first)][None, :, :budget]).all())
 
 
 def test_a_workspace_serves_every_smaller_call(B):
@@ -292,6 +365,10 @@ def test_evict_does_not_trust_its_lists(B):
     eff = np.array([table.shape[1] * page, 64, 0, 48])
     got = run_evict(B, make_cache(B, arrays, 4), score, told, table, out_table, budget, 2, 5, max_kv=10 ** 6)
     assert_evicted(got, br.evict(arrays, score, eff, table, out_table, budget, 2, 5))
+    for max_kv in (0, 10 ** 6):                             # no token at all
+        empty = np.zeros(4, np.int32)
+        got = run_evict(B, make_cache(B, arrays, 4), score, empty, table, out_table, budget, 2, 5, max_kv=max_kv)
+        assert_evicted(got, br.evict(arrays, score, empty, table, out_table, budget, 2, 5))
     got = run_evict(B, make_cache(B, arrays, 4), score, lens, table, out_table, budget, 2, 5, max_kv=50)
     assert_evicted(got, br.evict(arrays, score, np.minimum(lens, 50), table, out_table, budget, 2, 5))
 
