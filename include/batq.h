@@ -77,7 +77,7 @@ typedef enum {
     BATQ_ERR_SHAPE = 2,       /* K % 32 != 0, a size <= 0, or a leading dimension too small  */
     BATQ_ERR_DTYPE = 3,       /* unknown batq_dtype                                          */
     BATQ_ERR_UNSUPPORTED = 4, /* (g_outer, g_inner) not one of (4,8), (8,4), or unknown form;
-                                 a paged cache's head_dim not 64 or 128                      */
+                                 a paged cache's head_dim not 64 or 128, its width not 4 or 8 */
     BATQ_ERR_SINGULAR = 5,    /* G or some P_k is not invertible                             */
     BATQ_ERR_CLIP_RANGE = 6,  /* a clip ratio is not in (0, 1]                               */
     BATQ_ERR_WORKSPACE = 7,   /* workspace smaller than batq_linear_workspace()              */
@@ -389,7 +389,7 @@ batq_status batq_kv_dequantize(const uint8_t* codes, const uint8_t* scales, int6
                                int M, int K, int bits, void* out, batq_dtype odtype, int64_t ldo, void* stream);
 
 /* ------------------------------------------------------------------------------------
- * Paged 8-bit key/value cache (Sec. 3.2, "Self-Attention Module", for many sequences at once).
+ * Paged key/value cache, here in 8 bits (in 4: below) (Sec. 3.2, "Self-Attention Module", for many sequences at once).
  * Keys and values of all sequences live in pages of page_size tokens; a sequence owns any pages, in any order, and a
  * table lists them.  The arrays (DEVICE, caller-owned, 16-byte aligned) hold per page:
  *   codes   [kv_heads][page_size][head_dim] E4M3 bytes, batq_kv_paged_code_bytes() in all

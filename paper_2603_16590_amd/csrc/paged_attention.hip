@@ -74,6 +74,10 @@ __device__ __forceinline__ float shuffle_xor(float x, int d) { return __shfl_xor
 // The weights go in as two bf16 terms (2^-16): the products are not the bound here.  Measured: 4 sequences of about 131072 tokens, 28 query
 // and 4 key heads of 128: 73 us (367 MB, 5.0 TB/s, a large copy's rate); 64 sequences of up to 8192, 32 and 8 heads: 36 us.
 // Blocks of 64 tokens at two waves per SIMD: 40 us instead of 36; four waves per SIMD spill: 50 us.
+// Codes of 4 bits are half the bytes for the same vector instructions, and those with the waves' waits are the bound: 64 x 8192 tokens of 32 and 8
+// heads of 128 channels 145 us (570 MB, 3.9 TB/s; 8 bits 202 us, 5.5 TB/s), 4 of about 131072 under 28 and 4 heads 46 us.  Not better: keys and
+// values requested two blocks ahead, which leaves two waves per SIMD (163 us), each sum's two products apart (148), parts of 512 to 896
+// tokens (151 to 141 beside 140), four waves per SIMD (spills, 285), first parts of all sequences first (ragged ones 37 us instead of 33).
 template <int D, int NT, int BITS>
 __global__ void __launch_bounds__(256, NT == 1 ? 3 : 2)
 attend_few(const AttnArgs a) {
@@ -388,7 +392,7 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, const float* part_o,
 // exponentials, which add up where the two waves of a SIMD run in step.  A causal prompt of 8192 tokens with 32 query and 8 key
 // heads of 128: 598 us = 920 TFLOP/s.  Not better: two groups of waves a phase apart with a barrier for each (744), half of
 // the waves a tile behind (980, spills), 128 rows to a workgroup (835), raw codes through LDS (964), two or four operands
-// less or more read ahead (676 to 703 beside 676, profiled).
+// less or more read ahead (676 to 703 beside 676, profiled).  Codes of 4 bits take as long: 4096 queries behind 12288 tokens 955 us, 975 in 8 bits.
 // A workgroup of eight waves takes 256 rows (row = query token * group + head of the group) of one (sequence, key head), 32
 // to a wave, and walks the visible tokens in tiles of 64.  The codes of the next tile are requested while this one is
 // worked on, converted once for all eight waves and written to LDS as bf16:

@@ -146,7 +146,8 @@ __device__ __forceinline__ void list_keys(const u32x4& u, int t, uint32_t border
     *at += sum, *equal += all;
 }
 
-// A workgroup to a (sequence, key head).  KEYS > 0: up to KEYS keys a thread, read once and held in registers; 0: read in every pass.
+// A workgroup to a (sequence, key head): latencies and the vector instructions of one compute unit (32 pairs of 32768 tokens 24 us, 512 of 2112
+// 16 us; read in every pass, key by key, 99 us).  KEYS > 0: up to KEYS keys a thread, read once and held in registers; 0: read in every pass.
 // A wave has a run of neighbouring tokens.  Copies of the histogram keep lanes with equal bits apart (most scores share their exponent).
 template <int KEYS>
 __global__ void __launch_bounds__(kThreads)
@@ -192,7 +193,8 @@ select_kernel(const EvictArgs a) {
 }
 
 // Long sequences of few pairs: a workgroup to a chunk of tokens, with a launch for every pass.  The histograms of all passes and the
-// chunks' counts are in the workspace; every workgroup picks the passes' bins again.
+// chunks' counts are in the workspace; every workgroup picks the passes' bins again.  8 pairs of 131072 tokens: 30 us of six launches (one
+// workgroup each: 360); 32 pairs of 32768 are as fast with one workgroup each.
 constexpr int kChunkKeys = 8, kChunk = kThreads * kChunkKeys, kTeamWords = 3 * kBins;
 
 __device__ __forceinline__ Found found_before(const EvictArgs& a, int pair, int passes) {
@@ -282,7 +284,8 @@ team_list(const EvictArgs a) {
 
 constexpr int kMove = 64;                                   // tokens of a workgroup of the move
 
-// Moves the listed tokens: keys, values, scales and score.
+// Moves the listed tokens: keys, values, scales and score.  Bound by the copy: 64 x 8 x 2048 tokens of 128 channels in 8 bits 116 us (562 MB in and
+// out, 4.9 TB/s, a large copy's rate).
 template <int D, int BITS>
 __global__ void __launch_bounds__(256)
 move_kernel(const EvictArgs a) {

@@ -35,7 +35,10 @@ struct ScoreArgs : PagedLists {
 // The subtrahend of a row's exponents; a row that has seen nothing has no weights.
 __device__ __forceinline__ float ref_of(float lse) { return lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f; }
 
-// Few rows to a key head (decoding): bound by the stream of key codes, read once.  A workgroup takes a part of one (sequence, key
+// Few rows to a key head (decoding): bound by the stream of key codes, read once (64 x 8192 tokens of 8 heads of 128 channels in 4 bits:
+// 302 MB in 60 us, 5.0 TB/s), and for ragged sequences by a part's chain of loads (64 of up to 8192 tokens: 35 MB in 21 us; parts of 256, 512
+// tokens 26, 22 us there, but 86, 69 us for 64 x 8192; tokens shared out evenly over all workgroups 23 and 90: more registers, fewer waves;
+// requested one, two, three blocks ahead 24, 21.7, 22.9).  A workgroup takes a part of one (sequence, key
 // head), its four waves blocks of 32 tokens in turn.  S = Q K^T with the queries' operands in registers: lane (n, g) =
 // (l % 16, l / 16) loads channels [g D/4, (g + 1) D/4) of tokens 2n and 2n + 1 (the order in which a product runs over channels is
 // free), and element r of its results of tile x is row 16x + 4g + r: a token's sum is one over elements and four lanes.
@@ -154,7 +157,10 @@ score_few(const ScoreArgs a) {
     }
 }
 
-// Many rows (prompts, their last queries): bound by the matrix pipe and the vector instructions around the exponentials.  A
+// Many rows (prompts, their last queries): bound by the vector instructions around the exponentials (32 exponentials at half rate, 64 others: 512
+// clocks of a SIMD for 32 rows x 64 tokens, as many as the products take), with the products beside them: a prompt of 8192 tokens of 32 and 8 heads
+// of 128 channels 340 us (800 TFLOP/s; 1000 without causal), the last 64 queries of four of 32768 tokens, 28 and 4 heads, 53 us.  Weights formed
+// behind their own products instead of between the next ones: 400 and 57 us; three waves per SIMD instead of two spill (429).  A
 // workgroup has 256 tokens, 64 to a wave, whose keys stay in registers as operands, and walks its part of the rows that may see
 // them 64 at a time; they go through LDS, two buffers, requested a stage ahead.  S^T = K Q^T, so that a lane adds the weights
 // of its rows up token by token; the lanes' sums are added at the end.  Lane (n, h) = (l % 32, l / 32) holds channels
