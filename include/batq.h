@@ -504,7 +504,7 @@ batq_status batq_paged_attention_ex(const batq_paged_cache* cache, int cache_bit
  *           places are always set, so that pages need not be cleared.  Places that hold no token are left as they are.
  *   lse     DEVICE fp32 [total_q][q_heads]; a row with -infinity (it saw nothing) adds nothing
  * A batch whose queries are fewer than those of the attention (a prompt's last ones) has their rows alone in q and lse.  max_q and max_kv
- * bound what is served as there; q is read alone.  Sums are fp32, in an order that depends on the arguments alone.  A NaN score comes from
+ * bound what is served as there.  Sums are fp32, in an order that depends on the arguments alone.  A NaN score comes from
  * a NaN lse, or from a key that is NaN.  The tokens of a page that several sequences of a call share get the sum of one of them.
  *   workspace   DEVICE, 256-byte aligned, its contents need not be cleared, one for calls that may run at the same time each;
  *               batq_kv_paged_score_workspace() bytes are enough for every call of at most that batch, total_q, max_q and max_kv

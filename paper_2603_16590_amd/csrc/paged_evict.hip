@@ -42,9 +42,20 @@ struct Found {
     uint32_t bits, left, all;
 };
 
+// Sum of the waves' numbers before this one's.
+__device__ __forceinline__ int waves_before(const int* x, int wave) {
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves / 4; ++i) {
+        const int4 v = reinterpret_cast<const int4*>(x)[i];
+        sum += (4 * i < wave ? v.x : 0) + (4 * i + 1 < wave ? v.y : 0) + (4 * i + 2 < wave ? v.z : 0) + (4 * i + 3 < wave ? v.w : 0);
+    }
+    return sum;
+}
+
 // Of the bins' counts (thread i: bins 2047 - 2i and 2046 - 2i in c) the one with the left-th key from the largest, by a workgroup.
 __device__ __forceinline__ Found pick_bin(uint32_t c0, uint32_t c1, Found f, int pass) {
-    __shared__ uint32_t s_sum[kWaves];
+    __shared__ __align__(16) int s_sum[kWaves];
     __shared__ Found s_found;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     uint32_t upto = c0 + c1;                                // keys in this thread's bins and larger ones of the wave
@@ -53,10 +64,9 @@ __device__ __forceinline__ Found pick_bin(uint32_t c0, uint32_t c1, Found f, int
         const uint32_t v = __shfl_up(upto, d);
         if (lane >= d) upto += v;
     }
-    if (lane == 63) s_sum[wave] = upto;
+    if (lane == 63) s_sum[wave] = (int)upto;
     __syncthreads();
-    uint32_t before = upto - c0 - c1;
-    for (int w = 0; w < wave; ++w) before += s_sum[w];
+    uint32_t before = upto - c0 - c1 + (uint32_t)waves_before(s_sum, wave);
     const uint32_t top = kBins - 1 - 2 * tid;
     if (before < f.left && before + c0 >= f.left) s_found = Found{f.bits | top << shift_of(pass), f.left - before, c0};
     before += c0;
@@ -118,42 +128,63 @@ __device__ __forceinline__ uint32_t bin_count(const uint32_t* hist, int bin) {
     return v[0] + v[1] + v[2] + v[3];
 }
 
-// A wave's keys above the border, and on it (in all lanes).
+// A lane's keys above the border, and on it.
 __device__ __forceinline__ void count_keys(const u32x4& u, uint32_t border, int* gt, int* eq) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) *gt += __builtin_popcountll(__ballot(u[e] > border)), *eq += __builtin_popcountll(__ballot(u[e] == border));
+    for (int e = 0; e < 4; ++e) *gt += u[e] > border, *eq += u[e] == border;
+}
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+    return x;
+}
+// The sum of a number of 0 to 4 over the lanes before this one; over all of them in *all.
+__device__ __forceinline__ int sum_before(int c, int* all) {
+    int before = 0;
+    *all = 0;
+#pragma unroll
+    for (int bit = 0; bit < 3; ++bit) {
+        const uint64_t m = __ballot((c >> bit) & 1);
+        before += (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u)) << bit;
+        *all += __builtin_popcountll(m) << bit;
+    }
+    return before;
 }
 // 256 keys of a wave in order (lane l has tokens t .. t + 3): lists those above the border and, of those on it, the ones with fewer than
 // `left` before them.
 __device__ __forceinline__ void list_keys(const u32x4& u, int t, uint32_t border, int left, int* at, int* equal, int32_t* keep) {
-    const uint64_t below = (1ull << (threadIdx.x & 63)) - 1;
-    uint64_t m_eq[4], m[4];
-    int before = *equal, all = 0;
+    bool stays[4], on = false;
+    int c = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) m_eq[e] = __ballot(u[e] == border), before += __builtin_popcountll(m_eq[e] & below), all += __builtin_popcountll(m_eq[e]);
-    bool stays[4];
-    int place = *at, sum = 0;
+    for (int e = 0; e < 4; ++e) stays[e] = u[e] > border, on = on || u[e] == border;
+    if (*equal < left && __ballot(on)) {
+        int ties = 0, all;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        stays[e] = u[e] > border || (u[e] == border && before < left);
-        before += u[e] == border;
-        m[e] = __ballot(stays[e]);
-        place += __builtin_popcountll(m[e] & below), sum += __builtin_popcountll(m[e]);
+        for (int e = 0; e < 4; ++e) ties += u[e] == border;
+        int rank = *equal + sum_before(ties, &all);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (u[e] == border) stays[e] = rank++ < left;
+        *equal += all;
     }
 #pragma unroll
+    for (int e = 0; e < 4; ++e) c += stays[e];
+    int all;
+    int32_t* to = keep + *at + sum_before(c, &all);
+    *at += all;
+#pragma unroll
     for (int e = 0; e < 4; ++e)
-        if (stays[e]) keep[place++] = t + e;
-    *at += sum, *equal += all;
+        if (stays[e]) *to++ = t + e;
 }
 
-// A workgroup to a (sequence, key head): latencies and the vector instructions of one compute unit (32 pairs of 32768 tokens 24 us, 512 of 2112
-// 16 us; read in every pass, key by key, 99 us).  KEYS > 0: up to KEYS keys a thread, read once and held in registers; 0: read in every pass.
+// A workgroup to a (sequence, key head): latencies and the vector instructions of one compute unit (32 pairs of 32768 tokens 22 us, 512 of 2112
+// 16.6 us; read in every pass, key by key, 99 us).  KEYS > 0: up to KEYS keys a thread, read once and held in registers; 0: read in every pass.
 // A wave has a run of neighbouring tokens.  Copies of the histogram keep lanes with equal bits apart (most scores share their exponent).
 template <int KEYS>
 __global__ void __launch_bounds__(kThreads)
 select_kernel(const EvictArgs a) {
     __shared__ uint32_t s_hist[kBins * kCopies];
-    __shared__ int s_gt[kWaves], s_eq[kWaves];
+    __shared__ __align__(16) int s_gt[kWaves], s_eq[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pair = blockIdx.x;
     const Tokens x = tokens_of_pair(a, pair);
     const int run = KEYS ? KEYS / 4 : (x.len + 4 * kThreads - 1) / (4 * kThreads), t0 = wave * run * 256 + 4 * lane;      // of 256 tokens
@@ -184,10 +215,10 @@ select_kernel(const EvictArgs a) {
     const int left = (int)f.left;
     int gt = 0, eq = 0;
     each([&](const u32x4& u, int) { count_keys(u, f.bits, &gt, &eq); });
+    gt = wave_sum(gt), eq = wave_sum(eq);
     if (lane == 0) s_gt[wave] = gt, s_eq[wave] = eq;
     __syncthreads();
-    int at = 0, equal = 0;
-    for (int w = 0; w < wave; ++w) at += s_gt[w] + max(0, min(s_eq[w], left - equal)), equal += s_eq[w];
+    int equal = waves_before(s_eq, wave), at = waves_before(s_gt, wave) + min(equal, left);
     int32_t* const keep = a.keep + (size_t)pair * a.budget;
     each([&](const u32x4& u, int t) { list_keys(u, t, f.bits, left, &at, &equal, keep); });
 }
@@ -243,7 +274,7 @@ team_histogram(const EvictArgs a, int pass) {
 template <bool LIST>
 __global__ void __launch_bounds__(kThreads)
 team_list(const EvictArgs a) {
-    __shared__ int s_gt[kWaves], s_eq[kWaves], s_before[2];
+    __shared__ __align__(16) int s_gt[kWaves], s_eq[kWaves], s_before[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, pair = blockIdx.x / a.team_chunks, chunk = blockIdx.x % a.team_chunks;
     const Tokens x = tokens_of_pair(a, pair);
     if (x.len <= a.budget || chunk * kChunk >= x.len) return;
@@ -260,6 +291,7 @@ team_list(const EvictArgs a) {
     int gt = 0, eq = 0;
 #pragma unroll
     for (int k = 0; k < kChunkKeys / 4; ++k) count_keys(u[k], f.bits, &gt, &eq);
+    gt = wave_sum(gt), eq = wave_sum(eq);
     if (lane == 0) s_gt[wave] = gt, s_eq[wave] = eq;
     if (LIST && wave == 0) {                                // of the chunks before this one
 #pragma unroll
@@ -274,8 +306,7 @@ team_list(const EvictArgs a) {
             counts[chunk] = c;
         }
     } else {
-        int equal = s_before[1], at = s_before[0] + min(equal, left);
-        for (int w = 0; w < wave; ++w) at += s_gt[w] + max(0, min(s_eq[w], left - equal)), equal += s_eq[w];
+        int equal = s_before[1] + waves_before(s_eq, wave), at = s_before[0] + waves_before(s_gt, wave) + min(equal, left);
         int32_t* const keep = a.keep + (size_t)pair * a.budget;
 #pragma unroll
         for (int k = 0; k < kChunkKeys / 4; ++k) list_keys(u[k], t0 + 256 * k, f.bits, left, &at, &equal, keep);
