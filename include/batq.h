@@ -527,7 +527,8 @@ batq_status batq_kv_paged_score(const batq_paged_cache* cache, int cache_bits, c
  * Keys stay rotated by the positions that they were appended at, which the next append goes on counting from; a window of
  * later attention calls counts places.  A token's new place differs from head to head.
  *   workspace  as above; batq_kv_paged_evict_workspace() bytes are enough for every call of at most that batch, max_kv and budget
- * BATQ_ERR_SHAPE: also for batch * kv_heads from 2^22 / (max_kv / 8192 + 1) on, or from 2^24 / (min(budget, max_kv) / 64 + 1). */
+ * BATQ_ERR_SHAPE: also for a budget above 2^30, and for batch * kv_heads from 2^22 / (max_kv / 8192 + 1) on, or from
+ * 2^24 / (min(budget, max_kv) / 64 + 1). */
 size_t batq_kv_paged_evict_workspace(const batq_paged_cache* cache, int batch, int max_kv, int budget);
 batq_status batq_kv_paged_evict(const batq_paged_cache* cache, int cache_bits, float* score, const int32_t* kv_len,
                                 const int32_t* page_table, int table_width, const int32_t* out_table, int out_width, int batch,

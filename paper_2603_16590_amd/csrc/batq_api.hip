@@ -1040,7 +1040,7 @@ batq_status batq_kv_paged_score(const batq_paged_cache* cache, int cache_bits, c
 static batq_status check_evict_dims(const batq_paged_cache* c, int batch, int max_kv, int budget) {
     if (!c) return BATQ_ERR_NULL;
     if (batq_status st = check_paged_dims(c->num_pages, c->page_size, c->kv_heads, c->head_dim); st != BATQ_OK) return st;
-    if (batch < 0 || batch > (1 << 20) || max_kv < 0 || max_kv > (1 << 30) || budget < 1) return BATQ_ERR_SHAPE;
+    if (batch < 0 || batch > (1 << 20) || max_kv < 0 || max_kv > (1 << 30) || budget < 1 || budget > (1 << 30)) return BATQ_ERR_SHAPE;
     // a launch has fewer than 2^32 threads: workgroups of 1024 for 8192 tokens of a (sequence, key head) pair, of 256 for 64 kept ones
     const int64_t pairs = (int64_t)batch * c->kv_heads, kept = budget < max_kv ? budget : max_kv;
     if (pairs * (max_kv / 8192 + 1) >= 1 << 22 || pairs * (kept / 64 + 1) >= 1 << 24) return BATQ_ERR_SHAPE;

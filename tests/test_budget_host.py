@@ -96,3 +96,12 @@ def test_statements_of_the_tests():
     flat = s[table[0], 0].reshape(-1)[:40]
     chosen = set(np.argsort(-flat[2:37])[:15] + 2) | {0, 1, 37, 38, 39}
     assert n[0] == 20 and set(keep[0, 0]) == chosen and np.array_equal(sc[out[0], 0].reshape(-1)[:20], flat[keep[0, 0]])
+
+
+def test_budgets_past_two_to_the_thirty_are_refused(B):
+    """A list's places are counted in 32 bits, 1024 at a time: behind 2^31 - 1 - 1024 they would wrap to places before the list."""
+    ok = cache()
+    for budget in ((1 << 30) + 1, 2 ** 31 - 1024, 2 ** 31 - 1):
+        assert evict(B, ok, budget=budget, out_width=3) == 2 and evict(B, ok, budget=budget, out_width=3, batch=0) == 2
+        assert B.lib.batq_kv_paged_evict_workspace(C.byref(ok), 2, 1 << 20, budget) == 0
+    assert evict(B, ok, budget=1 << 30, out_width=3, batch=0) == 0
