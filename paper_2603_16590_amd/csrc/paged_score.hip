@@ -258,18 +258,19 @@ score_many(const ScoreArgs a) {
     const float* const l_first = a.lse + (size_t)s.begin * a.q_heads + h * a.group;
     const uint16_t* q_at[kLoads];
     int q_j[kLoads];
-    auto row_head = [&](int r, int* j) {                    // token and head of a row
-        const int i = r / a.group;
-        *j = r - i * a.group;
-        return i;
+    struct TokenHead {
+        int token, head;
     };
+    auto of_row = [&](int r) { return TokenHead{r / a.group, r % a.group}; };
 #pragma unroll
     for (int k = 0; k < kLoads; ++k) {
-        const int i = row_head(row_lo + tid / kCh + kPer * k, &q_j[k]);
-        q_at[k] = q_first + i * a.ldq + q_j[k] * D;
+        const TokenHead at = of_row(row_lo + tid / kCh + kPer * k);
+        q_j[k] = at.head;
+        q_at[k] = q_first + at.token * a.ldq + at.head * D;
     }
-    int l_j;
-    const float* l_at = l_first + row_head(row_lo + lane, &l_j) * (int64_t)a.q_heads + l_j;
+    const TokenHead l_row = of_row(row_lo + lane);
+    int l_j = l_row.head;
+    const float* l_at = l_first + l_row.token * (int64_t)a.q_heads + l_row.head;
     u32x4 qw[kLoads];
     float lw = 0.0f;
     auto request = [&](int r0) {                            // (rows past the end repeat the first one: they have no weights)

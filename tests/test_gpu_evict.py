@@ -216,6 +216,20 @@ def test_score_of_keys_and_rows_that_are_not_finite(B):
     br.assert_score(np.where(fine, got, 0.0), (np.where(fine, want, 0.0), np.where(fine, tol, 0.0)), np.where(fine, had, 0.0))
 
 
+@pytest.mark.parametrize("hq,hkv,lens,qs", [(3, 1, [700, 300], [400, 300]), (14, 2, [500], [173]), (48, 1, [400], [77]), (65, 1, [300, 90], [50, 21]),
+                                            (100, 1, [600], [64]), (254, 2, [270], [31]), (128, 1, [520], [70])])
+def test_each_row_of_many_takes_its_own_lse(B, hq, hkv, lens, qs):
+    """Groups that do not divide a stage of 64 rows, or are larger than one, with an lse that tells every query and head from all
+    others: weights by another row's would be off by 2 % at least (neighbouring heads by e, neighbouring queries by e^0.02)."""
+    rng = np.random.default_rng(hq + sum(qs))
+    D, page = 64, 16
+    arrays, qbits, q, cu, lens, table, T = br.batch_case(rng, lens, qs, hq, hkv, D, page, 8)
+    lse = (np.arange(T)[:, None] * 0.02 % 3 + np.arange(hq) % 5).astype(np.float32)
+    had = rng.uniform(0, 3, (arrays[0].shape[0], hkv, page)).astype(np.float32)
+    got = run_score(B, make_cache(B, arrays, 8), to_dev(qbits, "bf16"), lse, had, cu, lens, table)
+    br.assert_score(got, br.score(br.values(*arrays[:2], 8), q, lse, had, cu, lens, table, page, D ** -0.5, True, 0, False), had)
+
+
 # ---------------------------------------------------------------------------------------- eviction
 EVICT = [
     # lens, kv heads, D, page, budget, first, last
