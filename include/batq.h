@@ -55,7 +55,8 @@
  *     batq_paged_attention*, batq_kv_paged_*, batq_lora_add) only enqueue kernels: no host synchronisation, no allocation, no state kept between
  *     calls.  Which kernels run is a function of the call's arguments and the device
  *     alone, so a call gives the same bits on any stream, eagerly or while the stream
- *     is captured into a graph.  Scratch memory comes from the caller (`workspace`).
+ *     is captured into a graph.  (Lists that send two tokens of a call to one place, a slot or a page's scores, leave
+ *     unspecified what it holds.)  Scratch memory comes from the caller (`workspace`).
  *   - Argument errors are detected on the host before anything is launched and
  *     leave all outputs untouched.  Non-finite inputs are outside the contract.
  *   - Calls are thread-safe; a handle may be used by several threads at once (online
@@ -505,7 +506,15 @@ batq_status batq_paged_attention_ex(const batq_paged_cache* cache, int cache_bit
  *   lse     DEVICE fp32 [total_q][q_heads]; a row with -infinity (it saw nothing) adds nothing
  * A batch whose queries are fewer than those of the attention (a prompt's last ones) has their rows alone in q and lse.  max_q and max_kv
  * bound what is served as there.  Sums are fp32, in an order that depends on the arguments alone.  A NaN score comes from
- * a NaN lse, or from a key that is NaN.  The tokens of a page that several sequences of a call share get the sum of one of them.
+ * a NaN lse, or from a key that is NaN.
+ * A page of scores belongs to one entry of a call's tables: what a page holds that two entries list is unspecified (two sums meet in
+ * it, and from run to run another one may be the last).  Sequences of a call that share cache pages (a common prefix) take
+ * batq_kv_paged_score_ex, with score pages of their own:
+ *   score        has score_pages pages, num_pages or more (else BATQ_ERR_SHAPE)
+ *   score_table  DEVICE int32 [batch][table_width]: the page of `score` for the tokens of page page_table[b][i]; NULL: the same page.  A
+ *                token without a page in [0, num_pages), or without one of scores in [0, score_pages), takes no part
+ * Which pages of `score` a sequence takes is the caller's choice: those of pages that it owns alone, and others (those from num_pages
+ * on, say) beside pages that it shares.
  *   workspace   DEVICE, 256-byte aligned, its contents need not be cleared, one for calls that may run at the same time each;
  *               batq_kv_paged_score_workspace() bytes are enough for every call of at most that batch, total_q, max_q and max_kv
  * BATQ_ERR_SHAPE: also for batch * kv_heads * (max_kv / 256 + 1) from 2^24 on. */
@@ -513,14 +522,20 @@ size_t batq_kv_paged_score_workspace(const batq_paged_cache* cache, int q_heads,
 batq_status batq_kv_paged_score(const batq_paged_cache* cache, int cache_bits, const batq_paged_batch* b, const void* q,
                                 int64_t ldq, int q_heads, float scale, int causal, int window, const float* lse, float* score,
                                 int add, void* workspace, size_t workspace_bytes, void* stream);
+batq_status batq_kv_paged_score_ex(const batq_paged_cache* cache, int cache_bits, const batq_paged_batch* b, const void* q,
+                                   int64_t ldq, int q_heads, float scale, int causal, int window, const float* lse, float* score,
+                                   const int32_t* score_table, int score_pages, int add, void* workspace, size_t workspace_bytes,
+                                   void* stream);
 
 /* Eviction by score.  Of every sequence and key head n = min(kv_len[b], budget) tokens are kept: the first `first` and the last `last`
  * of them all (first + last <= budget) and those with the largest scores between (of equal ones the earlier; NaN, and tokens of pages
  * that do not exist, count as the smallest).  They move, in their order, to places 0 .. n - 1 of the pages out_table[b][0 ..]:
  * keys, values, scales and scores, byte for byte.  Every sequence moves, the short ones whole; pages of page_table are only read, so
- * they may be shared between sequences (a common prefix), and are the caller's to free afterwards.
+ * they may be shared between sequences (a common prefix), and are the caller's to free afterwards.  batq_kv_paged_evict_ex reads the
+ * scores from score_table's pages, as batq_kv_paged_score_ex has left them (a token without one counts as the smallest and
+ * moves with a score of 0), and writes them to those of out_table: every sequence then owns all of its pages, and their scores.
  *   out_table  DEVICE int32 [batch][out_width], out_width * page_size >= min(budget, max_kv, table_width * page_size); no page of it may be
- *              listed twice or be among those of page_table (what such pages hold then is unspecified)
+ *              listed twice or be among those of page_table or score_table (what such pages hold then is unspecified)
  *   keep       DEVICE int32 [batch][kv_heads][budget], out: the kept tokens' former places, ascending, then -1
  *   new_len    DEVICE int32 [batch], out: n; must not overlap kv_len
  *   kv_len, page_table, max_kv   as for the attention; nothing in the lists is trusted
@@ -534,6 +549,10 @@ batq_status batq_kv_paged_evict(const batq_paged_cache* cache, int cache_bits, f
                                 const int32_t* page_table, int table_width, const int32_t* out_table, int out_width, int batch,
                                 int max_kv, int budget, int first, int last, int32_t* keep, int32_t* new_len, void* workspace,
                                 size_t workspace_bytes, void* stream);
+batq_status batq_kv_paged_evict_ex(const batq_paged_cache* cache, int cache_bits, float* score, const int32_t* score_table, int score_pages,
+                                   const int32_t* kv_len, const int32_t* page_table, int table_width, const int32_t* out_table,
+                                   int out_width, int batch, int max_kv, int budget, int first, int last, int32_t* keep,
+                                   int32_t* new_len, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------------------
  * Low-rank adapters of many requests beside a shared projection:

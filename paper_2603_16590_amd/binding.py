@@ -85,8 +85,10 @@ SYMBOLS = {
     "batq_paged_attention_ex": (_i, [_vp, _i, _vp, _vp, _i64, _i, C.c_float, _i, _i, _vp, _i64, _vp, _vp, _sz, _vp]),
     "batq_kv_paged_score_workspace": (_sz, [_vp, _i, _i, _i, _i, _i]),
     "batq_kv_paged_score": (_i, [_vp, _i, _vp, _vp, _i64, _i, C.c_float, _i, _i, _vp, _vp, _i, _vp, _sz, _vp]),
+    "batq_kv_paged_score_ex": (_i, [_vp, _i, _vp, _vp, _i64, _i, C.c_float, _i, _i, _vp, _vp, _vp, _i, _i, _vp, _sz, _vp]),
     "batq_kv_paged_evict_workspace": (_sz, [_vp, _i, _i, _i]),
     "batq_kv_paged_evict": (_i, [_vp, _i, _vp, _vp, _vp, _i, _vp, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _sz, _vp]),
+    "batq_kv_paged_evict_ex": (_i, [_vp, _i, _vp, _vp, _i, _vp, _vp, _i, _vp, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _sz, _vp]),
     "batq_lora_workspace": (_sz, [_i, _i, _i, _i, _i]),
     "batq_lora_add": (_i, [_vp, _i, _i, _i, _i64, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _i64, _vp, _i64, _i, _vp, _sz, _vp]),
 }
@@ -795,17 +797,25 @@ def batq_kv_paged_score_workspace(cache: PagedCache, q_heads: int, batch: int, t
     return int(lib.batq_kv_paged_score_workspace(C.byref(cache._d), q_heads, batch, total_q, max_q, max_kv))
 
 
-def _score_array(score, cache: PagedCache, dev: int) -> int:
+def _score_array(score, cache: PagedCache, score_table, table, dev: int):
+    """The addresses of the scores and of their pages' table (or None), and the number of pages that they have."""
     import torch
-    return _list(score, torch.float32, (cache.num_pages, cache.kv_heads, cache.page_size), dev, "score")
+    if score_table is None:
+        return _list(score, torch.float32, (cache.num_pages, cache.kv_heads, cache.page_size), dev, "score"), None, cache.num_pages
+    pages = max(score.shape[0] if score.dim() else 0, cache.num_pages)
+    return (_list(score, torch.float32, (pages, cache.kv_heads, cache.page_size), dev, "score"),
+            _list(score_table, torch.int32, table.shape, dev, "score_table"), pages)
 
 
 def batq_kv_paged_score(cache: PagedCache, q, lse, score, cu_q, kv_len, page_table, max_q: int, max_kv: int,
-                        scale: Optional[float] = None, causal: bool = True, window: int = 0, add: bool = False, workspace=None):
+                        scale: Optional[float] = None, causal: bool = True, window: int = 0, add: bool = False, workspace=None,
+                        score_table=None):
     """What each cached token receives of the attention of the batch (q, lists, scale, causal, window as in
     batq_paged_attention; lse: fp32 [total_q, q_heads], as it returned it): the softmax weights summed over the queries and the
     query heads of a key head, into ``score`` (fp32 [pages, kv_heads, page_size]).  add: to what the tokens there have, except the
-    queries' own, which are new.  Returns score."""
+    queries' own, which are new.  Sequences that share pages of the cache (a common prefix) need pages of scores of their own, or
+    what the shared ones hold is unspecified: score_table (int32, as page_table) names the page of ``score`` (then of any number of
+    pages from the cache's on) for each of page_table's.  Returns score."""
     import torch
     if q.dim() != 2 or page_table.dim() != 2:
         raise ValueError("expected q [total_q, q_heads * head_dim] and page_table [batch, width]")
@@ -819,9 +829,10 @@ def batq_kv_paged_score(cache: PagedCache, q, lse, score, cu_q, kv_len, page_tab
         workspace = torch.empty((max(n, 16),), dtype=torch.uint8, device=q.device)
     b = _PagedBatch(_list(cu_q, torch.int32, (batch + 1,), dev, "cu_q"), _list(kv_len, torch.int32, (batch,), dev, "kv_len"),
                     _list(page_table, torch.int32, (batch, table_width), dev, "page_table"), batch, table_width, T, max_q, max_kv)
-    _check(lib.batq_kv_paged_score(cache.desc(dev), cache.bits, C.byref(b), q.data_ptr(), ldq, q_heads, D ** -0.5 if scale is None else scale,
-                                   causal, window, _list(lse, torch.float32, (T, q_heads), dev, "lse"), _score_array(score, cache, dev), add,
-                                   _scratch(workspace, dev), workspace.nbytes, torch._C._cuda_getCurrentRawStream(dev)), "batq_kv_paged_score")
+    p_score, p_table, pages = _score_array(score, cache, score_table, page_table, dev)
+    _check(lib.batq_kv_paged_score_ex(cache.desc(dev), cache.bits, C.byref(b), q.data_ptr(), ldq, q_heads, D ** -0.5 if scale is None else scale,
+                                      causal, window, _list(lse, torch.float32, (T, q_heads), dev, "lse"), p_score, p_table, pages, add,
+                                      _scratch(workspace, dev), workspace.nbytes, torch._C._cuda_getCurrentRawStream(dev)), "batq_kv_paged_score")
     return score
 
 
@@ -831,10 +842,11 @@ def batq_kv_paged_evict_workspace(cache: PagedCache, batch: int, max_kv: int, bu
 
 
 def batq_kv_paged_evict(cache: PagedCache, score, kv_len, page_table, out_table, max_kv: int, budget: int, first: int = 0,
-                        last: int = 0, keep=None, new_len=None, workspace=None):
+                        last: int = 0, keep=None, new_len=None, workspace=None, score_table=None):
     """Keep, of each sequence (kv_len: int32 [batch], page_table: int32 [batch, width]) and key head, the ``first`` tokens, the
     ``last`` ones and those with the largest scores between them, ``budget`` in all, and move them in their order to the pages of
-    out_table (int32 [batch, out width], none of them in use).  Returns (keep, new_len): int32 [batch, kv_heads, budget] former
+    out_table (int32 [batch, out width], none of them in use).  score_table: where the scores are, as in batq_kv_paged_score; they move to
+    out_table's pages of ``score``.  Returns (keep, new_len): int32 [batch, kv_heads, budget] former
     places of the kept tokens, then -1; int32 [batch] lengths."""
     import torch
     if page_table.dim() != 2 or out_table.dim() != 2:
@@ -848,7 +860,8 @@ def batq_kv_paged_evict(cache: PagedCache, score, kv_len, page_table, out_table,
     if workspace is None:
         n = batq_kv_paged_evict_workspace(cache, batch, max_kv, budget)
         workspace = torch.empty((max(n, 16),), dtype=torch.uint8, device=page_table.device)
-    _check(lib.batq_kv_paged_evict(cache.desc(dev), cache.bits, _score_array(score, cache, dev), _list(kv_len, torch.int32, (batch,), dev, "kv_len"),
+    p_score, p_table, pages = _score_array(score, cache, score_table, page_table, dev)
+    _check(lib.batq_kv_paged_evict_ex(cache.desc(dev), cache.bits, p_score, p_table, pages, _list(kv_len, torch.int32, (batch,), dev, "kv_len"),
                                    _list(page_table, torch.int32, (batch, table_width), dev, "page_table"), table_width,
                                    _list(out_table, torch.int32, (batch, out_width), dev, "out_table"), out_width, batch, max_kv, budget,
                                    first, last, _list(keep, torch.int32, (batch, cache.kv_heads, budget), dev, "keep"),

@@ -1013,17 +1013,25 @@ size_t batq_kv_paged_score_workspace(const batq_paged_cache* cache, int q_heads,
 batq_status batq_kv_paged_score(const batq_paged_cache* cache, int cache_bits, const batq_paged_batch* b, const void* q,
                                 int64_t ldq, int q_heads, float scale, int causal, int window, const float* lse, float* score,
                                 int add, void* workspace, size_t workspace_bytes, void* stream) {
+    return batq_kv_paged_score_ex(cache, cache_bits, b, q, ldq, q_heads, scale, causal, window, lse, score, nullptr,
+                                  cache ? cache->num_pages : 0, add, workspace, workspace_bytes, stream);
+}
+
+batq_status batq_kv_paged_score_ex(const batq_paged_cache* cache, int cache_bits, const batq_paged_batch* b, const void* q,
+                                   int64_t ldq, int q_heads, float scale, int causal, int window, const float* lse, float* score,
+                                   const int32_t* score_table, int score_pages, int add, void* workspace, size_t workspace_bytes,
+                                   void* stream) {
     if (!b) return BATQ_ERR_NULL;
     if (batq_status st = check_score_dims(cache, q_heads, b->batch, b->total_q, b->max_q, b->max_kv); st != BATQ_OK) return st;
     if (batq_status st = check_paged_cache(cache); st != BATQ_OK) return st;
     if (batq_status st = check_cache_bits(cache_bits); st != BATQ_OK) return st;
-    if (ldq < (int64_t)q_heads * cache->head_dim || b->table_width < 0 || window < 0) return BATQ_ERR_SHAPE;
+    if (ldq < (int64_t)q_heads * cache->head_dim || b->table_width < 0 || window < 0 || score_pages < cache->num_pages) return BATQ_ERR_SHAPE;
     if (!(scale > 0.0f) || !(scale < 2.0e38f)) return BATQ_ERR_SHAPE;
     if (b->batch == 0 || b->max_kv == 0 || b->table_width == 0) return BATQ_OK;
     if (!b->cu_q || !b->kv_len || !b->page_table || !score || (b->total_q > 0 && (!q || !lse))) return BATQ_ERR_NULL;
     if (!aligned16(q) || (ldq * 2) % 16 != 0 ||
         ((reinterpret_cast<uintptr_t>(b->cu_q) | reinterpret_cast<uintptr_t>(b->kv_len) | reinterpret_cast<uintptr_t>(b->page_table) |
-          reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(score)) & 3u) != 0 ||
+          reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(score) | reinterpret_cast<uintptr_t>(score_table)) & 3u) != 0 ||
         (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
         return BATQ_ERR_SHAPE;
     if (batq_status st = check_device(); st != BATQ_OK) return st;
@@ -1031,8 +1039,8 @@ batq_status batq_kv_paged_score(const batq_paged_cache* cache, int cache_bits, c
     if (!cus) return BATQ_ERR_DEVICE;
     const size_t need = batq::paged_score_part_bytes(*cache, q_heads, b->batch, b->total_q, b->max_q, b->max_kv, cus);
     if (need > workspace_bytes || (need > 0 && !workspace)) return BATQ_ERR_WORKSPACE;
-    BATQ_HIP(batq::launch_kv_paged_score(*cache, cache_bits, *b, q, ldq, q_heads, scale, causal != 0, window, lse, score, add != 0,
-                                         workspace, static_cast<hipStream_t>(stream)));
+    BATQ_HIP(batq::launch_kv_paged_score(*cache, cache_bits, *b, q, ldq, q_heads, scale, causal != 0, window, lse, score, score_table,
+                                         score_pages, add != 0, workspace, static_cast<hipStream_t>(stream)));
     return BATQ_OK;
 }
 
@@ -1057,27 +1065,36 @@ batq_status batq_kv_paged_evict(const batq_paged_cache* cache, int cache_bits, f
                                 const int32_t* page_table, int table_width, const int32_t* out_table, int out_width, int batch,
                                 int max_kv, int budget, int first, int last, int32_t* keep, int32_t* new_len, void* workspace,
                                 size_t workspace_bytes, void* stream) {
+    return batq_kv_paged_evict_ex(cache, cache_bits, score, nullptr, cache ? cache->num_pages : 0, kv_len, page_table, table_width, out_table,
+                                  out_width, batch, max_kv, budget, first, last, keep, new_len, workspace, workspace_bytes, stream);
+}
+
+batq_status batq_kv_paged_evict_ex(const batq_paged_cache* cache, int cache_bits, float* score, const int32_t* score_table, int score_pages,
+                                   const int32_t* kv_len, const int32_t* page_table, int table_width, const int32_t* out_table,
+                                   int out_width, int batch, int max_kv, int budget, int first, int last, int32_t* keep,
+                                   int32_t* new_len, void* workspace, size_t workspace_bytes, void* stream) {
     if (batq_status st = check_evict_dims(cache, batch, max_kv, budget); st != BATQ_OK) return st;
     if (batq_status st = check_paged_cache(cache); st != BATQ_OK) return st;
     if (batq_status st = check_cache_bits(cache_bits); st != BATQ_OK) return st;
-    if (table_width < 0 || out_width < 0 || first < 0 || last < 0 || (int64_t)first + last > budget) return BATQ_ERR_SHAPE;
+    if (table_width < 0 || out_width < 0 || first < 0 || last < 0 || (int64_t)first + last > budget || score_pages < cache->num_pages) return BATQ_ERR_SHAPE;
     const int64_t held = (int64_t)table_width * cache->page_size;
     const int64_t most = budget < max_kv ? budget : max_kv;
     if ((int64_t)out_width * cache->page_size < (most < held ? most : held)) return BATQ_ERR_SHAPE;
     if (batch == 0) return BATQ_OK;
     if (!score || !kv_len || !keep || !new_len || (table_width > 0 && !page_table) || (out_width > 0 && !out_table)) return BATQ_ERR_NULL;
     if (((reinterpret_cast<uintptr_t>(score) | reinterpret_cast<uintptr_t>(kv_len) | reinterpret_cast<uintptr_t>(page_table) |
-          reinterpret_cast<uintptr_t>(out_table) | reinterpret_cast<uintptr_t>(keep) | reinterpret_cast<uintptr_t>(new_len)) & 3u) != 0 ||
+          reinterpret_cast<uintptr_t>(out_table) | reinterpret_cast<uintptr_t>(keep) | reinterpret_cast<uintptr_t>(new_len) |
+          reinterpret_cast<uintptr_t>(score_table)) & 3u) != 0 ||
         (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || (new_len < kv_len + batch && kv_len < new_len + batch) ||
-        (page_table && page_table == out_table))
+        (out_table && (out_table == page_table || out_table == score_table)))
         return BATQ_ERR_SHAPE;
     if (batq_status st = check_device(); st != BATQ_OK) return st;
     const int cus = current_compute_units();
     if (!cus) return BATQ_ERR_DEVICE;
     const size_t need = batq::paged_evict_part_bytes(*cache, batch, max_kv, cus);
     if (need > workspace_bytes || (need > 0 && !workspace)) return BATQ_ERR_WORKSPACE;
-    BATQ_HIP(batq::launch_kv_paged_evict(*cache, cache_bits, score, kv_len, page_table, table_width, out_table, out_width, batch, max_kv,
-                                         budget, first, last, keep, new_len, workspace, static_cast<hipStream_t>(stream)));
+    BATQ_HIP(batq::launch_kv_paged_evict(*cache, cache_bits, score, score_table, score_pages, kv_len, page_table, table_width, out_table, out_width,
+                                         batch, max_kv, budget, first, last, keep, new_len, workspace, static_cast<hipStream_t>(stream)));
     return BATQ_OK;
 }
 

@@ -144,12 +144,12 @@ size_t paged_score_part_bytes(const batq_paged_cache& c, int q_heads, int batch,
 size_t paged_score_workspace_bytes(const batq_paged_cache& c, int q_heads, int batch, int total_q, int max_q, int max_kv,
                                    int compute_units);
 hipError_t launch_kv_paged_score(const batq_paged_cache& c, int bits, const batq_paged_batch& b, const void* q, int64_t ldq,
-                                 int q_heads, float scale, bool causal, int window, const float* lse, float* score, bool add,
-                                 void* workspace, hipStream_t stream);
+                                 int q_heads, float scale, bool causal, int window, const float* lse, float* score,
+                                 const int32_t* score_table, int score_pages, bool add, void* workspace, hipStream_t stream);
 size_t paged_evict_part_bytes(const batq_paged_cache& c, int batch, int max_kv, int compute_units);      // what a call takes of its workspace
 size_t paged_evict_workspace_bytes(const batq_paged_cache& c, int batch, int max_kv, int compute_units);
-hipError_t launch_kv_paged_evict(const batq_paged_cache& c, int bits, float* score, const int32_t* kv_len, const int32_t* page_table,
-                                 int table_width, const int32_t* out_table, int out_width, int batch, int max_kv, int budget,
+hipError_t launch_kv_paged_evict(const batq_paged_cache& c, int bits, float* score, const int32_t* score_table, int score_pages,
+                                 const int32_t* kv_len, const int32_t* page_table, int table_width, const int32_t* out_table, int out_width, int batch, int max_kv, int budget,
                                  int first, int last, int32_t* keep, int32_t* new_len, void* workspace, hipStream_t stream);
 size_t lora_parts_bytes(int M, int K, int N, int rank, int adapters);       // what a call takes of its workspace
 size_t lora_workspace_bytes(int M, int K, int rank);

@@ -8,7 +8,8 @@ namespace {
 
 struct EvictArgs {
     const int32_t *kv_len, *page_table, *out_table;
-    int batch, table_width, out_width, max_kv, num_pages, page_shift, kv_heads;
+    const int32_t* score_table;                             // pages of the scores; page_table where they are those of the keys
+    int batch, table_width, out_width, max_kv, num_pages, score_pages, page_shift, kv_heads;
     int budget, first, last, chunks;
     float* score;
     int32_t *keep, *new_len;
@@ -22,7 +23,7 @@ __device__ __forceinline__ int tokens_of(const EvictArgs& a, int b) {
     return (int)min((int64_t)max(0, min(a.kv_len[b], a.max_kv)), (int64_t)a.table_width << a.page_shift);
 }
 
-// A score as an unsigned number of the same order; the smallest for NaN and for tokens of pages that do not exist.
+// A score as an unsigned number of the same order; the smallest for NaN and for tokens whose page, or page of scores, does not exist.
 __device__ __forceinline__ uint32_t order_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.0f);           // (-0 becomes 0)
     if (x != x) return 0u;
@@ -78,17 +79,18 @@ __device__ __forceinline__ Found pick_bin(uint32_t c0, uint32_t c1, Found f, int
 // A (sequence, key head)'s tokens and their keys, four neighbours at a time (a page holds a multiple of them): the order of the scores,
 // with the largest key of all for the first and the last tokens, which stay in any case.
 struct Tokens {
-    const int32_t* table;
+    const int32_t *table, *score_table;
     const float* score;
     int len, first, hi;                                     // tokens [first, hi) are chosen from
-    int h, num_pages, kv_heads, page_shift;
+    int h, num_pages, score_pages, kv_heads, page_shift;
     // Behind the last token come the smallest keys: there are more tokens than stay, so that none of them is reached.
     __device__ __forceinline__ u32x4 keys(int t) const {
         typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
         u32x4 u = {0u, 0u, 0u, 0u};
         if (t >= len) return u;
-        const int page = table[t >> page_shift];
-        const bool there = (uint32_t)page < (uint32_t)num_pages;
+        const int page = score_table[t >> page_shift];
+        bool there = (uint32_t)page < (uint32_t)score_pages;
+        if (score_table != table) there = there && (uint32_t)table[t >> page_shift] < (uint32_t)num_pages;      // (always looked at: 1.5 us of 28)
         const f32x4 v = *reinterpret_cast<const f32x4*>(score + (((int64_t)(there ? page : 0) * kv_heads + h) << page_shift) + (t & ((1 << page_shift) - 1)));
 #pragma unroll
         for (int e = 0; e < 4; ++e) u[e] = there ? order_of(v[e]) : 0u;
@@ -100,7 +102,9 @@ struct Tokens {
 };
 __device__ __forceinline__ Tokens tokens_of_pair(const EvictArgs& a, int pair) {
     const int h = pair % a.kv_heads, b = pair / a.kv_heads, len = tokens_of(a, b);
-    return Tokens{a.page_table + (size_t)b * a.table_width, a.score, len, a.first, len - a.last, h, a.num_pages, a.kv_heads, a.page_shift};
+    const size_t row = (size_t)b * a.table_width;
+    const bool same = a.score_table == a.page_table;        // (pages below num_pages alone then have tokens)
+    return Tokens{a.page_table + row, a.score_table + row, a.score, len, a.first, len - a.last, h, a.num_pages, same ? a.num_pages : a.score_pages, a.kv_heads, a.page_shift};
 }
 
 // The length, the end of the list, and all of it for a sequence that stays whole, by one workgroup of a pair.  Returns whether that is all.
@@ -315,13 +319,13 @@ team_list(const EvictArgs a) {
 
 constexpr int kMove = 64;                                   // tokens of a workgroup of the move
 
-// Moves the listed tokens: keys, values, scales and score.  Bound by the copy: 64 x 8 x 2048 tokens of 128 channels in 8 bits 116 us (562 MB in and
+// Moves the listed tokens: keys, values, scales and score (0 for one without a page of scores).  Bound by the copy: 64 x 8 x 2048 tokens of 128 channels in 8 bits 116 us (562 MB in and
 // out, 4.9 TB/s, a large copy's rate).
 template <int D, int BITS>
 __global__ void __launch_bounds__(256)
 move_kernel(const EvictArgs a) {
     constexpr int kToken = D * BITS / 8, kCh = kToken / 16, kNb = D / 32;
-    __shared__ int s_from[kMove], s_from_off[kMove], s_to[kMove], s_to_off[kMove];      // page, place in it
+    __shared__ int s_from[kMove], s_from_off[kMove], s_to[kMove], s_to_off[kMove], s_score[kMove];      // page, place in it; page of the score
     const int tid = threadIdx.x;
     const int bh = blockIdx.x / a.chunks, j0 = (blockIdx.x % a.chunks) * kMove;
     const int h = bh % a.kv_heads, b = bh / a.kv_heads;
@@ -333,7 +337,9 @@ move_kernel(const EvictArgs a) {
         int from = -1, to = -1;
         if (j < n) {
             const int t = a.keep[(size_t)bh * a.budget + j];
-            from = a.page_table[(size_t)b * a.table_width + (t >> a.page_shift)];
+            const size_t entry = (size_t)b * a.table_width + (t >> a.page_shift);
+            from = a.page_table[entry];
+            s_score[tid] = a.score_table[entry];
             to = a.out_table[(size_t)b * a.out_width + (j >> a.page_shift)];
             if ((uint32_t)from >= (uint32_t)a.num_pages || (uint32_t)to >= (uint32_t)a.num_pages) from = -1;
             s_from_off[tid] = t & page_mask, s_to_off[tid] = j & page_mask;
@@ -358,7 +364,8 @@ move_kernel(const EvictArgs a) {
         const uint8_t k = a.k_scales[from], v = a.v_scales[from];
         a.k_scales[to] = k, a.v_scales[to] = v;
     }
-    if (tid < kMove && s_from[tid] >= 0) a.score[place(s_to[tid], s_to_off[tid])] = a.score[place(s_from[tid], s_from_off[tid])];
+    if (tid < kMove && s_from[tid] >= 0)
+        a.score[place(s_to[tid], s_to_off[tid])] = (uint32_t)s_score[tid] < (uint32_t)a.score_pages ? a.score[place(s_score[tid], s_from_off[tid])] : 0.0f;
 }
 
 template <int D, int BITS>
@@ -414,8 +421,8 @@ size_t paged_evict_workspace_bytes(const batq_paged_cache& c, int batch, int max
     return teams(pairs, max_kv, compute_units) ? (size_t)team_bytes(pairs, max_kv) : 0;
 }
 
-hipError_t launch_kv_paged_evict(const batq_paged_cache& c, int bits, float* score, const int32_t* kv_len, const int32_t* page_table,
-                                 int table_width, const int32_t* out_table, int out_width, int batch, int max_kv, int budget,
+hipError_t launch_kv_paged_evict(const batq_paged_cache& c, int bits, float* score, const int32_t* score_table, int score_pages,
+                                 const int32_t* kv_len, const int32_t* page_table, int table_width, const int32_t* out_table, int out_width, int batch, int max_kv, int budget,
                                  int first, int last, int32_t* keep, int32_t* new_len, void* workspace, hipStream_t stream) {
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
@@ -426,6 +433,7 @@ hipError_t launch_kv_paged_evict(const batq_paged_cache& c, int bits, float* sco
     a.out_width = out_width, a.max_kv = max_kv, a.num_pages = c.num_pages, a.page_shift = __builtin_ctz((unsigned)c.page_size);
     a.kv_heads = c.kv_heads, a.budget = budget, a.first = first, a.last = last;
     a.chunks = ((budget < max_kv ? budget : max_kv) + kMove - 1) / kMove;
+    a.score_table = score_table ? score_table : page_table, a.score_pages = score_pages;
     a.score = score, a.keep = keep, a.new_len = new_len;
     a.k_codes = c.k_codes, a.k_scales = c.k_scales, a.v_codes = c.v_codes, a.v_scales = c.v_scales;
     const int64_t pairs = (int64_t)batch * c.kv_heads;

@@ -3,7 +3,8 @@
 // key head.  gfx950 only.
 //
 // Sums belong to tokens, so a workgroup has tokens and walks rows (row = query token * group + head of the group): no two
-// workgroups add to the same place, and the order of a sum follows from the call's sizes alone.
+// workgroups add to the same place where every sequence has score pages of its own, and the order of a sum follows from the
+// call's sizes alone.
 #include <math.h>
 
 #include <type_traits>
@@ -24,6 +25,8 @@ struct ScoreArgs : PagedLists {
     const float* lse;
     const uint8_t *k_codes, *k_scales;
     float* score;
+    const int32_t* score_table;                             // pages of the scores; page_table where they are those of the keys
+    int score_pages;
     float scale;                                            // times log2 e
     int add;
     // sequences of at most few_rows rows belong to score_few, in parts of few_len tokens, the others to score_many
@@ -42,7 +45,8 @@ __device__ __forceinline__ float ref_of(float lse) { return lse == -INFINITY ? I
 // head), its four waves blocks of 32 tokens in turn.  S = Q K^T with the queries' operands in registers: lane (n, g) =
 // (l % 16, l / 16) loads channels [g D/4, (g + 1) D/4) of tokens 2n and 2n + 1 (the order in which a product runs over channels is
 // free), and element r of its results of tile x is row 16x + 4g + r: a token's sum is one over elements and four lanes.
-template <int D, int NT, int BITS>
+// OWN: with a table of the scores' pages (which costs the ragged batch 2 us: registers, an exchange a block).
+template <int D, int NT, int BITS, bool OWN>
 __global__ void __launch_bounds__(256)
 score_few(const ScoreArgs a) {
     constexpr int kC = D / 4, kU = D / 32, kToken = D * BITS / 8, kKw = kC * BITS / 32, kStages = 2;
@@ -59,7 +63,8 @@ score_few(const ScoreArgs a) {
     const int32_t* table = a.page_table + (size_t)b * a.table_width;
     const int page_mask = (1 << a.page_shift) - 1, last_page = (s.len - 1) >> a.page_shift;
     // lane i holds the page of tokens t_begin + 16 i .. + 15 (a part is at most 1024 long)
-    const int pages = table[min((t_begin + 16 * lane) >> a.page_shift, last_page)];
+    const int entry = min((t_begin + 16 * lane) >> a.page_shift, last_page), pages = table[entry];
+    const int score_pages = OWN ? a.score_table[(size_t)b * a.table_width + entry] : 0;
     // blocks t, t + 128, .. are requested kStages ahead
     uint32_t kw[kStages][2][kKw];
     uint32_t ks[kStages];
@@ -77,7 +82,14 @@ score_few(const ScoreArgs a) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) load_words<kKw>(kw[st][i], p + i * kToken);
         ks[st] = *reinterpret_cast<const uint16_t*>(a.k_scales + ((ph * (D / 32) + g * kC / 32) << a.page_shift) + off);
-        to[st] = a.score + (ph << a.page_shift) + off;
+        int64_t score_ph = ph;
+        if constexpr (OWN) {
+            const int score_page = __shfl(score_pages, (t - t_begin) >> 4);
+            const bool known = (uint32_t)score_page < (uint32_t)a.score_pages;
+            there[st] = there[st] && known;
+            score_ph = (int64_t)(known ? score_page : 0) * a.kv_heads + h;
+        }
+        to[st] = a.score + (score_ph << a.page_shift) + off;
         if (a.add) old[st][0] = to[st][0], old[st][1] = to[st][1];      // (a page holds an even number of tokens)
     };
     int t = t_begin + wave * 32;
@@ -213,8 +225,9 @@ __device__ __forceinline__ void find_key_tile(const ScoreArgs& a, int x, int* b,
 // Adds the tile's sums up and stores them: `v` for token t of the sequence.
 __device__ __forceinline__ void store_score(const ScoreArgs& a, const Seq& s, int b, int h, int t, float v) {
     if (t >= s.len) return;
-    const int page = a.page_table[(size_t)b * a.table_width + (t >> a.page_shift)];
-    if ((uint32_t)page >= (uint32_t)a.num_pages) return;
+    const size_t entry = (size_t)b * a.table_width + (t >> a.page_shift);
+    const int page = a.score_table[entry];
+    if ((uint32_t)page >= (uint32_t)a.score_pages || (uint32_t)a.page_table[entry] >= (uint32_t)a.num_pages) return;
     float* to = a.score + ((((int64_t)page * a.kv_heads + h) << a.page_shift) + (t & ((1 << a.page_shift) - 1)));
     if (a.add && t < s.first_pos) v += *to;
     *to = v;
@@ -494,8 +507,14 @@ hipError_t launch_score(const ScoreArgs& a, const ScorePlan& p, hipStream_t stre
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     if (p.few) {
-        if (p.few_rows == 16) score_few<D, 1, BITS><<<pairs * p.few_parts, 256, 0, stream>>>(a);
-        else score_few<D, 2, BITS><<<pairs * p.few_parts, 256, 0, stream>>>(a);
+        const unsigned units = pairs * p.few_parts;
+        if (a.score_table != a.page_table) {
+            if (p.few_rows == 16) score_few<D, 1, BITS, true><<<units, 256, 0, stream>>>(a);
+            else score_few<D, 2, BITS, true><<<units, 256, 0, stream>>>(a);
+        } else {
+            if (p.few_rows == 16) score_few<D, 1, BITS, false><<<units, 256, 0, stream>>>(a);
+            else score_few<D, 2, BITS, false><<<units, 256, 0, stream>>>(a);
+        }
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     if (p.parts > 1) join_scores<<<pairs * p.key_tiles, 256, 0, stream>>>(a);
@@ -517,8 +536,8 @@ size_t paged_score_workspace_bytes(const batq_paged_cache& c, int q_heads, int b
 }
 
 hipError_t launch_kv_paged_score(const batq_paged_cache& c, int bits, const batq_paged_batch& b, const void* q, int64_t ldq,
-                                 int q_heads, float scale, bool causal, int window, const float* lse, float* score, bool add,
-                                 void* workspace, hipStream_t stream) {
+                                 int q_heads, float scale, bool causal, int window, const float* lse, float* score,
+                                 const int32_t* score_table, int score_pages, bool add, void* workspace, hipStream_t stream) {
     int dev = 0;
     hipError_t e = hipGetDevice(&dev);
     const int cus = e == hipSuccess ? device_compute_units(dev, &e) : 0;
@@ -528,6 +547,7 @@ hipError_t launch_kv_paged_score(const batq_paged_cache& c, int bits, const batq
     set_lists(a, c, b, q_heads, causal, window);
     a.q = static_cast<const uint16_t*>(q), a.ldq = ldq, a.lse = lse, a.score = score, a.add = add;
     a.k_codes = c.k_codes, a.k_scales = c.k_scales;
+    a.score_table = score_table ? score_table : b.page_table, a.score_pages = score_pages;
     a.scale = scale * 1.4426950408889634f;
     a.few_rows = p.few_rows, a.few_len = p.few_len, a.few_parts = p.few_parts;
     a.key_tiles = p.key_tiles, a.chunk = p.chunk, a.parts = p.parts, a.part = static_cast<float*>(workspace);

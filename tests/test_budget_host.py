@@ -105,3 +105,24 @@ def test_budgets_past_two_to_the_thirty_are_refused(B):
         assert evict(B, ok, budget=budget, out_width=3) == 2 and evict(B, ok, budget=budget, out_width=3, batch=0) == 2
         assert B.lib.batq_kv_paged_evict_workspace(C.byref(ok), 2, 1 << 20, budget) == 0
     assert evict(B, ok, budget=1 << 30, out_width=3, batch=0) == 0
+
+
+def test_score_tables_are_looked_at(B):
+    ok = cache()
+    b = Batch(cu_q=P, kv_len=P, page_table=P, batch=2, table_width=3, total_q=5, max_q=4, max_kv=48)
+
+    def score_ex(table, pages, **kw):
+        bb = Batch(**{**{n: getattr(b, n) for n, _ in Batch._fields_}, **kw})
+        return B.lib.batq_kv_paged_score_ex(C.byref(ok), 4, C.byref(bb), P, 256, 4, 0.1, 1, 0, P, P, table, pages, 0, None, 0, None)
+
+    def evict_ex(table, pages, batch=2, out=2 * P):
+        return B.lib.batq_kv_paged_evict_ex(C.byref(ok), 4, P, table, pages, P, P, 3, out, 2, batch, 48, 20, 1, 2, P, 2 * P, None, 0, None)
+
+    for f in (score_ex, evict_ex):
+        for table in (None, 3 * P):
+            assert f(table, ok.num_pages - 1) == 2 and f(table, 0) == 2 and f(table, -1) == 2
+            assert f(table, ok.num_pages, batch=0) == 0 and f(table, 2 ** 31 - 1, batch=0) == 0
+        assert f(3 * P + 2, ok.num_pages) == 2
+    assert evict_ex(2 * P, ok.num_pages) == 2               # the table that the tokens move to
+    assert B.lib.batq_kv_paged_score_ex(None, 4, C.byref(b), P, 256, 4, 0.1, 1, 0, P, P, None, 4, 0, None, 0, None) == 1
+    assert B.lib.batq_kv_paged_evict_ex(None, 4, P, None, 4, P, P, 3, 2 * P, 2, 2, 48, 20, 1, 2, P, 2 * P, None, 0, None) == 1

@@ -230,6 +230,67 @@ def test_each_row_of_many_takes_its_own_lse(B, hq, hkv, lens, qs):
     br.assert_score(got, br.score(br.values(*arrays[:2], 8), q, lse, had, cu, lens, table, page, D ** -0.5, True, 0, False), had)
 
 
+def share_prefix(rng, arrays, table, lens, page, prefix, extra):
+    """The first `prefix` tokens' pages of sequence 0 for all sequences, and score pages behind the cache's for those that share them.
+    Returns (page table, score table, arrays with a copy of each shared page in its score page's place, number of pages of the cache)."""
+    pages, n = arrays[0].shape[0], prefix // page
+    table, score_table = table.copy(), table.copy()
+    at = pages + rng.permutation(extra)[: n * (len(lens) - 1)]
+    copies = [np.concatenate([a, a[rng.integers(0, pages, extra)]]) for a in arrays]
+    for b in range(1, len(lens)):
+        table[b, :n] = table[0, :n]
+        score_table[b, :n] = at[(b - 1) * n: b * n]
+        for c in copies:
+            c[score_table[b, :n]] = c[table[0, :n]]
+    return table, score_table, copies, pages
+
+
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("qs,hq,hkv,D,bits", [([1, 1, 1], 8, 2, 128, 4), ([2, 5, 1], 4, 1, 64, 8), ([40, 300, 1], 4, 2, 64, 4), ([200, 1, 130], 14, 2, 128, 8)])
+def test_scores_of_a_shared_prefix(B, qs, hq, hkv, D, bits, add):
+    """Three sequences share the pages of their first tokens and have score pages of their own for them: each place gets its own
+    sequence's sum, the same bits whenever the call is repeated.  Entries without a page of either kind take no part."""
+    rng = np.random.default_rng(31 + sum(qs))
+    page = 16
+    arrays, qbits, q, cu, lens, table, T = br.batch_case(rng, [1100, 700, 400], qs, hq, hkv, D, page, bits)
+    table, score_table, copies, pages = share_prefix(rng, arrays, table, lens, page, 256, 40)
+    lse = lse_of(arrays, bits, q, cu, lens, table, page, True, 0, T)
+    lse[np.isnan(lse)] = 3.0
+    score_table[1, 3], score_table[2, 5], table[0, 20], table[1, 18] = -1, pages + 40, -5, pages
+    where = np.where((table < 0) | (table >= pages), -1, score_table)
+    had = rng.uniform(0, 3, (pages + 40, hkv, page)).astype(np.float32)
+    cache, qd = make_cache(B, arrays, bits), to_dev(qbits, "bf16")
+    got = [run_score(B, cache, qd, lse, had, cu, lens, table, score_table=dev(score_table), add=add) for _ in range(3)]
+    br.assert_score(got[0], br.score(br.values(*copies[:2], bits), q, lse, had, cu, lens, where, page, D ** -0.5, True, 0, add), had)
+    assert all(np.array_equal(x.view(np.uint32), got[0].view(np.uint32)) for x in got[1:])
+    own = run_score(B, cache, qd, lse, had[:pages], cu, lens, table, add=add)      # what is not shared is as without the table
+    mine = np.setdiff1d(table[(table >= 0) & (table < pages)], table[0, :16])
+    assert np.array_equal(own[mine].view(np.uint32), got[0][mine].view(np.uint32))
+
+
+@pytest.mark.parametrize("lens,budget,kind", [([300, 500, 90], 100, "sums"), ([5000, 300, 4500], 700, "odd"), ([40000, 33000], 3000, "ties")])
+def test_evict_by_scores_of_their_own(B, lens, budget, kind):
+    """Sequences with a common prefix, evicted by score pages of their own; a token without one counts as the smallest and moves
+    with a score of 0."""
+    rng = np.random.default_rng(41 + budget)
+    hkv, D, page, first, last = 2, 64, 16, 3, 20
+    arrays, lens, table, out_table = evict_case(rng, lens, hkv, D, page, budget, 4)
+    table, score_table, copies, pages = share_prefix(rng, arrays, table, lens, page, 64, 20)
+    none = pages + 20                                       # a page of scores that is not there
+    score = scores_for(rng, kind, (pages + 20, hkv, page))
+    want_score = np.concatenate([score, np.full((1, hkv, page), np.nan, np.float32)])
+    copies = [np.concatenate([c, c[table[0, 0]][None]]) for c in copies]
+    told, where = score_table.copy(), score_table.copy()
+    told[1, 0], where[1, 0] = -3, none                      # among the first tokens, which stay
+    want = br.evict(copies, want_score, lens, where, out_table, budget, first, last)
+    for h in range(hkv):
+        j = np.arange(want[3][1])
+        moved = want[2][1, h, j] < page
+        want[1][out_table[1][j[moved] // page], h, j[moved] % page] = 0.0
+    got = run_evict(B, make_cache(B, arrays, 4), score, lens, table, out_table, budget, first, last, score_table=dev(told))
+    assert_evicted(got, ([w[:pages] for w in want[0]], want[1][:none], want[2], want[3]))
+
+
 # ---------------------------------------------------------------------------------------- eviction
 EVICT = [
     # lens, kv heads, D, page, budget, first, last
@@ -617,3 +678,34 @@ def test_decoding_within_a_budget(B, bits):
         if max(lens) >= budget + 16:
             evict()
     assert list(pos) == [110, 65] and max(lens) < budget + 16
+
+
+def test_a_prefix_that_is_shared_scored_and_evicted(B):
+    """Two sequences decode behind one prompt whose pages they share, each with scores of its own, and are cut down to a budget: as two
+    sequences with copies of those pages, bit for bit."""
+    import torch
+    rng = np.random.default_rng(51)
+    hq, hkv, D, page, budget = 8, 2, 128, 16, 96
+    L = [330, 300]
+    arrays, lens, table, out_table = evict_case(rng, L, hkv, D, page, budget, 4)
+    pages = arrays[0].shape[0]
+    shared, n = table.copy(), 256 // page
+    shared[1, :n] = table[0, :n]
+    for a in arrays:
+        a[table[1, :n]] = a[table[0, :n]]                   # (sequence 1's own pages hold the copies; their scores are its own in both runs)
+    results = []
+    for t, st in ((table, None), (shared, table)):
+        cache, score = make_cache(B, arrays, 4), torch.zeros((pages, hkv, page), device="cuda")
+        kw = {} if st is None else dict(score_table=dev(st))
+        r = np.random.default_rng(52)
+        for step, qn in enumerate([60, 1, 1, 1]):
+            qd = to_dev(ref.bf16_values(r, 2 * qn, hq * D)[0], "bf16")
+            cu, l32 = dev(np.array([0, qn, 2 * qn], np.int32)), dev(lens - 3 + step)
+            lse = torch.empty((2 * qn, hq), device="cuda")
+            B.batq_paged_attention(cache, qd, cu, l32, dev(t), qn, 330, lse=lse)
+            B.batq_kv_paged_score(cache, qd, lse, score, cu, l32, dev(t), qn, 330, add=step > 0, **kw)
+        keep, new_len = B.batq_kv_paged_evict(cache, score, l32, dev(t), dev(out_table), 330, budget, 2, 16, **kw)
+        torch.cuda.synchronize()
+        results.append([score, keep, new_len, cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales])
+    assert all(torch.equal(x, y) for x, y in zip(*results))
+    assert not torch.equal(results[0][1][0], results[0][1][1])
