@@ -502,13 +502,15 @@ batq_status batq_paged_attention_ex(const batq_paged_cache* cache, int cache_bit
  *   w[h][t] = sum of exp(scale * (q_i . k_t) - lse_i) over the queries i that see t and the query heads that read h
  *   score   DEVICE fp32 [num_pages][kv_heads][page_size], laid out as the cache's pages: a token's place is set to w, or with
  *           add != 0 to what it held plus w.  The queries' own tokens (the last cu_q[b + 1] - cu_q[b] of a sequence) are new: their
- *           places are always set, so that pages need not be cleared.  Places that hold no token are left as they are.
+ *           places are always set, so that pages need not be cleared.  Places that hold no token are left as they are, and with
+ *           add those of older tokens that no query sees: nothing is written to them (without add they are set to 0)
  *   lse     DEVICE fp32 [total_q][q_heads]; a row with -infinity (it saw nothing) adds nothing
  * A batch whose queries are fewer than those of the attention (a prompt's last ones) has their rows alone in q and lse.  max_q and max_kv
  * bound what is served as there.  Sums are fp32, in an order that depends on the arguments alone.  A NaN score comes from
  * a NaN lse, or from a key that is NaN.
  * A page of scores belongs to one entry of a call's tables: what a page holds that two entries list is unspecified (two sums meet in
- * it, and from run to run another one may be the last).  Sequences of a call that share cache pages (a common prefix) take
+ * it, and from run to run another one may be the last).  With add an entry whose tokens no query sees does not count: a page that was
+ * given back behind a window may be another sequence's.  Without add such an entry has to leave the table (-1).  Sequences of a call that share cache pages (a common prefix) take
  * batq_kv_paged_score_ex, with score pages of their own:
  *   score        has score_pages pages, num_pages or more (else BATQ_ERR_SHAPE)
  *   score_table  DEVICE int32 [batch][table_width]: the page of `score` for the tokens of page page_table[b][i]; NULL: the same page.  A

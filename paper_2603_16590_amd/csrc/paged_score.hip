@@ -38,6 +38,21 @@ struct ScoreArgs : PagedLists {
 // The subtrahend of a row's exponents; a row that has seen nothing has no weights.
 __device__ __forceinline__ float ref_of(float lse) { return lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f; }
 
+// Places of tokens before this one are not written: with `add`, those of old tokens that no query sees (pages that a sequence has
+// given back behind its window may be another one's).
+__device__ __forceinline__ int kept_below(const ScoreArgs& a, const Seq& s) { return !a.add ? 0 : s.n ? s.t_lo : s.first_pos; }
+
+// Stores a sum: `v` for token t of the sequence.
+__device__ __forceinline__ void store_score(const ScoreArgs& a, const Seq& s, int b, int h, int t, float v) {
+    if (t < kept_below(a, s) || t >= s.len) return;
+    const size_t entry = (size_t)b * a.table_width + (t >> a.page_shift);
+    const int page = a.score_table[entry];
+    if ((uint32_t)page >= (uint32_t)a.score_pages || (uint32_t)a.page_table[entry] >= (uint32_t)a.num_pages) return;
+    float* to = a.score + ((((int64_t)page * a.kv_heads + h) << a.page_shift) + (t & ((1 << a.page_shift) - 1)));
+    if (a.add && t < s.first_pos) v += *to;
+    *to = v;
+}
+
 // Few rows to a key head (decoding): bound by the stream of key codes, read once (64 x 8192 tokens of 8 heads of 128 channels in 4 bits:
 // 302 MB in 60 us, 5.0 TB/s), and for ragged sequences by a part's chain of loads (64 of up to 8192 tokens: 35 MB in 21 us; parts of 256, 512
 // tokens 26, 22 us there, but 86, 69 us for 64 x 8192; tokens shared out evenly over all workgroups 23 and 90: more registers, fewer waves;
@@ -45,6 +60,7 @@ __device__ __forceinline__ float ref_of(float lse) { return lse == -INFINITY ? I
 // head), its four waves blocks of 32 tokens in turn.  S = Q K^T with the queries' operands in registers: lane (n, g) =
 // (l % 16, l / 16) loads channels [g D/4, (g + 1) D/4) of tokens 2n and 2n + 1 (the order in which a product runs over channels is
 // free), and element r of its results of tile x is row 16x + 4g + r: a token's sum is one over elements and four lanes.
+// Blocks that no row sees are left out (64 x 8192 tokens behind a window of 1024: 17 us beside 65; 1 x 131072: 9.6 beside 19).
 // OWN: with a table of the scores' pages (which costs the ragged batch 2 us: registers, an exchange a block).
 template <int D, int NT, int BITS, bool OWN>
 __global__ void __launch_bounds__(256)
@@ -59,6 +75,11 @@ score_few(const ScoreArgs a) {
     const int rows = s.n * a.group;
     const int t_begin = part * a.few_len, t_end = min(s.len, t_begin + a.few_len);
     if (rows > a.few_rows || t_begin >= t_end) return;
+    // blocks of 32 tokens with one that some row sees: [b_lo, b_hi); the others' sums are zero
+    const int b_lo = min(t_end, t_begin + (max(0, s.t_lo - t_begin) & ~31)), b_hi = s.n ? max(b_lo, min(t_end, s.t_hi)) : b_lo;
+    for (int t = t_begin + threadIdx.x; t < b_lo; t += 256) store_score(a, s, b, h, t, 0.0f);
+    for (int t = b_lo + ((b_hi - b_lo + 31) & ~31) + threadIdx.x; t < t_end; t += 256) store_score(a, s, b, h, t, 0.0f);
+    if (b_lo == b_hi) return;
 
     const int32_t* table = a.page_table + (size_t)b * a.table_width;
     const int page_mask = (1 << a.page_shift) - 1, last_page = (s.len - 1) >> a.page_shift;
@@ -92,20 +113,20 @@ score_few(const ScoreArgs a) {
         to[st] = a.score + (score_ph << a.page_shift) + off;
         if (a.add) old[st][0] = to[st][0], old[st][1] = to[st][1];      // (a page holds an even number of tokens)
     };
-    int t = t_begin + wave * 32;
+    int t = b_lo + wave * 32;
 #pragma unroll
     for (int st = 0; st < kStages; ++st)
-        if (t + 128 * st < t_end) request(t + 128 * st, st);
+        if (t + 128 * st < b_hi) request(t + 128 * st, st);
 
     bf16x8 qf[NT][kU];
     float ref[NT][4];
     int lo[NT][4], hi[NT][4];                               // tokens [lo, hi) are visible to row 16x + 4g + r
 #pragma unroll
     for (int x = 0; x < NT; ++x) {
-        const int row = min(x * 16 + n, max(0, rows - 1)), i = row / a.group;
+        const int row = min(x * 16 + n, rows - 1), i = row / a.group;
         const uint16_t* p = a.q + (size_t)(s.begin + i) * a.ldq + (size_t)(h * a.group + row - i * a.group) * D + g * kC;
 #pragma unroll
-        for (int u = 0; u < kU; ++u) qf[x][u] = rows ? *reinterpret_cast<const bf16x8*>(p + 8 * u) : bf16x8{};
+        for (int u = 0; u < kU; ++u) qf[x][u] = *reinterpret_cast<const bf16x8*>(p + 8 * u);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int rr = x * 16 + 4 * g + r, ii = rr / a.group, pos = s.first_pos + ii;
@@ -119,10 +140,12 @@ score_few(const ScoreArgs a) {
     const bool full = rows == NT * 16;
     const int all_hi = !full ? 0 : a.causal ? min(s.len, s.first_pos + 1) : s.len;
     const int all_lo = first_seen(a, s.first_pos + s.n - 1);
-    while (t < t_end)
+    const int kept = kept_below(a, s);                      // (below t_end, or no row would see a token of the part)
+    const uint32_t places = (uint32_t)(t_end - kept);
+    while (t < b_hi)
 #pragma unroll
     for (int st = 0; st < kStages; ++st) {
-        if (st > 0 && t >= t_end) break;
+        if (st > 0 && t >= b_hi) break;
         f32x4 sc[NT][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -140,7 +163,7 @@ score_few(const ScoreArgs a) {
         float* const at = to[st];
         const f32x2 had = old[st];
         const bool stored = there[st];
-        if (t + 128 * kStages < t_end) request(t + 128 * kStages, st);
+        if (t + 128 * kStages < b_hi) request(t + 128 * kStages, st);
         const bool whole = t >= all_lo && t + 32 <= all_hi;
         float sum[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -162,8 +185,8 @@ score_few(const ScoreArgs a) {
         if (g == 0 && stored) {
             const int tok = t + 2 * n;
             const f32x2 v = {sum[0] + (a.add && tok < s.first_pos ? had[0] : 0.0f), sum[1] + (a.add && tok + 1 < s.first_pos ? had[1] : 0.0f)};
-            if (tok < t_end) at[0] = v[0];
-            if (tok + 1 < t_end) at[1] = v[1];
+            if ((uint32_t)(tok - kept) < places) at[0] = v[0];
+            if ((uint32_t)(tok + 1 - kept) < places) at[1] = v[1];
         }
         t += 128;
     }
@@ -222,17 +245,6 @@ __device__ __forceinline__ void find_key_tile(const ScoreArgs& a, int x, int* b,
     }
 }
 
-// Adds the tile's sums up and stores them: `v` for token t of the sequence.
-__device__ __forceinline__ void store_score(const ScoreArgs& a, const Seq& s, int b, int h, int t, float v) {
-    if (t >= s.len) return;
-    const size_t entry = (size_t)b * a.table_width + (t >> a.page_shift);
-    const int page = a.score_table[entry];
-    if ((uint32_t)page >= (uint32_t)a.score_pages || (uint32_t)a.page_table[entry] >= (uint32_t)a.num_pages) return;
-    float* to = a.score + ((((int64_t)page * a.kv_heads + h) << a.page_shift) + (t & ((1 << a.page_shift) - 1)));
-    if (a.add && t < s.first_pos) v += *to;
-    *to = v;
-}
-
 template <int D, int BITS>
 __global__ void __launch_bounds__(256, 2)
 score_many(const ScoreArgs a) {
@@ -259,7 +271,10 @@ score_many(const ScoreArgs a) {
     if (a.parts > 1) {
         row_lo = max(row_lo, part * a.chunk);
         row_hi = min(row_hi, (int)min((int64_t)0x7FFFFFFF, (int64_t)(part + 1) * a.chunk));
-        if (row_lo >= row_hi) return;                       // (its sum is not read)
+    }
+    if (row_lo >= row_hi) {                                 // (a part's sum is then not read)
+        if (a.parts == 1) store_score(a, s, b, h, tile0 + tid, 0.0f);
+        return;
     }
 
     // staging: a thread moves chunk tid % kCh of rows tid / kCh + kPer k of a stage, the first 64 threads a row's lse each.  A row's
@@ -309,7 +324,7 @@ score_many(const ScoreArgs a) {
         }
         if (wave == 0) s_ref[buf][lane] = r0 + lane < row_hi ? ref_of(lw) : INFINITY;
     };
-    if (row_lo < row_hi) request(row_lo);
+    request(row_lo);
     const int32_t* table = a.page_table + (size_t)b * a.table_width;
     bf16x8 kf[2][kU];
 #pragma unroll
@@ -331,7 +346,7 @@ score_many(const ScoreArgs a) {
     float acc[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) acc[i] = 0.0f;
-    if (row_lo < row_hi) stage(row_lo, 0);
+    stage(row_lo, 0);
     __syncthreads();
     // 32 rows' scores: chunk u of a lane's row is at (its chunk 0) ^ 16 u
     auto product = [&](v16f (&sc)[2], int buf, int sub) {

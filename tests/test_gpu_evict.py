@@ -291,6 +291,51 @@ def test_evict_by_scores_of_their_own(B, lens, budget, kind):
     assert_evicted(got, ([w[:pages] for w in want[0]], want[1][:none], want[2], want[3]))
 
 
+@pytest.mark.parametrize("lens,qs,hq,hkv,D,window", [([3000, 90], [1, 1], 8, 2, 128, 50), ([500, 700, 33], [3, 1, 0], 4, 2, 64, 100), ([900, 1500], [64, 100], 4, 1, 64, 200),
+                                                     ([1000], [5], 2, 1, 64, 1), ([3000, 2500], [700, 1], 8, 1, 128, 33), ([400, 300], [0, 2], 4, 1, 64, 0)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_tokens_that_no_query_sees(B, lens, qs, hq, hkv, D, window, causal):
+    """With add their places keep their bits (-0 among them, which a sum with 0 would turn to 0); without it they become 0."""
+    rng = np.random.default_rng(61 + sum(lens))
+    page = 16
+    arrays, qbits, q, cu, lens, table, T = br.batch_case(rng, lens, qs, hq, hkv, D, page, 4)
+    lse = lse_of(arrays, 4, q, cu, lens, table, page, causal, window, T)
+    had = np.where(rng.random((arrays[0].shape[0], hkv, page)) < 0.5, -0.0, rng.uniform(0, 3, (arrays[0].shape[0], hkv, page))).astype(np.float32)
+    cache, qd = make_cache(B, arrays, 4), to_dev(qbits, "bf16")
+    unseen = []
+    for b, L in enumerate(lens):
+        first = L - qs[b]
+        t = np.arange(max(0, first - window + 1) if window else 0) if qs[b] else np.arange(L)
+        unseen.append((table[b, t // page], t % page))
+    assert sum(len(x[0]) for x in unseen) > 100
+    for add in (True, False):
+        got = run_score(B, cache, qd, lse, had, cu, lens, table, causal=causal, window=window, add=add)
+        br.assert_score(got, br.score(br.values(*arrays[:2], 4), q, lse, had, cu, lens, table, page, D ** -0.5, causal, window, add), had)
+        for pg, off in unseen:
+            want = had[pg, :, off] if add else np.zeros((len(pg), hkv), np.float32)
+            assert np.array_equal(got[pg, :, off].view(np.uint32), want.view(np.uint32))
+
+
+@pytest.mark.parametrize("qn", [1, 40])
+def test_pages_given_back_behind_a_window(B, qn):
+    """A sequence's table still names pages behind its window that are another sequence's by now: with add they get the other's sums."""
+    rng = np.random.default_rng(71 + qn)
+    hq, hkv, D, page, window = 4, 2, 128, 16, 60
+    arrays, qbits, q, cu, lens, table, T = br.batch_case(rng, [900, 400], [qn, qn], hq, hkv, D, page, 4)
+    lse = lse_of(arrays, 4, q, cu, lens, table, page, True, window, T)
+    had = rng.uniform(0, 3, (arrays[0].shape[0], hkv, page)).astype(np.float32)
+    want = br.score(br.values(*arrays[:2], 4), q, lse, had, cu, lens, table, page, D ** -0.5, True, window, True)
+    gone = (900 - qn - window + 1) // page                  # pages before this one are seen by nobody
+    stale = table.copy()
+    stale[0, :gone] = np.resize(table[1, : -(-400 // page)], gone)
+    untouched = want[1].copy()
+    untouched[table[0, :gone]] = -1.0
+    cache, qd = make_cache(B, arrays, 4), to_dev(qbits, "bf16")
+    got = [run_score(B, cache, qd, lse, had, cu, lens, stale, window=window, add=True) for _ in range(3)]
+    br.assert_score(got[0], (want[0], untouched), had)
+    assert all(np.array_equal(x.view(np.uint32), got[0].view(np.uint32)) for x in got[1:])
+
+
 # ---------------------------------------------------------------------------------------- eviction
 EVICT = [
     # lens, kv heads, D, page, budget, first, last
