@@ -502,8 +502,11 @@ batq_status batq_paged_attention_ex(const batq_paged_cache* cache, int cache_bit
  *   w[h][t] = sum of exp(scale * (q_i . k_t) - lse_i) over the queries i that see t and the query heads that read h
  *   score   DEVICE fp32 [num_pages][kv_heads][page_size], laid out as the cache's pages: a token's place is set to w, or with
  *           add != 0 to what it held plus w.  The queries' own tokens (the last cu_q[b + 1] - cu_q[b] of a sequence) are new: their
- *           places are always set, so that pages need not be cleared.  Places that hold no token are left as they are, and with
- *           add those of older tokens that no query sees: nothing is written to them (without add they are set to 0)
+ *           places are always set.  Pages need not be cleared where each token is once a query of a scoring call, or where the
+ *           first call of a sequence is without add; with add, older tokens that were in no call before (a prompt of which the
+ *           last queries alone are scored) would keep what their pages' last owners left.  Places that hold no token are left as
+ *           they are, and with add those of older tokens that no query sees: nothing is written to them (without add they are
+ *           set to 0)
  *   lse     DEVICE fp32 [total_q][q_heads]; a row with -infinity (it saw nothing) adds nothing
  * A batch whose queries are fewer than those of the attention (a prompt's last ones) has their rows alone in q and lse.  max_q and max_kv
  * bound what is served as there.  Sums are fp32, in an order that depends on the arguments alone.  A NaN score comes from

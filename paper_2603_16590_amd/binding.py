@@ -813,7 +813,7 @@ def batq_kv_paged_score(cache: PagedCache, q, lse, score, cu_q, kv_len, page_tab
     """What each cached token receives of the attention of the batch (q, lists, scale, causal, window as in
     batq_paged_attention; lse: fp32 [total_q, q_heads], as it returned it): the softmax weights summed over the queries and the
     query heads of a key head, into ``score`` (fp32 [pages, kv_heads, page_size]).  add: to what the tokens there have, except the
-    queries' own, which are new.  Sequences that share pages of the cache (a common prefix) need pages of scores of their own, or
+    queries' own, which are new (a sequence's first call is without it, unless its queries are all of its tokens).  Sequences that share pages of the cache (a common prefix) need pages of scores of their own, or
     what the shared ones hold is unspecified: score_table (int32, as page_table) names the page of ``score`` (then of any number of
     pages from the cache's on) for each of page_table's.  Returns score."""
     import torch

@@ -336,6 +336,33 @@ def test_pages_given_back_behind_a_window(B, qn):
     assert all(np.array_equal(x.view(np.uint32), got[0].view(np.uint32)) for x in got[1:])
 
 
+@pytest.mark.parametrize("first", ["whole prompt, added", "last queries, set", "last queries, added"])
+def test_first_scores_in_pages_that_were_used_before(B, first):
+    """Pages full of other sequences' scores: a first call over the whole prompt may add, one of its last queries must not; the steps behind
+    it add.  (Added from the start, the last queries leave the old owners' scores in the earlier tokens' places.)"""
+    rng = np.random.default_rng(81)
+    hq, hkv, D, page, L = 4, 2, 64, 16, 210
+    arrays, qbits, q, _, lens, table, T = br.batch_case(rng, [L + 2], [L + 2], hq, hkv, D, page, 8)
+    kv, cache, qd = br.values(*arrays[:2], 8), make_cache(B, arrays, 8), to_dev(qbits, "bf16")
+    lse = lse_of(arrays, 8, q, np.array([0, L + 2]), lens, table, page, True, 0, T)
+    junk = np.full((arrays[0].shape[0], hkv, page), 1e3, np.float32)
+    begin, add = (0 if "whole" in first else L - 20), "added" in first
+    score, clean = junk, np.zeros_like(junk)
+    want, tol = clean.astype(np.float64), clean.astype(np.float64)
+    for lo, hi, a in ((begin, L, add), (L, L + 1, True), (L + 1, L + 2, True)):
+        cu, n = np.array([0, hi - lo], np.int32), np.array([hi], np.int32)
+        score = run_score(B, cache, qd[lo:hi], lse[lo:hi], score, cu, n, table, add=a)
+        w, t = br.score(kv, q[lo:hi], lse[lo:hi], clean, cu, n, table, page, D ** -0.5, True, 0, True)
+        want, tol = want + w, tol + np.maximum(t, 0) + 2.0 ** -24 * np.abs(want + w)
+    at = np.arange(L + 2)
+    at = (table[0, at // page], slice(None), at % page)
+    if first != "last queries, added":
+        assert np.all(np.abs(score[at] - want[at]) <= tol[at])
+    else:                                                   # old tokens: fp32 sums upon the thousand, each off by half a step of 2^-14
+        old = np.arange(L + 2)[:, None] < begin
+        assert np.all(np.abs(score[at] - want[at] - 1e3 * old) <= tol[at] + 3 * 2.0 ** -14 * old)
+
+
 # ---------------------------------------------------------------------------------------- eviction
 EVICT = [
     # lens, kv heads, D, page, budget, first, last
