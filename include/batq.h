@@ -486,8 +486,8 @@ batq_status batq_paged_attention(const batq_paged_cache* cache, const batq_paged
  *   codes   [kv_heads][page_size][head_dim / 2] bytes a page, channel 2 j of a token in bits 3:0 of its byte j, channel 2 j + 1 in
  *           bits 7:4; batq_kv_paged_code_bytes_ex() in all.  Scales as in a cache of 8 bits.
  * A block is clipped and quantised as batq_kv_append with act_bits 4 does.  All that is said above of the append and of the attention
- * holds for either width; the plain calls are these with cache_bits 8, and a workspace serves both.  No code of 4 bits is NaN: of
- * a NaN block the scale byte is 255. */
+ * holds for either width; the plain calls are these with cache_bits 8, and a workspace serves both.  No code of 4 bits is NaN:
+ * where the attention and the scores read NaN is in a block whose scale byte is 255, which the append never writes. */
 size_t batq_kv_paged_code_bytes_ex(int num_pages, int page_size, int kv_heads, int head_dim, int cache_bits);
 batq_status batq_kv_paged_append_ex(const batq_paged_cache* cache, int cache_bits, const batq_transform* tk,
                                     const batq_transform* tv, const batq_rope* rope, const void* q, int64_t ldq, int q_heads,

@@ -217,6 +217,44 @@ def test_append_of_many_tokens_equals_single_ones(B, D, rot, inter, dtype):
         assert np.array_equal(x, y)
 
 
+@pytest.mark.parametrize("D,M,rot,dtype", [(64, 40, 64, "bf16"), (128, 33, 0, "f32"), (128, 4489, 128, "bf16"), (64, 4489, 0, "f32")])
+@pytest.mark.parametrize("bits", [4, 8])
+def test_append_never_writes_scale_byte_255(B, D, M, rot, dtype, bits):
+    """Not for NaN and infinite elements either (their blocks' codes are nobody's promise); all other blocks are as without them."""
+    import torch
+    rng = np.random.default_rng(91 + M + D)
+    hkv, page = 3, 64
+    X = rng.standard_normal((M, 2 * hkv * D)).astype(np.float32)
+    if dtype == "bf16":
+        X = bi.bf16_bits_to_f32(bi.f32_to_bf16_bits(X))
+    odd = X.copy()
+    hit = np.zeros((M, 2 * hkv * D // 32), bool)
+    for i, x in enumerate((np.nan, -np.nan, np.inf, -np.inf, "all")):
+        m = (7 * i + 3) % M
+        if x == "all":
+            odd[m, : D] = np.nan
+            hit[m, : D // 32] = True
+        else:
+            odd[m, 5 + 32 * i], odd[m, hkv * D + 9] = x, x
+            hit[m, (5 + 32 * i) // 32] = hit[m, (hkv * D + 9) // 32] = True
+    if rot:                                                 # a rotated channel's partner is half of the rotation away
+        hit |= hit.reshape(M, 2, hkv, D // 32).any(3, keepdims=True).repeat(D // 32, 3).reshape(M, -1)
+    caches = []
+    for x in (X, odd):
+        xd = to_dev(bi.f32_to_bf16_bits(x), "bf16") if dtype == "bf16" else to_dev(x, "f32")
+        cache = B.PagedCache(-(-M // page), page, hkv, D, bits=bits)
+        B.batq_kv_paged_append(cache, xd[:, : hkv * D], xd[:, hkv * D:], torch.arange(M, device="cuda"),
+                               positions=torch.arange(M, dtype=torch.int32, device="cuda") if rot else None, rope=dev(ref.rope_table(M, rot)) if rot else None)
+        torch.cuda.synchronize()
+        caches.append(host(cache))
+    fine = ~hit.reshape(M, 2, hkv, D // 32)
+    for n in range(4):
+        a, b = (c[n].transpose(0, 2, 1, 3).reshape(-1, hkv, D // 32, 4 * bits) if n % 2 == 0 else c[n].transpose(0, 3, 1, 2).reshape(-1, hkv, D // 32, 1)
+                for c in caches)
+        assert np.array_equal(a[:M][fine[:, n // 2]], b[:M][fine[:, n // 2]])
+        assert n % 2 == 0 or not (b == 255).any()
+
+
 # ---------------------------------------------------------------------------------------- attention
 def run_attention(B, cache, qd, cu, lens, table, T, hq, max_q=None, max_kv=None, **kw):
     import torch
