@@ -781,3 +781,108 @@ def test_a_prefix_that_is_shared_scored_and_evicted(B):
         results.append([score, keep, new_len, cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales])
     assert all(torch.equal(x, y) for x, y in zip(*results))
     assert not torch.equal(results[0][1][0], results[0][1][1])
+
+
+def dirty(n, byte):
+    import torch
+    return torch.full((n,), byte, dtype=torch.uint8, device="cuda")
+
+
+def test_long_sequences_in_graphs_with_workspaces_of_larger_calls(B):
+    """Several workgroups to a (sequence, key head), whose histograms and counts are in the workspace: on another stream and replayed from
+    a graph, with other scores and lengths, eager calls between the replays, and workspaces of larger calls full of anything; every
+    replay against the statement."""
+    import torch
+    rng = np.random.default_rng(101)
+    hkv, D, page, budget, first, last, most = 2, 64, 256, 1500, 3, 200, 40000
+    arrays, lens, table, out_table = evict_case(rng, [most, 33000, 700], hkv, D, page, budget, 4)
+    cache = make_cache(B, arrays, 4)
+    need = B.batq_kv_paged_evict_workspace(cache, 3, most, budget)
+    larger = B.batq_kv_paged_evict_workspace(cache, 5, 200000, budget)
+    assert 0 < need < larger
+    ws = dirty(larger, 0xFF)
+    with pytest.raises(B.BatqError):                        # it is in use
+        B.batq_kv_paged_evict(cache, dev(np.zeros((arrays[0].shape[0], hkv, page), np.float32)), dev(lens), dev(table), dev(out_table), most, budget,
+                              workspace=dirty(256, 0))
+    score, dlens = torch.zeros((arrays[0].shape[0], hkv, page), device="cuda"), dev(lens)
+    keep, new_len = torch.zeros((3, hkv, budget), dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    dtable, dout = dev(table), dev(out_table)
+
+    def step(keep=keep, new_len=new_len):
+        B.batq_kv_paged_evict(cache, score, dlens, dtable, dout, most, budget, first, last, keep=keep, new_len=new_len, workspace=ws)
+
+    def restore(kind):
+        x = scores_for(rng, kind, tuple(score.shape))
+        for t, a in zip((cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales), arrays):
+            t.copy_(dev(a))
+        score.copy_(dev(x))
+        keep.fill_(-5), new_len.fill_(-5)
+        return x
+
+    def result():
+        return host(cache), score.cpu().numpy(), keep.cpu().numpy(), new_len.cpu().numpy()
+
+    x = restore("sums")
+    side, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    assert_evicted(result(), br.evict(arrays, x, lens, table, out_table, budget, first, last))
+    with torch.cuda.graph(g, stream=side):
+        step()
+    for rep, (kind, ls) in enumerate((("ties", [most, 33000, 700]), ("odd", [39000, 1499, 700]), ("same", [36000, 32768, 0]), ("sums", [33000, 8193, 1]))):
+        x = restore(kind)
+        dlens.copy_(torch.tensor(ls, dtype=torch.int32))
+        ws.fill_(0x7F + rep)
+        g.replay()
+        torch.cuda.synchronize()
+        got = result()
+        assert_evicted(got, br.evict(arrays, x, np.array(ls), table, out_table, budget, first, last))
+        score.copy_(dev(x))
+        step(torch.empty_like(keep), torch.empty_like(new_len))      # eager, between the replays
+        torch.cuda.synchronize()
+
+
+def test_calls_at_once_that_use_their_workspaces(B):
+    """Scores whose rows are cut into parts and evictions of long sequences, on two streams with dirty workspaces of their own."""
+    import torch
+    rng = np.random.default_rng(111)
+    hq, hkv, D, page, budget = 8, 1, 64, 64, 600
+    sides = []
+    for lens, qn in (([40000, 50], 400), ([35000, 33100, 900], 300)):
+        arrays, lens, table, out_table = evict_case(rng, lens, hkv, D, page, budget, 4)
+        n, L = len(lens), int(max(lens))
+        cu = np.arange(0, qn * n + 1, qn).astype(np.int32)
+        cache = make_cache(B, arrays, 4)
+        sizes = B.batq_kv_paged_score_workspace(cache, hq, n, qn * n, qn, L), B.batq_kv_paged_evict_workspace(cache, n, L, budget)
+        assert min(sizes) > 0
+        sides.append(dict(cache=cache, q=to_dev(ref.bf16_values(rng, qn * n, hq * D)[0], "bf16"), lse=torch.full((qn * n, hq), 9.0, device="cuda"),
+                          had=dev(scores_for(rng, "sums", (arrays[0].shape[0], hkv, page))), cu=dev(cu), lens=dev(lens), table=dev(table), out=dev(out_table),
+                          qn=qn, L=L, ws=[dirty(s, 0xFF) for s in sizes], stream=torch.cuda.Stream()))
+    small = dirty(256, 0)
+
+    def run(s, ws=None):
+        score, ws = s["had"].clone(), ws or s["ws"]
+        B.batq_kv_paged_score(s["cache"], s["q"], s["lse"], score, s["cu"], s["lens"], s["table"], s["qn"], s["L"], add=True, workspace=ws[0])
+        return (score,) + B.batq_kv_paged_evict(s["cache"], score, s["lens"], s["table"], s["out"], s["L"], budget, 1, 10, workspace=ws[1])
+
+    for s in sides:                                         # both calls take of their workspaces
+        with pytest.raises(B.BatqError):
+            run(s, [small, s["ws"][1]])
+        with pytest.raises(B.BatqError):
+            run(s, [s["ws"][0], small])
+    torch.cuda.synchronize()
+    want = [run(s) for s in sides]
+    torch.cuda.synchronize()
+    for rep in range(3):
+        got = []
+        for s in sides:
+            for w in s["ws"]:
+                w.fill_(0x55 + rep)
+            s["stream"].wait_stream(torch.cuda.current_stream())
+        for s in sides:
+            with torch.cuda.stream(s["stream"]):
+                got.append([run(s) for _ in range(3)][-1])
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for a, b in zip(got, want) for x, y in zip(a, b)), rep
