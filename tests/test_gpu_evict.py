@@ -886,3 +886,51 @@ def test_calls_at_once_that_use_their_workspaces(B):
                 got.append([run(s) for _ in range(3)][-1])
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for a, b in zip(got, want) for x, y in zip(a, b)), rep
+
+
+def test_plain_entry_points_are_those_of_eight_bits(B):
+    """batq_kv_paged_append and batq_paged_attention as a C program calls them (the binding takes the forms with a width), and
+    batq_kv_paged_score and batq_kv_paged_evict without a table of score pages: the bits of the others."""
+    import ctypes as C
+    import torch
+    from paper_2603_16590_amd.binding import _PagedBatch
+    rng = np.random.default_rng(121)
+    hq, hkv, D, page, budget = 4, 2, 128, 16, 50
+    lens, qs = [300, 77], [40, 1]
+    arrays, lens, table, out_table = evict_case(rng, lens, hkv, D, page, budget, 8)
+    cu, T = np.array([0, 40, 41], np.int32), 41
+    X = to_dev(ref.bf16_values(rng, T, (hq + 2 * hkv) * D)[0], "bf16")
+    q, k, v = X.split((hq * D, hkv * D, hkv * D), 1)
+    at = np.concatenate([lens[b] - qs[b] + np.arange(qs[b]) for b in range(2)])
+    owner = np.repeat([0, 1], qs)
+    slots = dev(table[owner, at // page].astype(np.int64) * page + at % page)
+    dcu, dlens, dtable, dout = dev(cu), dev(lens), dev(table), dev(out_table)
+    shape = (arrays[0].shape[0], hkv, page)
+    stream = torch.cuda.current_stream().cuda_stream
+    results = []
+    for plain in (False, True):
+        cache = make_cache(B, arrays, 8)
+        q_out, out = (torch.zeros((T, hq * D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        lse, score = torch.zeros((T, hq), device="cuda"), torch.zeros(shape, device="cuda")
+        keep, new_len = torch.zeros((2, hkv, budget), dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+        n = [B.batq_paged_attention_workspace(cache, hq, 2, T, 40, 300), B.batq_kv_paged_score_workspace(cache, hq, 2, T, 40, 300),
+             B.batq_kv_paged_evict_workspace(cache, 2, 300, budget)]
+        ws = dirty(max(n) + 256, 0xFF)
+        if plain:
+            c, b = C.byref(cache._d), C.byref(_PagedBatch(dcu.data_ptr(), dlens.data_ptr(), dtable.data_ptr(), 2, table.shape[1], T, 40, 300))
+            w = (ws.data_ptr(), ws.numel(), stream)
+            assert B.lib.batq_kv_paged_append(c, None, None, None, q.data_ptr(), q.stride(0), hq, q_out.data_ptr(), hq * D, k.data_ptr(), k.stride(0),
+                                              v.data_ptr(), v.stride(0), B.BF16, None, slots.data_ptr(), T, stream) == 0
+            assert B.lib.batq_paged_attention(c, b, q_out.data_ptr(), hq * D, hq, D ** -0.5, 1, 0, out.data_ptr(), hq * D, lse.data_ptr(), *w) == 0
+            assert B.lib.batq_kv_paged_score(c, 8, b, q_out.data_ptr(), hq * D, hq, D ** -0.5, 1, 0, lse.data_ptr(), score.data_ptr(), 0, *w) == 0
+            assert B.lib.batq_kv_paged_evict(c, 8, score.data_ptr(), dlens.data_ptr(), dtable.data_ptr(), table.shape[1], dout.data_ptr(), out_table.shape[1],
+                                             2, 300, budget, 2, 5, keep.data_ptr(), new_len.data_ptr(), *w) == 0
+        else:
+            B.batq_kv_paged_append(cache, k, v, slots, q=q, q_out=q_out)
+            B.batq_paged_attention(cache, q_out, dcu, dlens, dtable, 40, 300, out=out, lse=lse, workspace=ws)
+            B.batq_kv_paged_score(cache, q_out, lse, score, dcu, dlens, dtable, 40, 300, workspace=ws)
+            B.batq_kv_paged_evict(cache, score, dlens, dtable, dout, 300, budget, 2, 5, keep=keep, new_len=new_len, workspace=ws)
+        torch.cuda.synchronize()
+        results.append([q_out, out, lse, score, keep, new_len, cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales])
+    assert all(torch.equal(x, y) for x, y in zip(*results))
+    assert bool((results[0][4] >= 0).any()) and bool((results[0][1] != 0).any())
