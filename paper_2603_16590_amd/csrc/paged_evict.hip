@@ -155,8 +155,8 @@ __device__ __forceinline__ int sum_before(int c, int* all) {
     return before;
 }
 // 256 keys of a wave in order (lane l has tokens t .. t + 3): lists those above the border and, of those on it, the ones with fewer than
-// `left` before them.
-__device__ __forceinline__ void list_keys(const u32x4& u, int t, uint32_t border, int left, int* at, int* equal, int32_t* keep) {
+// `left` before them.  (More than `budget` only if scores or workspace are written to meanwhile: not behind the list then either.)
+__device__ __forceinline__ void list_keys(const u32x4& u, int t, uint32_t border, int left, int* at, int* equal, int32_t* keep, int budget) {
     bool stays[4], on = false;
     int c = 0;
 #pragma unroll
@@ -174,8 +174,10 @@ __device__ __forceinline__ void list_keys(const u32x4& u, int t, uint32_t border
 #pragma unroll
     for (int e = 0; e < 4; ++e) c += stays[e];
     int all;
-    int32_t* to = keep + *at + sum_before(c, &all);
+    const int before = sum_before(c, &all), begin = __builtin_amdgcn_readfirstlane(*at);
     *at += all;
+    if (begin < 0 || begin > budget - all) return;
+    int32_t* to = keep + begin + before;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
         if (stays[e]) *to++ = t + e;
@@ -224,7 +226,7 @@ select_kernel(const EvictArgs a) {
     __syncthreads();
     int equal = waves_before(s_eq, wave), at = waves_before(s_gt, wave) + min(equal, left);
     int32_t* const keep = a.keep + (size_t)pair * a.budget;
-    each([&](const u32x4& u, int t) { list_keys(u, t, f.bits, left, &at, &equal, keep); });
+    each([&](const u32x4& u, int t) { list_keys(u, t, f.bits, left, &at, &equal, keep, a.budget); });
 }
 
 // Long sequences of few pairs: a workgroup to a chunk of tokens, with a launch for every pass.  The histograms of all passes and the
@@ -313,7 +315,7 @@ team_list(const EvictArgs a) {
         int equal = s_before[1] + waves_before(s_eq, wave), at = s_before[0] + waves_before(s_gt, wave) + min(equal, left);
         int32_t* const keep = a.keep + (size_t)pair * a.budget;
 #pragma unroll
-        for (int k = 0; k < kChunkKeys / 4; ++k) list_keys(u[k], t0 + 256 * k, f.bits, left, &at, &equal, keep);
+        for (int k = 0; k < kChunkKeys / 4; ++k) list_keys(u[k], t0 + 256 * k, f.bits, left, &at, &equal, keep, a.budget);
     }
 }
 
@@ -329,14 +331,14 @@ move_kernel(const EvictArgs a) {
     const int tid = threadIdx.x;
     const int bh = blockIdx.x / a.chunks, j0 = (blockIdx.x % a.chunks) * kMove;
     const int h = bh % a.kv_heads, b = bh / a.kv_heads;
-    const int n = min(tokens_of(a, b), a.budget);
+    const int len = tokens_of(a, b), n = min(len, a.budget);
     if (j0 >= n) return;
     const int page_mask = (1 << a.page_shift) - 1;
     if (tid < kMove) {
         const int j = j0 + tid;
         int from = -1, to = -1;
         if (j < n) {
-            const int t = a.keep[(size_t)bh * a.budget + j];
+            const int t = min((uint32_t)a.keep[(size_t)bh * a.budget + j], (uint32_t)len - 1);      // (the caller's memory: not trusted)
             const size_t entry = (size_t)b * a.table_width + (t >> a.page_shift);
             from = a.page_table[entry];
             s_score[tid] = a.score_table[entry];

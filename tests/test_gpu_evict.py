@@ -934,3 +934,38 @@ def test_plain_entry_points_are_those_of_eight_bits(B):
         results.append([q_out, out, lse, score, keep, new_len, cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales])
     assert all(torch.equal(x, y) for x, y in zip(*results))
     assert bool((results[0][4] >= 0).any()) and bool((results[0][1] != 0).any())
+
+
+@pytest.mark.parametrize("L,alias", [(500, "new_len"), (40000, "new_len"), (40000, "workspace"), (500, "score")])
+def test_evict_stays_within_its_arrays(B, L, alias):
+    """Lists, lengths, scores and workspace that lie on each other make what is kept unspecified; nothing but the pages of out_table, and
+    what is handed over to be written, is written to."""
+    import torch
+    rng = np.random.default_rng(131 + L)
+    hkv, D, page, budget = 2, 64, 64, 1024 if L > 1000 else 192
+    arrays, lens, table, out_table = evict_case(rng, [L, L], hkv, D, page, budget, 4)
+    cache, pages = make_cache(B, arrays, 4), arrays[0].shape[0]
+    need = B.batq_kv_paged_evict_workspace(cache, 2, L, budget)
+    size = 2 * hkv * budget
+    words = max(pages * hkv * page, 4 * need, 8 * size)
+    store = torch.full((words + 2048,), 12345678, dtype=torch.int32, device="cuda")
+    at = 1024                                               # (4 KiB: the workspace's alignment)
+    score = store[at: at + pages * hkv * page].view(torch.float32).view(pages, hkv, page)
+    score.copy_(dev(scores_for(rng, "sums", tuple(score.shape))))
+    keep = torch.full((size + 2048,), 12345678, dtype=torch.int32, device="cuda")
+    kept = keep[1024: 1024 + size].view(2, hkv, budget)
+    new_len, ws = torch.zeros(2, dtype=torch.int32, device="cuda"), dirty(max(need, 256), 0xFF)
+    if alias == "new_len":
+        new_len = kept.view(-1)[budget - 1: budget + 1]     # in the middle of the lists
+    elif alias == "workspace":
+        ws = store[at: at + need // 4].view(torch.uint8)
+        assert need <= score.nbytes
+    else:
+        kept = store[at: at + size].view(2, hkv, budget)
+    B.batq_kv_paged_evict(cache, score, dev(lens), dev(table), dev(out_table), L, budget, 2, 5, keep=kept, new_len=new_len, workspace=ws)
+    torch.cuda.synchronize()
+    assert bool((store[:at] == 12345678).all()) and bool((store[at + pages * hkv * page:] == 12345678).all())
+    assert bool((keep[:1024] == 12345678).all()) and bool((keep[1024 + size:] == 12345678).all())
+    rest = np.setdiff1d(np.arange(pages), out_table)
+    for got, a in zip(host(cache), arrays):
+        assert np.array_equal(got[rest], a[rest])
