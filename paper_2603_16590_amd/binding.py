@@ -683,6 +683,12 @@ def _list(t, dtype, shape, dev: int, what: str) -> int:
     return t.data_ptr()
 
 
+def _fits(*numbers: int) -> None:
+    """Numbers that the library takes as 32-bit ones: ctypes would drop their high bits without a word."""
+    if max(numbers) > 0x7FFFFFFF:
+        raise ValueError(f"sizes and bounds have to be below 2^31, got {max(numbers)}")
+
+
 def _scratch(t, dev: int) -> int:
     if t.get_device() != dev or not t.is_contiguous():
         raise ValueError("workspace: expected a contiguous tensor on the current device")
@@ -760,6 +766,7 @@ def batq_kv_paged_append(cache: PagedCache, k, v, slots, positions=None, q=None,
 
 def batq_paged_attention_workspace(cache: PagedCache, q_heads: int, batch: int, total_q: int, max_q: int, max_kv: int) -> int:
     """Bytes of scratch that every batq_paged_attention call within these bounds can run with on the current device."""
+    _fits(q_heads, batch, total_q, max_q, max_kv)
     return int(lib.batq_paged_attention_workspace(C.byref(cache._d), q_heads, batch, total_q, max_q, max_kv))
 
 
@@ -771,6 +778,7 @@ def batq_paged_attention(cache: PagedCache, q, cu_q, kv_len, page_table, max_q: 
     import torch
     if q.dim() != 2 or page_table.dim() != 2:
         raise ValueError("expected q [total_q, q_heads * head_dim] and page_table [batch, width]")
+    _fits(max_q, max_kv, window)
     dev, D = _device(), cache.head_dim
     T, width = q.shape
     batch, table_width = page_table.shape
@@ -794,6 +802,7 @@ def batq_paged_attention(cache: PagedCache, q, cu_q, kv_len, page_table, max_q: 
 
 def batq_kv_paged_score_workspace(cache: PagedCache, q_heads: int, batch: int, total_q: int, max_q: int, max_kv: int) -> int:
     """Bytes of scratch that every batq_kv_paged_score call within these bounds can run with on the current device."""
+    _fits(q_heads, batch, total_q, max_q, max_kv)
     return int(lib.batq_kv_paged_score_workspace(C.byref(cache._d), q_heads, batch, total_q, max_q, max_kv))
 
 
@@ -819,6 +828,7 @@ def batq_kv_paged_score(cache: PagedCache, q, lse, score, cu_q, kv_len, page_tab
     import torch
     if q.dim() != 2 or page_table.dim() != 2:
         raise ValueError("expected q [total_q, q_heads * head_dim] and page_table [batch, width]")
+    _fits(max_q, max_kv, window)
     dev, D = _device(), cache.head_dim
     T, width = q.shape
     batch, table_width = page_table.shape
@@ -838,6 +848,7 @@ def batq_kv_paged_score(cache: PagedCache, q, lse, score, cu_q, kv_len, page_tab
 
 def batq_kv_paged_evict_workspace(cache: PagedCache, batch: int, max_kv: int, budget: int) -> int:
     """Bytes of scratch that every batq_kv_paged_evict call within these bounds can run with on the current device."""
+    _fits(batch, max_kv, budget)
     return int(lib.batq_kv_paged_evict_workspace(C.byref(cache._d), batch, max_kv, budget))
 
 
@@ -851,6 +862,7 @@ def batq_kv_paged_evict(cache: PagedCache, score, kv_len, page_table, out_table,
     import torch
     if page_table.dim() != 2 or out_table.dim() != 2:
         raise ValueError("expected page_table [batch, width] and out_table [batch, out width]")
+    _fits(max_kv, budget, first, last)
     dev = _device()
     (batch, table_width), out_width = page_table.shape, out_table.shape[1]
     if keep is None:

@@ -126,3 +126,22 @@ def test_score_tables_are_looked_at(B):
     assert evict_ex(2 * P, ok.num_pages) == 2               # the table that the tokens move to
     assert B.lib.batq_kv_paged_score_ex(None, 4, C.byref(b), P, 256, 4, 0.1, 1, 0, P, P, None, 4, 0, None, 0, None) == 1
     assert B.lib.batq_kv_paged_evict_ex(None, 4, P, None, 4, P, P, 3, 2 * P, 2, 2, 48, 20, 1, 2, P, 2 * P, None, 0, None) == 1
+
+
+def test_numbers_past_32_bits_are_not_cut(B):
+    """2^32 + 5 is no bound of 5, and a window of 2^32 is not none."""
+    import torch
+    q, table, far = torch.zeros((1, 64)), torch.zeros((1, 2), dtype=torch.int32), (1 << 32) + 5
+    for kw in (dict(max_q=far, max_kv=5), dict(max_q=1, max_kv=far), dict(max_q=1, max_kv=5, window=1 << 32)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            B.batq_paged_attention(None, q, None, None, table, **kw)
+        with pytest.raises(ValueError, match="2\\^31"):
+            B.batq_kv_paged_score(None, q, None, None, None, None, table, **kw)
+    good = dict(max_kv=5, budget=4, first=1, last=1)
+    for name in good:
+        with pytest.raises(ValueError, match="2\\^31"):
+            B.batq_kv_paged_evict(None, None, None, table, table, **{**good, name: far})
+    for f, n in ((B.batq_paged_attention_workspace, 5), (B.batq_kv_paged_score_workspace, 5), (B.batq_kv_paged_evict_workspace, 3)):
+        for i in range(n):
+            with pytest.raises(ValueError, match="2\\^31"):
+                f(None, *[far if k == i else 1 for k in range(n)])
