@@ -685,8 +685,11 @@ def _list(t, dtype, shape, dev: int, what: str) -> int:
 
 def _fits(*numbers: int) -> None:
     """Numbers that the library takes as 32-bit ones: ctypes would drop their high bits without a word."""
-    if max(numbers) > 0x7FFFFFFF:
+    if max(numbers) > _INT_MAX:
         raise ValueError(f"sizes and bounds have to be below 2^31, got {max(numbers)}")
+
+
+_INT_MAX = 0x7FFFFFFF                                       # (calls look at all of their numbers at once first)
 
 
 def _scratch(t, dev: int) -> int:
@@ -778,7 +781,8 @@ def batq_paged_attention(cache: PagedCache, q, cu_q, kv_len, page_table, max_q: 
     import torch
     if q.dim() != 2 or page_table.dim() != 2:
         raise ValueError("expected q [total_q, q_heads * head_dim] and page_table [batch, width]")
-    _fits(max_q, max_kv, window)
+    if (max_q | max_kv | window) > _INT_MAX:
+        _fits(max_q, max_kv, window)
     dev, D = _device(), cache.head_dim
     T, width = q.shape
     batch, table_width = page_table.shape
@@ -828,7 +832,8 @@ def batq_kv_paged_score(cache: PagedCache, q, lse, score, cu_q, kv_len, page_tab
     import torch
     if q.dim() != 2 or page_table.dim() != 2:
         raise ValueError("expected q [total_q, q_heads * head_dim] and page_table [batch, width]")
-    _fits(max_q, max_kv, window)
+    if (max_q | max_kv | window) > _INT_MAX:
+        _fits(max_q, max_kv, window)
     dev, D = _device(), cache.head_dim
     T, width = q.shape
     batch, table_width = page_table.shape
@@ -862,7 +867,8 @@ def batq_kv_paged_evict(cache: PagedCache, score, kv_len, page_table, out_table,
     import torch
     if page_table.dim() != 2 or out_table.dim() != 2:
         raise ValueError("expected page_table [batch, width] and out_table [batch, out width]")
-    _fits(max_kv, budget, first, last)
+    if (max_kv | budget | first | last) > _INT_MAX:
+        _fits(max_kv, budget, first, last)
     dev = _device()
     (batch, table_width), out_width = page_table.shape, out_table.shape[1]
     if keep is None:
