@@ -522,6 +522,8 @@ batq_status batq_paged_attention_ex(const batq_paged_cache* cache, int cache_bit
  * on, say) beside pages that it shares.
  *   workspace   DEVICE, 256-byte aligned, its contents need not be cleared, one for calls that may run at the same time each;
  *               batq_kv_paged_score_workspace() bytes are enough for every call of at most that batch, total_q, max_q and max_kv
+ * Work is planned for max_kv: far above the lengths it costs time, here as in the attention and the eviction (64 sequences of up to 8192 tokens:
+ * 19 us with max_kv 8192, 45 with 131072), so that a captured step for each range of lengths pays.
  * BATQ_ERR_SHAPE: also for batch * kv_heads * (max_kv / 256 + 1) from 2^24 on. */
 size_t batq_kv_paged_score_workspace(const batq_paged_cache* cache, int q_heads, int batch, int total_q, int max_q, int max_kv);
 batq_status batq_kv_paged_score(const batq_paged_cache* cache, int cache_bits, const batq_paged_batch* b, const void* q,

@@ -183,7 +183,7 @@ __device__ __forceinline__ void list_keys(const u32x4& u, int t, uint32_t border
         if (stays[e]) *to++ = t + e;
 }
 
-// A workgroup to a (sequence, key head): latencies and the vector instructions of one compute unit (32 pairs of 32768 tokens 22 us, 512 of 2112
+// A workgroup to a (sequence, key head): latencies and the vector instructions of one compute unit (32 pairs of 32768 tokens 23 us, 512 of 2112
 // 16.6 us; read in every pass, key by key, 99 us).  KEYS > 0: up to KEYS keys a thread, read once and held in registers; 0: read in every pass.
 // A wave has a run of neighbouring tokens.  Copies of the histogram keep lanes with equal bits apart (most scores share their exponent).
 template <int KEYS>

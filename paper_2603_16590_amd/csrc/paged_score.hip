@@ -61,7 +61,8 @@ __device__ __forceinline__ void store_score(const ScoreArgs& a, const Seq& s, in
 // (l % 16, l / 16) loads channels [g D/4, (g + 1) D/4) of tokens 2n and 2n + 1 (the order in which a product runs over channels is
 // free), and element r of its results of tile x is row 16x + 4g + r: a token's sum is one over elements and four lanes.
 // Blocks that no row sees are left out (64 x 8192 tokens behind a window of 1024: 17 us beside 65; 1 x 131072: 9.6 beside 19).
-// OWN: with a table of the scores' pages (which costs the ragged batch 2 us: registers, an exchange a block).
+// OWN: with a table of the scores' pages (ragged batch 19.8 us beside 19.5 in a graph; looked at in one kernel for both, calls without one
+// took 22.8 instead of 20.6).
 template <int D, int NT, int BITS, bool OWN>
 __global__ void __launch_bounds__(256)
 score_few(const ScoreArgs a) {
